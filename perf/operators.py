@@ -21,6 +21,9 @@ The shapes are those of this repository's workloads: Llama-style layers of
 the 350M and 1B models, a 7B matrix, the 1024 x 1024 linear layer, and ragged
 ones.  Gradients are a rank of 16 over noise, as those of a matrix are;
 pseudo gradients are noise of the workers' own scales, as in the other cases.
+The replicas of the outer cases are fp32: a second step right after the first
+has no pseudo gradient then, where with bf16 replicas it would step along the
+rounding errors of theta, which no two orders of summation agree on.
 """
 import torch
 
@@ -64,16 +67,16 @@ def listed():
         _case("local-1b-bf16", "local_step", "bf16", LAYER_1B, vectors=4096),
         # The 1024 x 1024 linear layer with four workers, one of them anomalous.
         _case("outer-linear1m-k4-f32", "outer_step", "f32", "1024x1024", k=4, anomalous=1),
-        # The outer step of a 350M layer, eight bf16 workers.
-        _case("outer-350m-k8-bf16", "outer_step", "bf16", LAYER_350M, vectors=2048, k=8),
-        # The outer step of a 1B layer, eight bf16 workers, one of them anomalous.
-        _case("outer-1b-k8-bf16", "outer_step", "bf16", LAYER_1B, vectors=4096, k=8, anomalous=1),
+        # The outer step of a 350M layer, eight workers.
+        _case("outer-350m-k8-f32", "outer_step", "f32", LAYER_350M, vectors=2048, k=8),
+        # The outer step of a 1B layer, eight workers, one of them anomalous.
+        _case("outer-1b-k8-f32", "outer_step", "f32", LAYER_1B, vectors=4096, k=8, anomalous=1),
     ]
 
 
 def draw(rng):
     op = rng.choice(["orthogonalize", "orthogonalize", "local_step", "local_step", "outer_step"])
-    dtype = rng.choice(["bf16", "bf16", "f32"])
+    dtype = rng.choice(["bf16", "bf16", "f32"]) if op != "outer_step" else "f32"
     k = rng.choice([2, 3, 4, 5, 8, 8, 16]) if op == "outer_step" else 0
     most = 6.0e11 if op == "orthogonalize" else 4.0e11  # multiply-adds of the plain products, of 2.2e12 listed
     hidden = int(32 * (4096 / 32) ** rng.random())
