@@ -356,6 +356,104 @@ edit_status_t edit_group_state_get(edit_group_t h, int32_t layer, edit_layer_sta
 edit_status_t edit_group_state_set(edit_group_t h, int32_t layer, const edit_layer_state_t *in);
 void edit_group_destroy(edit_group_t h);
 
+/* ---- orthogonalised updates -------------------------------------------- */
+
+/* Optimizers that step a matrix along its orthogonalised update (Muon):
+ * every matrix U of an update becomes O(U), the result of a few Newton-Schulz
+ * products that bring its singular values near one and keep its singular
+ * vectors,
+ *
+ *     X <- U / ||U||_F;     steps times:  A = X X^T,  X <- a X + (b A + c A^2) X
+ *
+ * (on X^T where rows > cols, so that A has the smaller side; a matrix of
+ * zeros gives zeros).  The paper leaves OuterOpt (Algorithm 2) and the
+ * workers' local optimizer open; the calls below offer O(U) by itself, as a
+ * worker's local step, and as the OuterOpt of the outer step.
+ *
+ * A handle serves one sync unit layout: `numel` elements, stored flat as
+ * everywhere in this library, of which each matrix takes rows * cols
+ * consecutive ones from `offset` on, row by row.  Matrices may begin anywhere
+ * (no alignment) and must not overlap; elements of no matrix (gains, biases)
+ * are treated as each call says.  A matrix with zero rows or columns is
+ * skipped.  A NaN or an infinity in a matrix makes its whole O NaN and leaves
+ * the other matrices alone.
+ *
+ * Precision.  Products run on the fp16 matrix cores with fp32 sums.  X is held
+ * to 22 bits as the sum of two fp16 values, and A is taken about its mean
+ * diagonal.  EDIT_ORTHO_FAST multiplies the high halves only: O is off by 1e-4
+ * to 1e-3 of its norm (an iteration rounded to bf16 is off by 1e-2 to 9e-2).
+ * EDIT_ORTHO_FULL takes three products (high*high, high*low, low*high) and is
+ * off by as much as an fp32 iteration, at 2.2 to 2.8 times the time.
+ * Norms are summed in fp64, steps are taken in fp64 and rounded once.  Results
+ * are the same bit for bit on every run.
+ *
+ * The handle owns its workspace (14 to 16 bytes per element of a square
+ * matrix, with FULL 20 to 22), made by edit_ortho_init; the calls allocate
+ * nothing, do not synchronise and can be captured into HIP graphs.  Calls on
+ * one handle, replays of graphs that hold them included, use the same
+ * workspace and must not overlap: order them on one stream or with events. */
+#define EDIT_ORTHO_MAX_STEPS 32
+
+typedef enum { EDIT_ORTHO_FAST = 0, EDIT_ORTHO_FULL = 1 } edit_ortho_precision_t;
+
+typedef struct {
+  int64_t offset;     /* first element in the unit                              */
+  int32_t rows, cols; /* row-major; each up to 2^24, rows * cols up to 2^30     */
+  double scale;       /* factor s of O in the steps, e.g. sqrt(max(1, rows/cols)) */
+} edit_ortho_matrix_t;
+
+typedef struct {
+  int64_t numel;                       /* elements of the unit, >= 0            */
+  const edit_ortho_matrix_t *matrices; /* [num_matrices]; copied at init        */
+  int32_t num_matrices;                /* >= 0                                  */
+  int32_t dtype;                       /* edit_dtype_t of x, out, param, grad   */
+  int32_t precision;                   /* edit_ortho_precision_t                */
+  int32_t steps;                       /* Newton-Schulz steps, 1..EDIT_ORTHO_MAX_STEPS */
+  const double *coefficients;          /* [steps * 3] a, b, c of each step; NULL: */
+                                       /* 3.4445, -4.7750, 2.0315 for all      */
+} edit_ortho_config_t;
+
+typedef struct edit_ortho *edit_ortho_t; /* opaque, library-owned */
+
+/* Create a handle on the current device.  EDIT_EINVAL for a bad layout, type
+ * or step count, a scale that is not finite, and for coefficients that are not
+ * finite or take a singular value from [0, 1] beyond 4, or the polynomial a +
+ * b x + c x^2 on the way beyond 15 (fp16 holds no more); EDIT_ENODEV off
+ * gfx950, EDIT_ENOMEM. */
+edit_status_t edit_ortho_init(const edit_ortho_config_t *cfg, edit_ortho_t *out);
+
+/* out = O(x) for every matrix, both [numel] of the handle's type.  Elements of
+ * no matrix are neither read nor written.  `out` may be `x`; otherwise they
+ * must not overlap.  16-byte aligned device pointers, here and below. */
+edit_status_t edit_ortho_apply(edit_ortho_t h, const void *x, void *out, void *stream);
+
+/* One local step of a worker on the matrices of its replica:
+ *     m <- mu m + g;    u = g + mu m (nesterov != 0) or m;
+ *     p <- (1 - lr * weight_decay) p - lr s O(u)
+ * param p and grad g of the handle's type, momentum m fp32 (zero at first).
+ * Elements of no matrix are neither read nor written (another optimizer
+ * steps them).  The three must not overlap.  EDIT_EINVAL for a mu outside
+ * [0, 1) and for lr or weight_decay that are negative or not finite. */
+edit_status_t edit_ortho_local_step(edit_ortho_t h, void *param, const void *grad, float *momentum, double lr,
+                                    double mu, double weight_decay, int32_t nesterov, void *stream);
+
+/* One outer step of unit `layer` as edit_outer_step_layer takes it (norms,
+ * z-test, EMA, weights, clip, rollback, state_get), with the matrices of
+ * `ortho` stepped along their orthogonalised Nesterov direction:
+ *     b' = rho b + g,  g = -beta Delta_bar;
+ *     theta' = theta - nu s O(g + rho b')       (matrices)
+ *     theta' = theta - nu (g + rho b')          (other elements)
+ * and every replica set to theta'.  O has no magnitude of its own, so beta
+ * acts through the momentum only, and nu is the step's size.  `ortho`'s numel
+ * must be the unit's and its device the handle's; its dtype does not matter
+ * here.  Not available with EDIT_ONE_PASS.  Otherwise arguments, ownership
+ * and errors as in edit_outer_step_layer. */
+edit_status_t edit_outer_step_layer_ortho(edit_outer_t h, int32_t layer, edit_ortho_t ortho, float *theta,
+                                          float *momentum, void *const *replicas, void *stream);
+
+/* Release the workspace (waits for the device's pending work). */
+void edit_ortho_destroy(edit_ortho_t h);
+
 /* ---- measurement helpers (not part of the method) ---------------------- */
 
 /* every > 0: steps of units whose index is a multiple of `every` record HIP

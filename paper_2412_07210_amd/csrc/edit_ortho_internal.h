@@ -1,0 +1,111 @@
+// Internal declarations of the orthogonalised updates (edit_ortho_* and
+// edit_outer_step_layer_ortho), shared by edit_ortho_kernels.hip and
+// edit_ortho_runtime.hip.  Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "edit_outer.h"
+#include "edit_outer_internal.h"
+
+namespace edit {
+
+// Powers of two that the fp16 operands are stored at, so that neither their
+// high nor their low halves leave fp16's range: X (entries up to its largest
+// singular value, about 1) at kScaleX, A - sI and the polynomial at kScaleA.
+// The low half of a value v is v's rounding error, about v / 4096; fp16 keeps
+// it down to 2^-24 / scale.
+constexpr float kScaleX = 8192.f;
+constexpr float kScaleA = 2048.f;
+// The largest |sigma| and |polynomial| that the scales leave room for
+// (65504 / 8192 and 65504 / 2048 / 2, the difference of two of its values).
+constexpr double kMaxSigma = 4.0;
+constexpr double kMaxPoly = 15.0;
+
+constexpr int kOrthoPad = 64;           // leading dimensions are multiples of this (zero behind the matrix)
+constexpr int kOrthoStreamThreads = 256;
+constexpr int kOrthoMaxChunks = 512;    // chunks (norm partials) of one matrix
+constexpr int kOrthoLoadTile = 64;      // side of the load pass's tiles
+
+// One matrix of a unit: r = min(rows, cols), c = max(rows, cols).  The
+// working matrix X is r x c: the stored one, or its transpose where rows >
+// cols.  Every array is zero behind its r or c columns.
+struct OrthoMat {
+  _Float16* x[2];     // X, high and low halves                          [r][ldc]
+  _Float16* t[2][2];  // X^T, [buffer][high, low]                        [c][ldr]
+  _Float16* g[2];     // R = A - sI                                      [r][ldr]
+  _Float16* q[2];     // (b + 2cs) R + c R^2                             [r][ldr]
+  double* norm_part;  // sums of squares of the update's chunks
+  double* x_part;     // sums of squares of the X tiles of the last product
+  double* shift;      // s of this iteration
+  int64_t offset;     // of the matrix in the unit
+  double scale;       // its factor in a step
+  int32_t rows, cols, r, c, ldr, ldc;
+  int32_t chunks, x_tiles;
+  int32_t tall;       // rows > cols: X is the stored matrix transposed
+  int32_t pad_;
+};
+
+// Elements [begin, end) of the unit: of matrix `mat`, partial `slot`; of no
+// matrix with mat = -1.
+struct OrthoChunk {
+  int64_t begin, end;
+  int32_t mat, slot;
+};
+
+// Tile (m, n) of a matrix; mat = -1: none.
+struct OrthoTile {
+  int32_t mat, m, n, slot;
+};
+
+// What the update of a call is made from.
+enum OrthoSource { kSourcePlain = 0, kSourceLocal = 1, kSourceOuter = 2 };
+
+struct OrthoCall {
+  OrthoSource source;
+  bool bf16;            // type of x / out, param / grad or the replicas
+  const void* x;        // plain: the update;  local: the gradient
+  void* out;            // plain: the result;  local: the parameters
+  float* momentum;      // local, outer
+  float* theta;         // outer
+  float* u;             // [numel] scratch: outer's update, and every call's O in the end
+  void* const* reps;    // outer: K replicas (host array)
+  const UnitRecord* rec;
+  int32_t workers;
+  int32_t nesterov;     // local
+  double mu, keep, lr;  // momentum; 1 - lr * decay; step length
+};
+
+struct OrthoCoef {
+  double a, b, c;
+};
+
+// Products of an iteration.
+enum OrthoProduct { kProductGram = 0, kProductSquare = 1, kProductUpdate = 2 };
+
+struct OrthoTiles {
+  const OrthoTile* tile;  // device
+  int32_t count;
+};
+
+// Pass over the update: momentum and update of the call, and the chunks' sums of squares.
+hipError_t launch_ortho_source(const OrthoCall& call, const OrthoMat* mats, const OrthoChunk* chunks, int count,
+                               hipStream_t stream);
+// X and X^T of the update over its norm.
+hipError_t launch_ortho_load(bool full, const OrthoCall& call, const OrthoMat* mats, const OrthoTile* tiles, int count,
+                             hipStream_t stream);
+// One product of an iteration; `side`: of its tiles, `from`: the X^T buffer read, `last`: O to `u` instead of X.
+hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const OrthoMat* mats, const OrthoTiles& tiles,
+                                const OrthoCoef& coef, int from, bool first, bool last, float* u, hipStream_t stream);
+// The call's outputs from O.
+hipError_t launch_ortho_apply(const OrthoCall& call, const OrthoMat* mats, const OrthoChunk* chunks, int count,
+                              hipStream_t stream);
+
+// The outer step's part of a handle: its argument check and, after the
+// decision has been enqueued, the orthogonalised update (edit_ortho_runtime.hip).
+edit_status_t check_ortho_unit(const edit_ortho* h, int64_t numel, int device);
+edit_status_t enqueue_ortho_outer(edit_ortho* h, bool bf16, float* theta, float* momentum, void* const* replicas,
+                                  int workers, const UnitRecord* rec, double lr, double rho, hipStream_t stream);
+
+}  // namespace edit

@@ -1,0 +1,434 @@
+// Host runtime of the orthogonalised updates (include/edit_outer.h,
+// "orthogonalised updates").
+//
+// A handle owns, for one unit layout, a workspace for every matrix and the
+// tables its launches run over: chunks of the unit for the streaming passes,
+// tiles of all matrices for the products.  A call enqueues source -> load ->
+// steps x (gram, square, update) -> apply on the caller's stream.
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <new>
+#include <string>
+#include <vector>
+
+#include "edit_group_internal.h"
+#include "edit_ortho_internal.h"
+
+using namespace edit;
+
+namespace {
+
+#define ORTHO_TRY(expr)               \
+  do {                                \
+    const edit_status_t st_ = (expr); \
+    if (st_ != EDIT_OK) return st_;   \
+  } while (0)
+
+edit_status_t ofail(edit_status_t s, const std::string& msg) { return set_error(s, msg.c_str()); }
+
+edit_status_t ofail_hip(hipError_t e, const char* what) {
+  return ofail(EDIT_EHIP, std::string(what) + ": " + hipGetErrorString(e));
+}
+
+int64_t oceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t oround_up(int64_t a, int64_t b) { return oceil_div(a, b) * b; }
+
+constexpr double kDefaultCoef[3] = {3.4445, -4.7750, 2.0315};
+constexpr int64_t kMaxSide = int64_t(1) << 24;
+constexpr int64_t kMaxMatrix = int64_t(1) << 30;
+constexpr int kXcds = 8;                          // workgroups go to the XCDs in turn
+constexpr int kProductSide = 128;
+
+struct Tables {
+  std::vector<OrthoMat> mats;
+  std::vector<OrthoChunk> chunks;
+  int matrix_chunks = 0;  // the first ones belong to matrices
+  std::vector<OrthoTile> load, gram, update;
+};
+
+}  // namespace
+
+struct edit_ortho {
+  int64_t numel = 0;
+  bool bf16 = false, full = false;
+  int device = 0;
+  std::vector<OrthoCoef> coef;
+  char* arena = nullptr;
+  OrthoMat* mats = nullptr;
+  OrthoChunk* chunks = nullptr;
+  int matrix_chunks = 0, all_chunks = 0;
+  OrthoTile* load = nullptr;
+  int load_tiles = 0;
+  OrthoTiles gram{}, update{};
+  float* u = nullptr;
+};
+
+namespace {
+
+// Singular values start within [0, 1] (the Frobenius norm is 1); their images
+// and the polynomial have to stay within what the fp16 scales leave room for.
+edit_status_t check_coefficients(const std::vector<OrthoCoef>& coef) {
+  double top = 1.0;
+  for (size_t k = 0; k < coef.size(); ++k) {
+    const OrthoCoef& q = coef[k];
+    const std::string where = "coefficients of step " + std::to_string(k);
+    if (!std::isfinite(q.a) || !std::isfinite(q.b) || !std::isfinite(q.c))
+      return ofail(EDIT_EINVAL, where + " must be finite");
+    constexpr int kGrid = 4096;
+    double next = 0.0, poly = 0.0;
+    for (int i = 0; i <= kGrid; ++i) {
+      const double s = top * i / kGrid, x = s * s, p = q.a + q.b * x + q.c * x * x;
+      poly = std::max(poly, std::fabs(p));
+      next = std::max(next, std::fabs(s * p));
+    }
+    if (!(poly <= kMaxPoly)) return ofail(EDIT_EINVAL, where + ": |a + b x + c x^2| exceeds 15");
+    if (!(next <= kMaxSigma)) return ofail(EDIT_EINVAL, where + " take a singular value beyond 4");
+    top = next;
+  }
+  return EDIT_OK;
+}
+
+edit_status_t check_layout(const edit_ortho_config_t* cfg) {
+  if (cfg->numel < 0) return ofail(EDIT_EINVAL, "numel must be >= 0");
+  if (cfg->num_matrices < 0) return ofail(EDIT_EINVAL, "num_matrices must be >= 0");
+  if (cfg->num_matrices > 0 && !cfg->matrices) return ofail(EDIT_EINVAL, "matrices must not be NULL");
+  if (cfg->dtype != EDIT_F32 && cfg->dtype != EDIT_BF16)
+    return ofail(EDIT_EINVAL, "dtype must be EDIT_F32 or EDIT_BF16");
+  if (cfg->precision != EDIT_ORTHO_FAST && cfg->precision != EDIT_ORTHO_FULL)
+    return ofail(EDIT_EINVAL, "precision must be EDIT_ORTHO_FAST or EDIT_ORTHO_FULL");
+  if (cfg->steps < 1 || cfg->steps > EDIT_ORTHO_MAX_STEPS)
+    return ofail(EDIT_EINVAL, "steps must be in 1.." + std::to_string(EDIT_ORTHO_MAX_STEPS));
+  std::vector<std::pair<int64_t, int64_t>> used;
+  for (int i = 0; i < cfg->num_matrices; ++i) {
+    const edit_ortho_matrix_t& m = cfg->matrices[i];
+    const std::string where = "matrix " + std::to_string(i);
+    if (m.rows < 0 || m.cols < 0) return ofail(EDIT_EINVAL, where + ": rows and cols must be >= 0");
+    if (m.rows > kMaxSide || m.cols > kMaxSide) return ofail(EDIT_EINVAL, where + ": rows and cols must be at most 2^24");
+    const int64_t n = static_cast<int64_t>(m.rows) * m.cols;
+    // Padding to multiples of 64 at most doubles a side above 64, and 64 sides
+    // of 2^24 are 2^30: byte offsets within a matrix stay below 2^32.
+    if (n > kMaxMatrix) return ofail(EDIT_EINVAL, where + " is too large");
+    if (m.offset < 0 || m.offset > cfg->numel || n > cfg->numel - m.offset)
+      return ofail(EDIT_EINVAL, where + " reaches beyond the unit");
+    if (!std::isfinite(m.scale)) return ofail(EDIT_EINVAL, where + ": scale must be finite");
+    if (n) used.push_back({m.offset, m.offset + n});
+  }
+  std::sort(used.begin(), used.end());
+  for (size_t i = 1; i < used.size(); ++i)
+    if (used[i].first < used[i - 1].second) return ofail(EDIT_EINVAL, "matrices must not overlap");
+  return EDIT_OK;
+}
+
+// The tiles of all matrices, so that the workgroups of an XCD (every eighth)
+// take neighbouring tiles of a matrix, whose operands they share in its L2;
+// matrices with the longest sums first, so that short ones fill the end.
+std::vector<OrthoTile> spread(const std::vector<std::vector<OrthoTile>>& of_matrix, const std::vector<int>& order) {
+  std::vector<OrthoTile> list[kXcds];
+  int turn = 0;  // matrices of few tiles start on different XCDs
+  for (int m : order) {
+    const std::vector<OrthoTile>& t = of_matrix[m];
+    const size_t n = t.size();
+    for (int x = 0; x < kXcds; ++x) {
+      std::vector<OrthoTile>& to = list[(x + turn) % kXcds];
+      to.insert(to.end(), t.begin() + n * x / kXcds, t.begin() + n * (x + 1) / kXcds);
+    }
+    turn = (turn + static_cast<int>(n % kXcds)) % kXcds;
+  }
+  size_t longest = 0;
+  for (const auto& l : list) longest = std::max(longest, l.size());
+  std::vector<OrthoTile> out;
+  for (size_t i = 0; i < longest; ++i)
+    for (const auto& l : list) out.push_back(i < l.size() ? l[i] : OrthoTile{-1, 0, 0, 0});
+  while (!out.empty() && out.back().mat < 0) out.pop_back();
+  return out;
+}
+
+// [begin, end) in about `most` chunks at most, cut at whole vectors.
+void add_chunks(std::vector<OrthoChunk>& out, int64_t begin, int64_t end, int mat, int most, int* count) {
+  constexpr int64_t kUnit = 2048;
+  const int64_t size = std::max(4 * kUnit, oround_up(oceil_div(end - begin, most), kUnit));
+  int slot = 0;
+  for (int64_t at = begin; at < end;) {
+    const int64_t to = std::min(end, at / kUnit * kUnit + size);
+    out.push_back({at, to, mat, slot++});
+    at = to;
+  }
+  if (count) *count = slot;
+}
+
+Tables make_tables(const edit_ortho_config_t* cfg) {
+  Tables t;
+  std::vector<std::pair<int64_t, int64_t>> used;
+  std::vector<std::vector<OrthoTile>> gram, update;
+  for (int i = 0; i < cfg->num_matrices; ++i) {
+    const edit_ortho_matrix_t& in = cfg->matrices[i];
+    if (in.rows == 0 || in.cols == 0) continue;
+    const int k = static_cast<int>(t.mats.size());
+    OrthoMat m = {};
+    m.offset = in.offset;
+    m.scale = in.scale;
+    m.rows = in.rows, m.cols = in.cols;
+    m.r = std::min(in.rows, in.cols), m.c = std::max(in.rows, in.cols);
+    m.ldr = static_cast<int32_t>(oround_up(m.r, kOrthoPad)), m.ldc = static_cast<int32_t>(oround_up(m.c, kOrthoPad));
+    m.tall = in.rows > in.cols;
+    const int64_t end = in.offset + static_cast<int64_t>(in.rows) * in.cols;
+    used.push_back({in.offset, end});
+    add_chunks(t.chunks, in.offset, end, k, kOrthoMaxChunks, &m.chunks);
+    for (int32_t a = 0; a < oceil_div(in.rows, kOrthoLoadTile); ++a)
+      for (int32_t b = 0; b < oceil_div(in.cols, kOrthoLoadTile); ++b) t.load.push_back({k, a, b, 0});
+    const int32_t tr = static_cast<int32_t>(oceil_div(m.r, kProductSide)), tc = static_cast<int32_t>(oceil_div(m.c, kProductSide));
+    gram.emplace_back();
+    for (int32_t a = 0; a < tr; ++a)
+      for (int32_t b = 0; b <= a; ++b) gram.back().push_back({k, a, b, 0});
+    update.emplace_back();
+    for (int32_t a = 0; a < tc; ++a)
+      for (int32_t b = 0; b < tr; ++b) update.back().push_back({k, a, b, m.x_tiles++});
+    t.mats.push_back(m);
+  }
+  t.matrix_chunks = static_cast<int>(t.chunks.size());
+  std::sort(used.begin(), used.end());
+  int64_t at = 0;
+  used.push_back({cfg->numel, cfg->numel});
+  for (const auto& [lo, hi] : used) {
+    if (lo > at) add_chunks(t.chunks, at, lo, -1, INT_MAX, nullptr);
+    at = hi;
+  }
+  std::vector<int> order(t.mats.size());
+  for (size_t i = 0; i < order.size(); ++i) order[i] = static_cast<int>(i);
+  std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return t.mats[a].c > t.mats[b].c; });
+  t.gram = spread(gram, order);
+  std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return t.mats[a].r > t.mats[b].r; });
+  t.update = spread(update, order);
+  return t;
+}
+
+// Hands out 256-byte aligned pieces of the arena; with no arena it counts.
+struct Carver {
+  char* base;
+  size_t at = 0;
+  template <typename T>
+  T* take(size_t count) {
+    const size_t here = at;
+    at += (count * sizeof(T) + 255) & ~size_t(255);
+    return base ? reinterpret_cast<T*>(base + here) : nullptr;
+  }
+};
+
+size_t lay_out(edit_ortho* h, Tables& t, char* base) {
+  Carver c{base};
+  for (OrthoMat& m : t.mats) {
+    const size_t x = static_cast<size_t>(m.r) * m.ldc, xt = static_cast<size_t>(m.c) * m.ldr,
+                 a = static_cast<size_t>(m.r) * m.ldr;
+    for (auto& p : m.x) p = c.take<_Float16>(x);
+    for (auto& b : m.t) {
+      b[0] = c.take<_Float16>(xt);
+      b[1] = h->full ? c.take<_Float16>(xt) : nullptr;
+    }
+    for (auto& p : m.g) p = c.take<_Float16>(a);
+    m.q[0] = c.take<_Float16>(a);
+    m.q[1] = h->full ? c.take<_Float16>(a) : nullptr;
+    m.norm_part = c.take<double>(m.chunks);
+    m.x_part = c.take<double>(m.x_tiles);
+    m.shift = c.take<double>(1);
+  }
+  h->u = c.take<float>(static_cast<size_t>(h->numel));
+  h->mats = c.take<OrthoMat>(t.mats.size());
+  h->chunks = c.take<OrthoChunk>(t.chunks.size());
+  h->load = c.take<OrthoTile>(t.load.size());
+  OrthoTile* gram = c.take<OrthoTile>(t.gram.size());
+  OrthoTile* update = c.take<OrthoTile>(t.update.size());
+  h->gram = {gram, static_cast<int32_t>(t.gram.size())};
+  h->update = {update, static_cast<int32_t>(t.update.size())};
+  h->matrix_chunks = t.matrix_chunks;
+  h->all_chunks = static_cast<int>(t.chunks.size());
+  h->load_tiles = static_cast<int>(t.load.size());
+  return c.at;
+}
+
+template <typename T>
+hipError_t upload(const T* to, const std::vector<T>& from) {
+  if (from.empty()) return hipSuccess;
+  return hipMemcpy(const_cast<T*>(to), from.data(), from.size() * sizeof(T), hipMemcpyHostToDevice);
+}
+
+edit_status_t check_ortho_device(const edit_ortho* h) {
+  int dev = -1;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return ofail_hip(e, "hipGetDevice");
+  if (dev != h->device)
+    return ofail(EDIT_EINVAL, "call made with device " + std::to_string(dev) +
+                                  " current; the handle belongs to device " + std::to_string(h->device));
+  return EDIT_OK;
+}
+
+edit_status_t check_buffer(const void* p, const char* name) {
+  if (!p) return ofail(EDIT_EINVAL, std::string(name) + " must not be NULL");
+  if (reinterpret_cast<uintptr_t>(p) & 15u) return ofail(EDIT_EINVAL, std::string(name) + " must be 16-byte aligned");
+  return EDIT_OK;
+}
+
+bool buffers_overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + static_cast<uintptr_t>(b_bytes) && y < x + static_cast<uintptr_t>(a_bytes);
+}
+
+edit_status_t enqueue(edit_ortho* h, OrthoCall call, hipStream_t s) {
+  call.u = h->u;
+  hipError_t e = launch_ortho_source(call, h->mats, h->chunks,
+                                     call.source == kSourceOuter ? h->all_chunks : h->matrix_chunks, s);
+  if (e != hipSuccess) return ofail_hip(e, "source pass launch");
+  if (h->matrix_chunks == 0) return EDIT_OK;
+  if ((e = launch_ortho_load(h->full, call, h->mats, h->load, h->load_tiles, s)) != hipSuccess)
+    return ofail_hip(e, "load pass launch");
+  const int steps = static_cast<int>(h->coef.size());
+  for (int k = 0; k < steps; ++k) {
+    const bool first = k == 0, last = k == steps - 1;
+    e = launch_ortho_product(kProductGram, h->full, kProductSide, h->mats, h->gram, h->coef[k], k & 1, first, last, h->u, s);
+    if (e == hipSuccess)
+      e = launch_ortho_product(kProductSquare, h->full, kProductSide, h->mats, h->gram, h->coef[k], k & 1, first, last, h->u, s);
+    if (e == hipSuccess)
+      e = launch_ortho_product(kProductUpdate, h->full, kProductSide, h->mats, h->update, h->coef[k], k & 1, first, last, h->u, s);
+    if (e != hipSuccess) return ofail_hip(e, "product launch");
+  }
+  if ((e = launch_ortho_apply(call, h->mats, h->chunks, h->matrix_chunks, s)) != hipSuccess)
+    return ofail_hip(e, "apply pass launch");
+  return EDIT_OK;
+}
+
+}  // namespace
+
+namespace edit {
+
+edit_status_t check_ortho_unit(const edit_ortho* h, int64_t numel, int device) {
+  if (h->numel != numel)
+    return ofail(EDIT_EINVAL, "the ortho handle is for units of " + std::to_string(h->numel) + " elements, the unit has " +
+                                  std::to_string(numel));
+  if (h->device != device)
+    return ofail(EDIT_EINVAL, "the ortho handle belongs to device " + std::to_string(h->device));
+  return EDIT_OK;
+}
+
+edit_status_t enqueue_ortho_outer(edit_ortho* h, bool bf16, float* theta, float* momentum, void* const* replicas,
+                                  int workers, const UnitRecord* rec, double lr, double rho, hipStream_t stream) {
+  OrthoCall c = {};
+  c.source = kSourceOuter;
+  c.bf16 = bf16;
+  c.momentum = momentum;
+  c.theta = theta;
+  c.reps = replicas;
+  c.rec = rec;
+  c.workers = h->numel == 0 ? 0 : workers;
+  c.mu = rho;
+  c.lr = lr;
+  return enqueue(h, c, stream);
+}
+
+}  // namespace edit
+
+extern "C" {
+
+edit_status_t edit_ortho_init(const edit_ortho_config_t* cfg, edit_ortho_t* out) {
+  set_error(EDIT_OK, "");
+  if (!cfg || !out) return ofail(EDIT_EINVAL, "cfg and out must not be NULL");
+  *out = nullptr;
+  try {
+    ORTHO_TRY(check_layout(cfg));
+    std::vector<OrthoCoef> coef(cfg->steps);
+    for (int k = 0; k < cfg->steps; ++k) {
+      const double* q = cfg->coefficients ? cfg->coefficients + 3 * k : kDefaultCoef;
+      coef[k] = {q[0], q[1], q[2]};
+    }
+    ORTHO_TRY(check_coefficients(coef));
+    int dev = 0, num_cu = 0;
+    ORTHO_TRY(current_gfx950(&dev, &num_cu));
+    edit_ortho* h = new (std::nothrow) edit_ortho;
+    if (!h) return ofail(EDIT_ENOMEM, "host allocation failed");
+    h->numel = cfg->numel;
+    h->bf16 = cfg->dtype == EDIT_BF16;
+    h->full = cfg->precision == EDIT_ORTHO_FULL;
+    h->device = dev;
+    h->coef = coef;
+    Tables t = make_tables(cfg);
+    const size_t total = std::max<size_t>(lay_out(h, t, nullptr), 256);
+    hipError_t e = hipMalloc(reinterpret_cast<void**>(&h->arena), total);
+    if (e != hipSuccess) {
+      delete h;
+      return ofail(EDIT_ENOMEM, std::string("hipMalloc of the workspace: ") + hipGetErrorString(e));
+    }
+    e = hipMemset(h->arena, 0, total);  // what pads the matrices stays zero
+    lay_out(h, t, h->arena);
+    if (e == hipSuccess) e = upload(h->mats, t.mats);
+    if (e == hipSuccess) e = upload(h->chunks, t.chunks);
+    if (e == hipSuccess) e = upload(h->load, t.load);
+    if (e == hipSuccess) e = upload(h->gram.tile, t.gram);
+    if (e == hipSuccess) e = upload(h->update.tile, t.update);
+    if (e == hipSuccess) e = hipDeviceSynchronize();
+    if (e != hipSuccess) {
+      (void)hipFree(h->arena);
+      delete h;
+      return ofail_hip(e, "edit_ortho_init");
+    }
+    *out = h;
+    return EDIT_OK;
+  } catch (const std::exception&) {  // the tables' host memory
+    return ofail(EDIT_ENOMEM, "host allocation failed");
+  }
+}
+
+edit_status_t edit_ortho_apply(edit_ortho_t h, const void* x, void* out, void* stream) {
+  if (!h) return ofail(EDIT_EINVAL, "NULL handle");
+  ORTHO_TRY(check_ortho_device(h));
+  if (h->matrix_chunks == 0) return EDIT_OK;
+  ORTHO_TRY(check_buffer(x, "x"));
+  ORTHO_TRY(check_buffer(out, "out"));
+  const int64_t bytes = h->numel * (h->bf16 ? 2 : 4);
+  if (x != out && buffers_overlap(x, bytes, out, bytes))
+    return ofail(EDIT_EINVAL, "x and out must be the same buffer or not overlap");
+  OrthoCall c = {};
+  c.source = kSourcePlain;
+  c.bf16 = h->bf16;
+  c.x = x;
+  c.out = out;
+  return enqueue(h, c, reinterpret_cast<hipStream_t>(stream));
+}
+
+edit_status_t edit_ortho_local_step(edit_ortho_t h, void* param, const void* grad, float* momentum, double lr, double mu,
+                                    double weight_decay, int32_t nesterov, void* stream) {
+  if (!h) return ofail(EDIT_EINVAL, "NULL handle");
+  if (!(mu >= 0.0 && mu < 1.0)) return ofail(EDIT_EINVAL, "mu must be in [0, 1)");
+  if (!(lr >= 0.0) || !std::isfinite(lr)) return ofail(EDIT_EINVAL, "lr must be finite and >= 0");
+  if (!(weight_decay >= 0.0) || !std::isfinite(weight_decay))
+    return ofail(EDIT_EINVAL, "weight_decay must be finite and >= 0");
+  ORTHO_TRY(check_ortho_device(h));
+  if (h->matrix_chunks == 0) return EDIT_OK;
+  ORTHO_TRY(check_buffer(param, "param"));
+  ORTHO_TRY(check_buffer(grad, "grad"));
+  ORTHO_TRY(check_buffer(momentum, "momentum"));
+  const int64_t bytes = h->numel * (h->bf16 ? 2 : 4);
+  if (buffers_overlap(param, bytes, grad, bytes) || buffers_overlap(param, bytes, momentum, 4 * h->numel) ||
+      buffers_overlap(grad, bytes, momentum, 4 * h->numel))
+    return ofail(EDIT_EINVAL, "param, grad and momentum must not overlap");
+  OrthoCall c = {};
+  c.source = kSourceLocal;
+  c.bf16 = h->bf16;
+  c.x = grad;
+  c.out = param;
+  c.momentum = momentum;
+  c.nesterov = nesterov != 0;
+  c.mu = mu;
+  c.keep = 1.0 - lr * weight_decay;
+  c.lr = lr;
+  return enqueue(h, c, reinterpret_cast<hipStream_t>(stream));
+}
+
+void edit_ortho_destroy(edit_ortho_t h) {
+  if (!h) return;
+  if (h->arena) {
+    (void)hipDeviceSynchronize();
+    (void)hipFree(h->arena);
+  }
+  delete h;
+}
+
+}  // extern "C"

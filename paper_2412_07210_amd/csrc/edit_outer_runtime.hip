@@ -21,6 +21,7 @@
 #include "disjoint_ranges.h"
 #include "edit_outer_internal.h"
 #include "edit_group_internal.h"
+#include "edit_ortho_internal.h"
 
 #define EDIT_TRY(expr)                    \
   do {                                    \
@@ -743,6 +744,30 @@ edit_status_t edit_outer_apply_layer(edit_outer_t h, int32_t layer, const double
   EDIT_TRY(q.event(u, layer, 1));
   EDIT_TRY(q.event(u, layer, 2));
   EDIT_TRY(q.update(&d, 1));
+  EDIT_TRY(q.event(u, layer, 3));
+  return q.finish(layer);
+}
+
+edit_status_t edit_outer_step_layer_ortho(edit_outer_t h, int32_t layer, edit_ortho_t ortho, float* theta,
+                                          float* momentum, void* const* replicas, void* stream) {
+  if (!h || !ortho) return fail(EDIT_EINVAL, "NULL handle");
+  if (h->one_pass) return fail(EDIT_EINVAL, "edit_outer_step_layer_ortho is not available with EDIT_ONE_PASS");
+  EDIT_TRY(check_step(h, layer, theta, momentum, replicas));
+  EDIT_TRY(check_device(h));
+  Unit& u = h->units[layer];
+  EDIT_TRY(check_ortho_unit(ortho, u.n, h->device));
+  const int K = h->cfg.num_workers;
+  const bool bf16 = h->cfg.replica_dtype == EDIT_BF16;
+  Enqueue q{h, reinterpret_cast<hipStream_t>(stream), decide_params(h), K, bf16};
+  UnitDesc d = q.desc(layer, theta, momentum, replicas);
+  q.cache_end(&d, 1);
+  EDIT_TRY(q.event(u, layer, 0));
+  EDIT_TRY(q.gram(&d, 1));
+  EDIT_TRY(q.decide(&d, 1));
+  EDIT_TRY(q.event(u, layer, 1));
+  EDIT_TRY(q.event(u, layer, 2));
+  EDIT_TRY(enqueue_ortho_outer(ortho, bf16, theta, momentum, replicas, K, u.rec, h->cfg.outer_lr, h->cfg.momentum,
+                               q.s));
   EDIT_TRY(q.event(u, layer, 3));
   return q.finish(layer);
 }

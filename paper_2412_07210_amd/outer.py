@@ -9,9 +9,10 @@ if the library is missing or fails to load, EditOuterError is raised.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
-from typing import List, Optional, Sequence
+from typing import List, Optional, Sequence, Union
 
 import numpy as np
 import torch
@@ -36,7 +37,10 @@ EXPORTS = (
     "edit_outer_set_profiling", "edit_outer_kernel_times", "edit_outer_update_probe", "edit_outer_copy_probe",
     "edit_group_init", "edit_group_norm", "edit_group_weights", "edit_group_apply",
     "edit_group_state_get", "edit_group_state_set", "edit_group_destroy",
+    "edit_outer_step_layer_ortho",
 )
+ORTHO_EXPORTS = ("edit_ortho_init", "edit_ortho_apply", "edit_ortho_local_step", "edit_ortho_destroy")
+ORTHO_FAST, ORTHO_FULL = 0, 1
 
 
 class EditOuterError(RuntimeError):
@@ -76,6 +80,27 @@ class _LayerState(ctypes.Structure):
         ("anomalous", ctypes.c_uint8 * MAX_K),
         ("synced_norm", ctypes.c_double),
         ("clip_coef", ctypes.c_double),
+    ]
+
+
+class _OrthoMatrix(ctypes.Structure):
+    _fields_ = [
+        ("offset", ctypes.c_int64),
+        ("rows", ctypes.c_int32),
+        ("cols", ctypes.c_int32),
+        ("scale", ctypes.c_double),
+    ]
+
+
+class _OrthoConfig(ctypes.Structure):
+    _fields_ = [
+        ("numel", ctypes.c_int64),
+        ("matrices", ctypes.POINTER(_OrthoMatrix)),
+        ("num_matrices", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("precision", ctypes.c_int32),
+        ("steps", ctypes.c_int32),
+        ("coefficients", ctypes.POINTER(ctypes.c_double)),
     ]
 
 
@@ -145,6 +170,17 @@ def load_library() -> ctypes.CDLL:
     lib.edit_group_state_set.restype = st
     lib.edit_group_destroy.argtypes = [vp]
     lib.edit_group_destroy.restype = None
+    lib.edit_ortho_init.argtypes = [ctypes.POINTER(_OrthoConfig), ctypes.POINTER(vp)]
+    lib.edit_ortho_init.restype = st
+    lib.edit_ortho_apply.argtypes = [vp, vp, vp, vp]
+    lib.edit_ortho_apply.restype = st
+    lib.edit_ortho_local_step.argtypes = [vp, vp, vp, vp, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+                                          ctypes.c_int32, vp]
+    lib.edit_ortho_local_step.restype = st
+    lib.edit_ortho_destroy.argtypes = [vp]
+    lib.edit_ortho_destroy.restype = None
+    lib.edit_outer_step_layer_ortho.argtypes = [vp, ctypes.c_int32, vp, vp, vp, ctypes.POINTER(vp), vp]
+    lib.edit_outer_step_layer_ortho.restype = st
     _lib = lib
     return lib
 
@@ -354,6 +390,18 @@ class EditOuter:
                           theta.data_ptr(), momentum.data_ptr(), ptrs,
                           _stream_handle(stream, self.device)),
                "edit_outer_apply_layer")
+
+    def step_layer_ortho(self, layer: int, ortho: "Orthogonalizer", theta: torch.Tensor, momentum: torch.Tensor,
+                         replicas: Sequence[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Enqueue one outer step of unit `layer` whose matrices, as `ortho`
+        names them, move along their orthogonalised Nesterov direction
+        (edit_outer_step_layer_ortho); in place on all tensors."""
+        if not isinstance(ortho, Orthogonalizer):
+            raise TypeError("ortho must be an Orthogonalizer")
+        ptrs = self._unit_tensors(layer, theta, momentum, replicas)
+        _check(self._call(self._lib.edit_outer_step_layer_ortho, int(layer), ortho._h, theta.data_ptr(),
+                          momentum.data_ptr(), ptrs, _stream_handle(stream, self.device)),
+               "edit_outer_step_layer_ortho")
 
     def prepare_round(self, units: Sequence[tuple], layers: Optional[Sequence[int]] = None,
                       host: bool = False) -> "RoundPlan":
@@ -591,6 +639,146 @@ class SyncGroupWorker:
         st.ema_mean[self.rank] = float(ema_mean)
         st.ema_std[self.rank] = float(ema_std)
         self._call(self._lib.edit_group_state_set, "edit_group_state_set", int(layer), ctypes.byref(st))
+
+
+@dataclass
+class OrthoConfig:
+    """The matrices of one sync unit and how their updates are orthogonalised."""
+    numel: int                                  # elements of the unit
+    matrices: Sequence[tuple]                   # (offset, rows, cols) of each, row-major
+    dtype: str = "bf16"                         # of updates, parameters and gradients: "bf16" or "f32"
+    # s of each matrix in the steps: "spectral" = sqrt(max(1, rows / cols)),
+    # "rms" = 0.2 sqrt(max(rows, cols)), which moves an element about as far as
+    # 0.2 lr, or one number per matrix
+    scale: Union[str, Sequence[float]] = "spectral"
+    steps: int = 5                              # Newton-Schulz steps
+    # (a, b, c) for all steps or one triple per step; None: 3.4445, -4.7750, 2.0315
+    coefficients: Optional[Sequence] = None
+    precision: Optional[str] = None             # "fast" or "full"; None: "fast" for bf16, "full" for f32
+
+    def scales(self) -> List[float]:
+        if self.scale == "spectral":
+            return [math.sqrt(max(1.0, r / c)) if r and c else 0.0 for _, r, c in self.matrices]
+        if self.scale == "rms":
+            return [0.2 * math.sqrt(max(r, c)) for _, r, c in self.matrices]
+        if isinstance(self.scale, str):
+            raise ValueError("scale must be 'spectral', 'rms' or one number per matrix")
+        if len(self.scale) != len(self.matrices):
+            raise ValueError(f"expected {len(self.matrices)} scales, got {len(self.scale)}")
+        return [float(x) for x in self.scale]
+
+
+class Orthogonalizer:
+    """Orthogonalised updates of the matrices of one sync unit layout
+    (edit_ortho_* of the C ABI).  Calls share the handle's workspace: order
+    them on one stream or with events."""
+
+    def __init__(self, cfg: OrthoConfig, device: Optional[torch.device] = None):
+        self._h = None
+        self.cfg = cfg
+        device = torch.device("cuda") if device is None else torch.device(device)
+        if device.type != "cuda":
+            raise ValueError("the handle needs a GPU device")
+        c, keep = self._c_config(cfg)
+        if device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        self.device = device
+        self._numel = int(cfg.numel)
+        self._torch_dtype = torch.bfloat16 if cfg.dtype == "bf16" else torch.float32
+        self._covered = sum(int(r) * int(k) for _, r, k in cfg.matrices) == self._numel
+        self._lib = load_library()
+        h = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            _check(self._lib.edit_ortho_init(ctypes.byref(c), ctypes.byref(h)), "edit_ortho_init")
+        del keep  # the arrays that the configuration points to
+        self._h = h
+
+    @staticmethod
+    def _c_config(cfg: OrthoConfig):
+        """The C configuration, and the arrays it points to."""
+        if cfg.dtype not in ("bf16", "f32"):
+            raise ValueError("dtype must be 'bf16' or 'f32'")
+        precision = cfg.precision or ("fast" if cfg.dtype == "bf16" else "full")
+        if precision not in ("fast", "full"):
+            raise ValueError("precision must be 'fast' or 'full'")
+        steps = int(cfg.steps)
+        coef = None
+        if cfg.coefficients is not None:
+            flat = np.asarray(cfg.coefficients, dtype=np.float64)
+            if flat.shape == (3,):
+                flat = np.tile(flat, (max(steps, 0), 1))
+            if flat.shape != (steps, 3):
+                raise ValueError(f"coefficients must be one triple or {steps} of them")
+            coef = (ctypes.c_double * flat.size)(*flat.reshape(-1).tolist())
+        for m in cfg.matrices:
+            for x in m:
+                if int(x) != x:
+                    raise ValueError("a matrix is (offset, rows, cols) in whole numbers")
+            if not all(abs(int(x)) < 2 ** 31 for x in m[1:]):
+                raise ValueError("rows and cols must be below 2^31")
+        mats = (_OrthoMatrix * max(1, len(cfg.matrices)))(
+            *[_OrthoMatrix(int(o), int(r), int(k), s) for (o, r, k), s in zip(cfg.matrices, cfg.scales())])
+        c = _OrthoConfig(int(cfg.numel), mats, len(cfg.matrices), BF16 if cfg.dtype == "bf16" else F32,
+                         ORTHO_FULL if precision == "full" else ORTHO_FAST, steps, coef)
+        return c, (mats, coef)
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h.value:
+            with torch.cuda.device(self.device):
+                self._lib.edit_ortho_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def _arg(self, t: torch.Tensor, dtype: torch.dtype, what: str) -> int:
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{what} must be a torch.Tensor")
+        if t.device != self.device or t.dtype != dtype or not t.is_contiguous() or t.numel() != self._numel:
+            raise ValueError(f"{what} must be a contiguous {dtype} tensor of {self._numel} elements on {self.device}")
+        return t.data_ptr()
+
+    def _call(self, fn, what: str, *args) -> None:
+        if torch.cuda.current_device() != self.device.index:
+            with torch.cuda.device(self.device):
+                status = fn(self._h, *args)
+        else:
+            status = fn(self._h, *args)
+        _check(status, what)
+
+    def orthogonalize(self, x: torch.Tensor, out: Optional[torch.Tensor] = None,
+                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Enqueue out = O(x) for every matrix (edit_ortho_apply) and return
+        `out`, which may be `x`.  A new `out` is zero outside the matrices; a
+        given one keeps what it holds there."""
+        px = self._arg(x, self._torch_dtype, "x")
+        if out is None:
+            out = torch.empty_like(x)
+            if not self._covered:
+                with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+                    out.zero_()
+        self._call(self._lib.edit_ortho_apply, "edit_ortho_apply", px, self._arg(out, self._torch_dtype, "out"),
+                   _stream_handle(stream, self.device))
+        return out
+
+    def local_step(self, param: torch.Tensor, grad: torch.Tensor, momentum: torch.Tensor, lr: float,
+                   mu: float = 0.95, weight_decay: float = 0.0, nesterov: bool = True,
+                   stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Enqueue one local step of the unit's matrices (edit_ortho_local_step),
+        in place on param and momentum (fp32)."""
+        self._call(self._lib.edit_ortho_local_step, "edit_ortho_local_step",
+                   self._arg(param, self._torch_dtype, "param"), self._arg(grad, self._torch_dtype, "grad"),
+                   self._arg(momentum, torch.float32, "momentum"), float(lr), float(mu), float(weight_decay),
+                   int(bool(nesterov)), _stream_handle(stream, self.device))
 
 
 def copy_probe(dst: torch.Tensor, src: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
