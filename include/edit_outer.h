@@ -387,8 +387,8 @@ void edit_group_destroy(edit_group_t h);
  * Norms are summed in fp64, steps are taken in fp64 and rounded once.  Results
  * are the same bit for bit on every run.
  *
- * The handle owns its workspace (14 to 16 bytes per element of a square
- * matrix, with FULL 20 to 22), made by edit_ortho_init; the calls allocate
+ * The handle owns its workspace (10 bytes per element and 6 more per element
+ * of A, with FULL 12 and 8), made by edit_ortho_init; the calls allocate
  * nothing, do not synchronise and can be captured into HIP graphs.  Calls on
  * one handle, replays of graphs that hold them included, use the same
  * workspace and must not overlap: order them on one stream or with events. */
@@ -398,7 +398,7 @@ typedef enum { EDIT_ORTHO_FAST = 0, EDIT_ORTHO_FULL = 1 } edit_ortho_precision_t
 
 typedef struct {
   int64_t offset;     /* first element in the unit                              */
-  int32_t rows, cols; /* row-major; each up to 2^24, rows * cols up to 2^30     */
+  int32_t rows, cols; /* row-major; each up to 2^24, rows * cols up to 2^29     */
   double scale;       /* factor s of O in the steps, e.g. sqrt(max(1, rows/cols)) */
 } edit_ortho_matrix_t;
 

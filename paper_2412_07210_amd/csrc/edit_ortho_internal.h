@@ -18,8 +18,8 @@ namespace edit {
 // it down to 2^-24 / scale.
 constexpr float kScaleX = 8192.f;
 constexpr float kScaleA = 2048.f;
-// The largest |sigma| and |polynomial| that the scales leave room for
-// (65504 / 8192 and 65504 / 2048 / 2, the difference of two of its values).
+// The largest |sigma| and |polynomial| that the scales leave room for, with a
+// factor of two for rounding (65504 / 8192 / 2 and 65504 / 2048 / 2).
 constexpr double kMaxSigma = 4.0;
 constexpr double kMaxPoly = 15.0;
 
@@ -30,21 +30,21 @@ constexpr int kOrthoLoadTile = 64;      // side of the load pass's tiles
 
 // One matrix of a unit: r = min(rows, cols), c = max(rows, cols).  The
 // working matrix X is r x c: the stored one, or its transpose where rows >
-// cols.  Every array is zero behind its r or c columns.
+// cols.  Every array is zero behind its r columns.
 struct OrthoMat {
-  _Float16* x[2];     // X, high and low halves                          [r][ldc]
-  _Float16* t[2][2];  // X^T, [buffer][high, low]                        [c][ldr]
-  _Float16* g[2];     // R = A - sI                                      [r][ldr]
-  _Float16* q[2];     // (b + 2cs) R + c R^2                             [r][ldr]
+  // High and low halves; with FULL they share the first array (Layout in the
+  // kernels) and there is no second.
+  _Float16* t[2][2];  // X^T, [buffer][half]: [c][ldr], and rows of zeros to a multiple of kOrthoPad
+  _Float16* g[2];     // R = A - sI                            [r][ldr]
+  _Float16* q[1];     // the update product's polynomial F     [r][ldr]
   double* norm_part;  // sums of squares of the update's chunks
   double* x_part;     // sums of squares of the X tiles of the last product
   double* shift;      // s of this iteration
   int64_t offset;     // of the matrix in the unit
   double scale;       // its factor in a step
-  int32_t rows, cols, r, c, ldr, ldc;
+  int32_t rows, cols, r, c, ldr;
   int32_t chunks, x_tiles;
   int32_t tall;       // rows > cols: X is the stored matrix transposed
-  int32_t pad_;
 };
 
 // Elements [begin, end) of the unit: of matrix `mat`, partial `slot`; of no
@@ -54,7 +54,7 @@ struct OrthoChunk {
   int32_t mat, slot;
 };
 
-// Tile (m, n) of a matrix; mat = -1: none.
+// Tile (m, n) of a matrix: of its rows and columns (load), of C's p and q (products); mat = -1: none.
 struct OrthoTile {
   int32_t mat, m, n, slot;
 };
@@ -92,10 +92,10 @@ struct OrthoTiles {
 // Pass over the update: momentum and update of the call, and the chunks' sums of squares.
 hipError_t launch_ortho_source(const OrthoCall& call, const OrthoMat* mats, const OrthoChunk* chunks, int count,
                                hipStream_t stream);
-// X and X^T of the update over its norm.
+// X^T of the update over its norm.
 hipError_t launch_ortho_load(bool full, const OrthoCall& call, const OrthoMat* mats, const OrthoTile* tiles, int count,
                              hipStream_t stream);
-// One product of an iteration; `side`: of its tiles, `from`: the X^T buffer read, `last`: O to `u` instead of X.
+// One product of an iteration; `side`: of its tiles, `from`: the X^T buffer read, `last`: O to `u` instead of X^T.
 hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const OrthoMat* mats, const OrthoTiles& tiles,
                                 const OrthoCoef& coef, int from, bool first, bool last, float* u, hipStream_t stream);
 // The call's outputs from O.

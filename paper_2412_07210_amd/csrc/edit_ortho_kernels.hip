@@ -5,17 +5,18 @@
 //
 //   source   u of the call (the update itself; a worker's momentum step; the
 //            outer step's Nesterov direction) and its sums of squares
-//   load     X = u / ||u||_F, and X^T
-//   gram     A = X X^T              } steps times, each a launch over the
-//   square   polynomial of A        } tiles of all matrices
-//   update   X <- (polynomial) X    }
+//   load     X = u / ||u||_F
+//   gram     A = X X^T               } steps times, each a launch over the
+//   square   F = a I + b A + c A^2   } tiles of all matrices
+//   update   X <- F X                }
 //   apply    the call's outputs from O = X
 //
 // Numerics.  The products run on the fp16 matrix cores with fp32 sums.  Two
 // things keep them near 32 bits of X at that price:
-//  * X is held to 22 bits as the sum of two fp16 values (high + low).  The
-//    term a X of an iteration uses both; a product uses the high half
-//    (EDIT_ORTHO_FAST), or high*high + high*low + low*high (EDIT_ORTHO_FULL).
+//  * X is held to 22 bits as the sum of two fp16 values (high + low).  A
+//    product takes the high halves (EDIT_ORTHO_FAST), and the low half of X
+//    enters the next X times F's mean diagonal; or it takes high*high +
+//    high*low + low*high (EDIT_ORTHO_FULL).
 //  * A is taken about its mean diagonal s = ||X||_F^2 / r: with R = A - sI,
 //      a + b A + c A^2 = (a + bs + cs^2) + (b + 2cs) R + c R^2
 //    for any s.  Once the singular values are near one, R is small where A is
@@ -227,8 +228,31 @@ __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
   lo = static_cast<_Float16>(v - static_cast<float>(hi));
 }
 
-// One 64 x 64 tile of a stored matrix per block: X = u / ||u|| at kScaleX,
-// written in the stored orientation and, through LDS, transposed.
+// How the halves of a matrix lie in memory.  The 128 bytes of a cache line are
+// what one row of a slab takes, so that a load asks the L2 for whole lines:
+//   FAST  high and low halves in arrays of their own, 64 high ones a line
+//   FULL  one array, 32 columns' high halves and then their low ones a line
+template <bool FULL>
+struct Layout {
+  __device__ static int64_t pitch(int ld) { return FULL ? 2 * static_cast<int64_t>(ld) : ld; }
+  __device__ static int64_t at(int row, int col, int ld) {  // of a high half; the low one: see low()
+    return row * pitch(ld) + (FULL ? 2 * (col & ~31) + (col & 31) : col);
+  }
+  template <typename T>
+  __device__ static T* low(T* hi, T* lo) {  // the array of low halves
+    return FULL ? hi + 32 : lo;
+  }
+};
+
+// A pointer read from a table, which the compiler would take for one to any
+// memory (and wait for LDS on each use).
+template <typename T>
+__device__ __forceinline__ T* as_global(T* p) {
+  return (T*)(__attribute__((address_space(1))) T*)p;
+}
+
+// One 64 x 64 tile of a stored matrix per block: X^T = u / ||u|| at kScaleX,
+// through LDS where that transposes.
 template <int SOURCE, bool BF16, bool FULL>
 __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_load_kernel(OrthoArgs a, const OrthoMat* __restrict__ mats,
                                                                         const OrthoTile* __restrict__ tiles) {
@@ -243,15 +267,9 @@ __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_load_kernel(OrthoAr
   const double inv = sum > 0.0 ? kScaleX / sqrt(sum) : (sum == 0.0 ? 0.0 : sum);
   const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
   const int row0 = t.m * T, col0 = t.n * T;
-  _Float16* nat_hi = mt.tall ? mt.t[0][0] : mt.x[0];
-  _Float16* nat_lo = mt.tall ? mt.t[0][1] : mt.x[1];
-  _Float16* tr_hi = mt.tall ? mt.x[0] : mt.t[0][0];
-  _Float16* tr_lo = mt.tall ? mt.x[1] : mt.t[0][1];
-  const int64_t ld_nat = mt.tall ? mt.ldr : mt.ldc;
-  const int64_t ld_tr = mt.tall ? mt.ldc : mt.ldr;
-  // X^T needs its low half in the products only
-  const bool nat_has_lo = FULL || !mt.tall;
-  const bool tr_has_lo = FULL || mt.tall;
+  using L = Layout<FULL>;
+  _Float16* x_hi = as_global(mt.t[0][0]);
+  _Float16* x_lo = L::low(x_hi, as_global(mt.t[0][1]));
   for (int y = ty; y < T; y += kOrthoStreamThreads / 64) {
     const int row = row0 + y, col = col0 + tx;
     float v = 0.f;
@@ -269,54 +287,82 @@ __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_load_kernel(OrthoAr
       v = static_cast<float>(u * inv);
       _Float16 hi, lo;
       split(v, hi, lo);
-      nat_hi[row * ld_nat + col] = hi;
-      if (nat_has_lo) nat_lo[row * ld_nat + col] = lo;
-      lds[y][tx] = __builtin_bit_cast(uint16_t, hi) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, lo)) << 16;
+      if (mt.tall) {  // X^T is the stored matrix
+        const int64_t at = L::at(row, col, mt.ldr);
+        x_hi[at] = hi;
+        x_lo[at] = lo;
+      } else {
+        lds[y][tx] = __builtin_bit_cast(uint16_t, hi) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, lo)) << 16;
+      }
     }
   }
+  if (mt.tall) return;
   __syncthreads();
   for (int y = ty; y < T; y += kOrthoStreamThreads / 64) {
     const int col = col0 + y, row = row0 + tx;
     if (row < mt.rows && col < mt.cols) {
       const uint32_t w = lds[tx][y];
-      tr_hi[col * ld_tr + row] = __builtin_bit_cast(_Float16, static_cast<uint16_t>(w));
-      if (tr_has_lo) tr_lo[col * ld_tr + row] = __builtin_bit_cast(_Float16, static_cast<uint16_t>(w >> 16));
+      const int64_t at = L::at(col, row, mt.ldr);
+      x_hi[at] = __builtin_bit_cast(_Float16, static_cast<uint16_t>(w));
+      x_lo[at] = __builtin_bit_cast(_Float16, static_cast<uint16_t>(w >> 16));
     }
   }
 }
 
 // ---------------------------------------------------------------- products
 
-// Product C[m][n] = sum_k P[m][k] Q[n][k] over the tiles of all matrices, both
-// operands row by row along k:
-//   gram    P = Q = X          C -> R = C - sI                (symmetric)
-//   square  P = Q = R          C -> (b + 2cs) R + c C         (symmetric)
-//   update  P = X^T, Q = poly  C -> X^T' = (a + bs + cs^2) X^T + C
-// Symmetric products take the tiles with m >= n and store each twice.
+// Product C[p][q] = sum_k P[p][k] Q[q][k] over the tiles of all matrices:
+//   gram    P = Q = X, read from X^T          C -> R = C - sI          (symmetric)
+//   square  P = Q = R                         C -> F = (b + 2cs) R + c C, FULL: + (a + bs + cs^2) I   (symmetric)
+//   update  P = F, Q = X^T                    C^T -> X^T of the next iteration
+// X lives as X^T only, so an iteration reads and writes one array of the
+// matrix's size: the gram product reads its operands across the rows of LDS
+// (the transposing LDS reads of gfx950).  The term (a + bs + cs^2) X is part of
+// F X with FULL; with FAST F's diagonal would round it to 11 bits, so the
+// update product takes it from the operand tiles as they pass through LDS, and
+// the low half of X in its epilogue.  Symmetric products take the tiles with
+// p >= q and store each twice.
 struct ProductArgs {
   double a, b, c;
   int32_t from, first, last;
 };
 
-template <int PRODUCT, bool FULL, int BM, int BN, int WM, int WN, int BK>
+// LDS holds two slabs of both operands: 64 values of k (FAST), or 32 with both
+// halves (FULL); 128 bytes for each of the operands' rows either way.
+template <bool FULL, int BP, int BQ, int WP, int WQ>
 struct ProductShape {
-  static constexpr int kWaves = (BM / WM) * (BN / WN);
+  static constexpr int kSlabK = FULL ? 32 : 64;
+  static constexpr int kWaves = (BP / WP) * (BQ / WQ);
   static constexpr int kThreads = kWaves * 64;
-  static constexpr int kHalves = FULL ? 2 : 1;
-  static constexpr int kRowBytes = BK * 2;
-  static constexpr int kChunks = kRowBytes / 16;            // 16-byte chunks of a row
-  static constexpr int kStage = (BM + BN) * kRowBytes * kHalves;
-  static constexpr int kRowsPerLoad = 1024 / kRowBytes;     // rows that a wave's load fills
-  static constexpr int kLoadsP = BM / kRowsPerLoad / kWaves;
-  static constexpr int kLoadsQ = BN / kRowsPerLoad / kWaves;
+  static constexpr int kBytesP = BP * 128, kBytesQ = BQ * 128;
+  static constexpr int kSlab = kBytesP + kBytesQ;
+  static constexpr int kLoadsP = kBytesP / 1024 / kWaves;  // of a wave, 1 KB each
+  static constexpr int kLoadsQ = kBytesQ / 1024 / kWaves;
+  static_assert(kLoadsP * kWaves * 1024 == kBytesP && kLoadsQ * kWaves * 1024 == kBytesQ, "whole loads");
+  static_assert(kOrthoPad % kSlabK == 0, "whole slabs");
+  static_assert(2 * kSlab <= 160 * 1024 - 256, "two slabs, and the sums of block_sum");
+  static_assert(!FULL || WP >= WQ, "the order of the reads");
 };
 
-// LDS holds rows of BK values; the 16-byte chunks of a row are permuted by
-// its number, so that the 16 rows that a wave reads at once lie in different
-// banks.
-template <int CHUNKS>
-__device__ __forceinline__ int chunk_swizzle(int row) {
-  return CHUNKS == 8 ? (row & 7) : ((row >> 1) & 3);
+// How an operand lies in a slab and is read from it: 16 lanes at a time, lane l
+// for row `side` + l of the tile unless said otherwise.
+enum Reading {
+  kAlong,   // an operand's row is a slab row: a lane reads 16 bytes of it
+  kBlocks,  // the same, lane l for row side + 8 (l / 4) + l mod 4: with side + 4,
+            // a lane of the product's results gets eight neighbours of a column
+  kAcross,  // a value of k is a slab row: four lanes read 32 bytes of it, and the
+            // 16 lanes exchange theirs (the transposing read of gfx950)
+};
+
+// A slab's rows of 16-byte chunks are permuted within a row by its number, so
+// that what a wave reads in one cycle (256 bytes) lies in different banks.
+template <Reading READING, int CHUNKS>
+__device__ __forceinline__ int chunk_swizzle(int row, int chunk) {
+  if constexpr (READING == kAlong) return chunk ^ ((row >> 1) & 7);  // 16 rows from a multiple of 16 on
+  if constexpr (READING == kBlocks) return chunk ^ (((row >> 1) & 1) | ((row >> 2) & 6));
+  // rows 0..3 and 8..11, or 4..7 and 12..15, of sixteen
+  if constexpr (CHUNKS >= 16) return chunk ^ (((row & 3) | ((row >> 1) & 4)) << 1);
+  return chunk ^ ((((row >> 1) & 1) | ((row >> 2) & 2)) << 1);
 }
 
 // 16 bytes a lane from global memory to LDS, no register in between: lane l's
@@ -330,16 +376,154 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, const void* base, uint
                : "memory");
 }
 
-template <int PRODUCT, bool FULL, int BM, int BN, int WM, int WN, int BK>
-__global__ __launch_bounds__((ProductShape<PRODUCT, FULL, BM, BN, WM, WN, BK>::kThreads)) void ortho_product_kernel(
-    const OrthoMat* __restrict__ mats, const OrthoTile* __restrict__ tiles, ProductArgs args, float* __restrict__ out) {
-  using S = ProductShape<PRODUCT, FULL, BM, BN, WM, WN, BK>;
-  __shared__ __align__(128) char smem[2 * S::kStage];
+// The byte offsets of a lane's loads of a tile's first slab: `rows` x `ld` is
+// the operand.  Rows (along k) or columns (across) past its end read the last
+// ones; what they give is not stored.
+template <Reading READING, bool FULL, int SIDE, int WAVES, int LOADS>
+__device__ __forceinline__ void tile_offsets(uint32_t (&off)[LOADS], int side0, int rows, int ld, int wave, int lane) {
+  constexpr bool ACROSS = READING == kAcross;
+  constexpr int kChunks = !ACROSS ? 8 : FULL ? SIDE / 4 : SIDE / 8;
+  constexpr int kRowsPerLoad = 64 / kChunks;
+  const int pitch = static_cast<int>(Layout<FULL>::pitch(ld));
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int row = (wave + i * WAVES) * kRowsPerLoad + lane / kChunks;
+    const int chunk = chunk_swizzle<READING, kChunks>(row, lane % kChunks);
+    const int g = ACROSS ? row : min(side0 + row, rows - 1);
+    const int col = ACROSS ? min((FULL ? 2 * side0 : side0) + 8 * chunk, pitch - 8) : 8 * chunk;
+    off[i] = (static_cast<uint32_t>(g) * static_cast<uint32_t>(pitch) + static_cast<uint32_t>(col)) * 2u;
+  }
+}
+
+typedef __fp16 fp16x4 __attribute__((__vector_size__(8)));
+
+// A lane's eight values of its row of a slab's operand: of FAST's k = 32 part +
+// 8 (lane / 16) .., of FULL's k = 8 (lane / 16) .. and half `part`.
+template <Reading READING, bool FULL, int SIDE>
+__device__ __forceinline__ half8 read_operand(const char* slab, int side, int part, int lane) {
+  if constexpr (READING == kAcross) {
+    // 16 lanes give four rows of 16 values and get four values of 16 columns
+    constexpr int kChunks = FULL ? SIDE / 4 : SIDE / 8;
+    half8 out;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int row = (FULL ? 0 : 32 * part) + 8 * (lane >> 4) + 4 * h + ((lane & 15) >> 2);
+      const int col = (side >> 3) + ((lane & 3) >> 1);  // in chunks of one half
+      const int chunk = chunk_swizzle<kAcross, kChunks>(row, FULL ? 2 * (col & ~3) + 4 * part + (col & 3) : col);
+      const char* at = slab + (row * kChunks + chunk) * 16 + 8 * (lane & 1);
+      const half4 v = __builtin_bit_cast(
+          half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) fp16x4*)(at)));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[4 * h + e] = v[e];
+    }
+    return out;
+  } else {
+    const int row = side + (READING == kBlocks ? 2 * (lane & 12) + (lane & 3) : lane & 15);
+    return *reinterpret_cast<const half8*>(slab + row * 128 +
+                                           chunk_swizzle<READING, 8>(row, 4 * part + (lane >> 4)) * 16);
+  }
+}
+
+// All of the wave's loads into LDS have landed and its reads of LDS are done,
+// for every wave of the block.  The wait is the builtin one, which the compiler
+// counts: with scalar loads outstanding it could only wait for all reads of LDS
+// at each use of one.
+__device__ __forceinline__ void slab_barrier() {
+  asm volatile("" : : : "memory");
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" : : : "memory");
+}
+
+// The 4 x 4 transpose of what four neighbouring lanes hold: lane q of each
+// quad gives v[e] = element (e, q) and gets (q, e).
+template <int CTRL>
+__device__ __forceinline__ uint32_t quad_move(uint32_t x) {
+  return static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ void quad_transpose(uint32_t (&v)[4], int lane) {
+  constexpr int kSwap1 = 1 | 0 << 2 | 3 << 4 | 2 << 6;  // lanes 1 0 3 2
+  constexpr int kSwap2 = 2 | 3 << 2 | 0 << 4 | 1 << 6;  // lanes 2 3 0 1
+  const bool odd = lane & 1, high = lane & 2;
+#pragma unroll
+  for (int e = 0; e < 4; e += 2) {
+    const uint32_t got = quad_move<kSwap1>(odd ? v[e] : v[e + 1]);
+    v[e] = odd ? got : v[e];
+    v[e + 1] = odd ? v[e + 1] : got;
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const uint32_t got = quad_move<kSwap2>(high ? v[e] : v[e + 2]);
+    v[e] = high ? got : v[e];
+    v[e + 2] = high ? v[e + 2] : got;
+  }
+}
+
+// A value as its (high, low) halves in 32 bits, and four of them in two rows.
+__device__ __forceinline__ uint32_t pack_split(float v) {
+  _Float16 hi, lo;
+  split(v, hi, lo);
+  return __builtin_bit_cast(uint16_t, hi) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, lo)) << 16;
+}
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+template <bool LOW>
+__device__ __forceinline__ void store_split(_Float16* hi, _Float16* lo, int64_t at, const uint32_t (&v)[4]) {
+  *reinterpret_cast<u32x2*>(hi + at) =
+      u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x05040100), __builtin_amdgcn_perm(v[3], v[2], 0x05040100)};
+  if constexpr (LOW)
+    *reinterpret_cast<u32x2*>(lo + at) =
+        u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x07060302), __builtin_amdgcn_perm(v[3], v[2], 0x07060302)};
+}
+__device__ __forceinline__ float join(const half4& hi, const half4& lo, int e) {
+  return static_cast<float>(hi[e]) + static_cast<float>(lo[e]);
+}
+
+// One tile of a product per block.  While one slab is multiplied, the loads of
+// the next are under way.  A wave's operands are read a step ahead of their
+// use: each register is read anew right after its last use, and the barrier
+// between slabs stands before the last step of a slab, so that the first reads
+// of the next one run under that step's products.
+template <int PRODUCT, bool FULL, bool LAST, int BP, int BQ, int WP, int WQ>
+__global__ __launch_bounds__((ProductShape<FULL, BP, BQ, WP, WQ>::kThreads),
+                             2)  // waves per SIMD that the registers are budgeted for
+void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __restrict__ tiles, ProductArgs args,
+                          float* __restrict__ out) {
+  using S = ProductShape<FULL, BP, BQ, WP, WQ>;
+  constexpr Reading kReadP = PRODUCT == kProductGram ? kAcross : PRODUCT == kProductUpdate ? kBlocks : kAlong;
+  constexpr Reading kReadQ = PRODUCT == kProductGram ? kAcross : kAlong;
+  using L = Layout<FULL>;
+  __shared__ __align__(256) char smem[2 * S::kSlab];
   const OrthoTile t = tiles[blockIdx.x];
   if (t.mat < 0) return;
-  const OrthoMat& mt = mats[t.mat];
+  const OrthoMat mt = mats[t.mat];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = mt.r, c = mt.c, ld = mt.ldr;
+
+  const _Float16* x_t = args.from ? mt.t[1][0] : mt.t[0][0];
+  const _Float16* q = PRODUCT == kProductSquare ? mt.g[0] : x_t;
+  const _Float16* p = PRODUCT == kProductUpdate ? mt.q[0] : q;
+  uint32_t off_p[S::kLoadsP], off_q[S::kLoadsQ];
+  tile_offsets<kReadP, FULL, BP, S::kWaves>(off_p, t.m * BP, r, ld, wave, lane);
+  tile_offsets<kReadQ, FULL, BQ, S::kWaves>(off_q, t.n * BQ, PRODUCT == kProductUpdate ? c : r, ld, wave, lane);
+
+  const uint32_t lds0 = static_cast<uint32_t>(
+      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)(smem)));  // byte offset in LDS
+  const int64_t step = PRODUCT == kProductGram ? S::kSlabK * L::pitch(ld) : 64;
+  const int slabs = (PRODUCT == kProductGram ? (c + kOrthoPad - 1) / kOrthoPad * kOrthoPad : ld) / S::kSlabK;
+  // Slab n, or of its loads those with number part mod parts.
+  auto fetch = [&](int n, int part = 0, int parts = 1) {
+    const uint32_t at = lds0 + (n & 1) * S::kSlab;
+    const _Float16* from_p = p + n * step;
+    const _Float16* from_q = q + n * step;
+#pragma unroll
+    for (int i = 0; i < S::kLoadsP; ++i)
+      if (i % parts == part) load_to_lds(at + (wave + i * S::kWaves) * 1024, from_p, off_p[i]);
+#pragma unroll
+    for (int i = 0; i < S::kLoadsQ; ++i)
+      if (i % parts == part) load_to_lds(at + S::kBytesP + (wave + i * S::kWaves) * 1024, from_q, off_q[i]);
+  };
+  fetch(0);
 
   // s of this iteration: the mean of A's diagonal, ||X||^2 / r (1 / r at first)
   double s;
@@ -348,227 +532,238 @@ __global__ __launch_bounds__((ProductShape<PRODUCT, FULL, BM, BN, WM, WN, BK>::k
       s = 1.0;
     } else {
       s = 0.0;
-      for (int i = threadIdx.x; i < mt.x_tiles; i += S::kThreads) s += mt.x_part[i];
+      for (int i = threadIdx.x; i < mt.x_tiles; i += S::kThreads) s += as_global(mt.x_part)[i];
       s = block_sum<S::kThreads>(s);
     }
-    s /= mt.r;
-    if (t.m == 0 && t.n == 0 && threadIdx.x == 0) *mt.shift = s;
+    s /= r;
+    if (t.m == 0 && t.n == 0 && threadIdx.x == 0) *as_global(mt.shift) = s;
   } else {
-    s = *mt.shift;
+    s = *as_global(mt.shift);
+  }
+  const double keep = args.a + args.b * s + args.c * s * s;
+
+  constexpr int FP = WP / 16, FQ = WQ / 16;
+  static_assert(!FULL || FP >= FQ, "the order of the reads");
+  const int wp = (wave % (BP / WP)) * WP, wq = (wave / (BP / WP)) * WQ;
+  f32x4 acc[FP][FQ];
+#pragma unroll
+  for (int i = 0; i < FP; ++i)
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // The update product's results: lane l holds C^T[q][p .. p+7], q = l mod 16, p
+  // = 8 (l / 16), of each pair of 16 x 16 blocks.  FAST adds X's low half to
+  // them, which is read ahead of the sums.
+  const int p8 = t.m * BP + wp + 8 * (lane >> 4), q0 = t.n * BQ + wq + (lane & 15);
+  _Float16* to_hi = as_global(args.from ? mt.t[0][0] : mt.t[1][0]);
+  _Float16* to_lo = L::low(to_hi, as_global(mt.t[0][1]));  // FAST: read and written in place
+  constexpr bool kLow = PRODUCT == kProductUpdate && !FULL;
+  const float keep_lo = static_cast<float>(keep);
+  half8 xl[kLow ? FP / 2 : 1][kLow ? FQ : 1];
+  if constexpr (kLow) {
+#pragma unroll
+    for (int i = 0; i < FP; i += 2)
+#pragma unroll
+      for (int j = 0; j < FQ; ++j)
+        xl[i / 2][j] = *reinterpret_cast<const half8*>(
+            to_lo + L::at(min(q0 + j * 16, c - 1), min(p8 + i * 16, ld - 8), ld));
   }
 
-  const _Float16* p[2];
-  const _Float16* q[2];
-  int ld, rows_p, rows_q;
-  if constexpr (PRODUCT == kProductGram) {
-    p[0] = q[0] = mt.x[0], p[1] = q[1] = mt.x[1];
-    ld = mt.ldc, rows_p = rows_q = mt.r;
-  } else if constexpr (PRODUCT == kProductSquare) {
-    p[0] = q[0] = mt.g[0], p[1] = q[1] = mt.g[1];
-    ld = mt.ldr, rows_p = rows_q = mt.r;
-  } else {
-    p[0] = mt.t[args.from][0], p[1] = mt.t[args.from][1];
-    q[0] = mt.q[0], q[1] = mt.q[1];
-    ld = mt.ldr, rows_p = mt.c, rows_q = mt.r;
-  }
-
-  // Byte offsets of this lane's loads.  Rows past the end read the last one:
-  // what they give is not stored.
-  uint32_t off_p[S::kLoadsP], off_q[S::kLoadsQ];
-  const int lrow = lane / S::kChunks, lchunk = lane % S::kChunks;
-#pragma unroll
-  for (int i = 0; i < S::kLoadsP; ++i) {
-    const int row = (wave + i * S::kWaves) * S::kRowsPerLoad + lrow;
-    const int g = min(t.m * BM + row, rows_p - 1);
-    off_p[i] = (static_cast<uint32_t>(g) * static_cast<uint32_t>(ld)) * 2u +
-               16u * (lchunk ^ chunk_swizzle<S::kChunks>(row));
-  }
-#pragma unroll
-  for (int i = 0; i < S::kLoadsQ; ++i) {
-    const int row = (wave + i * S::kWaves) * S::kRowsPerLoad + lrow;
-    const int g = min(t.n * BN + row, rows_q - 1);
-    off_q[i] = (static_cast<uint32_t>(g) * static_cast<uint32_t>(ld)) * 2u +
-               16u * (lchunk ^ chunk_swizzle<S::kChunks>(row));
-  }
-
-  const uint32_t lds0 = static_cast<uint32_t>(
-      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)(smem)));  // byte offset in LDS
-  constexpr int kPBytes = BM * S::kRowBytes, kQBytes = BN * S::kRowBytes;
-  auto fetch = [&](int stage, int k) {
-    const uint32_t at = lds0 + stage * S::kStage;
-#pragma unroll
-    for (int h = 0; h < S::kHalves; ++h) {
-#pragma unroll
-      for (int i = 0; i < S::kLoadsP; ++i)
-        load_to_lds(at + h * kPBytes + (wave + i * S::kWaves) * 1024, p[h] + k * BK, off_p[i]);
-#pragma unroll
-      for (int i = 0; i < S::kLoadsQ; ++i)
-        load_to_lds(at + S::kHalves * kPBytes + h * kQBytes + (wave + i * S::kWaves) * 1024, q[h] + k * BK, off_q[i]);
-    }
+  auto slab = [&](int n) { return smem + (n & 1) * S::kSlab; };
+  auto read_p = [&](const char* at, int part, int i) {
+    return read_operand<kReadP, FULL, BP>(at, wp + (kReadP == kBlocks ? 16 * (i & ~1) + 4 * (i & 1) : 16 * i), part, lane);
+  };
+  auto read_q = [&](const char* at, int part, int j) {
+    return read_operand<kReadQ, FULL, BQ>(at + S::kBytesP, wq + j * 16, part, lane);
+  };
+  auto mul = [&](const half8& x, const half8& y, f32x4& to) {
+    to = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, to, 0, 0, 0);
+  };
+  // Slab n + 1 has landed, and slab n is read: slab n + 2 takes its place.
+  auto next_slab = [&](int n) {
+    slab_barrier();
+    if (n + 2 < slabs) fetch(n + 2);
   };
 
-  constexpr int FM = WM / 16, FN = WN / 16;
-  const int wm = (wave % (BM / WM)) * WM, wn = (wave / (BM / WM)) * WN;
-  f32x4 acc[FM][FN];
+  slab_barrier();
+  if (slabs > 1) fetch(1);
+  if constexpr (!FULL) {
+    half8 pf[FP], qf[2][FQ];
 #pragma unroll
-  for (int i = 0; i < FM; ++i)
+    for (int j = 0; j < FQ; ++j) qf[0][j] = read_q(slab(0), 0, j);
 #pragma unroll
-    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-  const int frow = lane & 15, fchunk = lane >> 4;
-  const int steps = ld / BK;
-  fetch(0, 0);
-  for (int k = 0; k < steps; ++k) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();  // stage k has landed for all waves, and all have read stage k - 1
-    if (k + 1 < steps) fetch((k + 1) & 1, k + 1);
-    const char* st = smem + (k & 1) * S::kStage;
+    for (int i = 0; i < FP; ++i) pf[i] = read_p(slab(0), 0, i);
+    const int own0 = t.m * BP + wp;
+    const float keep_hi = static_cast<float>(keep) * kScaleA;
+    for (int n = 0; n < slabs; ++n) {
+      const char* at = slab(n);
+      if constexpr (PRODUCT == kProductUpdate) {
+        // This slab holds X^T at p = 64 n .. of all q: where that is the wave's
+        // own part of C, the term (a + bs + cs^2) X of the high half goes in.
+        const int d = 64 * n - own0;
+        if (d > -64 && d < WP) {
 #pragma unroll
-    for (int kk = 0; kk < BK / 32; ++kk) {
-      half8 pf[S::kHalves][FM], qf[S::kHalves][FN];
+          for (int i = 0; i < FP; ++i) {
+            const int in_slab = 16 * (i & ~1) - d;  // of a pair's 32 values of p
+            if (in_slab >= 0 && in_slab < 64)
 #pragma unroll
-      for (int h = 0; h < S::kHalves; ++h) {
+              for (int j = 0; j < FQ; ++j) {
+                const int row = wq + j * 16 + (lane & 15);
+                const int chunk = chunk_swizzle<kReadQ, 8>(row, (in_slab >> 3) + (lane >> 4));
+                const half4 x = *reinterpret_cast<const half4*>(at + S::kBytesP + row * 128 + chunk * 16 + 8 * (i & 1));
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
-          const int row = wm + i * 16 + frow;
-          pf[h][i] = *reinterpret_cast<const half8*>(
-              st + h * kPBytes + row * S::kRowBytes + 16 * ((kk * 4 + fchunk) ^ chunk_swizzle<S::kChunks>(row)));
-        }
-#pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          const int row = wn + j * 16 + frow;
-          qf[h][j] = *reinterpret_cast<const half8*>(
-              st + S::kHalves * kPBytes + h * kQBytes + row * S::kRowBytes +
-              16 * ((kk * 4 + fchunk) ^ chunk_swizzle<S::kChunks>(row)));
+                for (int e = 0; e < 4; ++e) acc[i][j][e] += keep_hi * static_cast<float>(x[e]);
+              }
+          }
         }
       }
 #pragma unroll
-      for (int i = 0; i < FM; ++i)
+      for (int kk = 0; kk < 2; ++kk) {
+        if (kk == 1) next_slab(n);
+        const char* next = kk == 0 ? at : slab(n + 1);  // behind the last one: read, not used
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pf[0][i], qf[0][j], acc[i][j], 0, 0, 0);
-          if constexpr (FULL) {
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pf[0][i], qf[1][j], acc[i][j], 0, 0, 0);
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pf[1][i], qf[0][j], acc[i][j], 0, 0, 0);
-          }
+        for (int j = 0; j < FQ; ++j) qf[kk ^ 1][j] = read_q(next, kk ^ 1, j);
+#pragma unroll
+        for (int i = 0; i < FP; ++i) {
+#pragma unroll
+          for (int j = 0; j < FQ; ++j) mul(pf[i], qf[kk][j], acc[i][j]);
+          pf[i] = read_p(next, kk ^ 1, i);
+          __builtin_amdgcn_sched_barrier(0);
         }
+      }
+    }
+  } else {
+    half8 ph[FP], qh[FQ], pl[FP], ql[FQ];
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) qh[j] = read_q(slab(0), 0, j);
+#pragma unroll
+    for (int i = 0; i < FP; ++i) ph[i] = read_p(slab(0), 0, i);
+    for (int n = 0; n < slabs; ++n) {
+      const char* at = slab(n);
+#pragma unroll
+      for (int i = 0; i < FP; ++i) {
+        pl[i] = read_p(at, 1, i);
+        if (i < FQ) ql[i] = read_q(at, 1, i);
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) mul(ph[i], qh[j], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i = 0; i < FP; ++i) {
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) mul(pl[i], qh[j], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      next_slab(n);
+      const char* next = slab(n + 1);  // behind the last one: read, not used
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) qh[j] = read_q(next, 0, j);
+#pragma unroll
+      for (int i = 0; i < FP; ++i) {
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) mul(ph[i], ql[j], acc[i][j]);
+        ph[i] = read_p(next, 0, i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   }
 
-  // Lane l holds C[m .. m+3][n] of each 16 x 16 block: m = 4 (l / 16), n = l mod 16.
-  const int m0 = t.m * BM + wm + 4 * (lane >> 4), n0 = t.n * BN + wn + (lane & 15);
+  // Values behind the matrix become the zeros that its padding holds anyway.
   if constexpr (PRODUCT != kProductUpdate) {
-    const int r = mt.r;
-    const int64_t ldr = mt.ldr;
-    _Float16* dst_hi = PRODUCT == kProductGram ? mt.g[0] : mt.q[0];
-    _Float16* dst_lo = PRODUCT == kProductGram ? mt.g[1] : mt.q[1];
-    // the polynomial's low half goes into products only
-    constexpr bool kLow = PRODUCT == kProductGram || FULL;
-    const float shift = static_cast<float>(s * kScaleA);
+    // Lane l holds C[p .. p+3][q] of each 16 x 16 block, p = 4 (l / 16), q = l mod 16.
+    const int p0 = t.m * BP + wp + 4 * (lane >> 4);
+    const int quad = lane & 3;
+    const _Float16* r_hi = as_global(mt.g[0]);
+    const _Float16* r_lo = L::low(r_hi, as_global<const _Float16>(mt.g[1]));
+    _Float16* dst_hi = as_global(PRODUCT == kProductGram ? mt.g[0] : mt.q[0]);
+    _Float16* dst_lo = L::low(dst_hi, as_global(mt.g[1]));  // the square product's only with FULL
+    // F's low half goes into products only, R's into F as well
+    constexpr bool kStoreLow = PRODUCT == kProductGram || FULL;
+    // with FAST the update product adds the diagonal term itself, unrounded
+    const float diag = PRODUCT == kProductGram ? static_cast<float>(-s * kScaleA)
+                       : FULL                  ? static_cast<float>(keep * kScaleA)
+                                               : 0.f;
     const float lin = static_cast<float>(args.b + 2.0 * args.c * s);
-    const float quad = static_cast<float>(args.c) / kScaleA;
+    const float quadratic = static_cast<float>(args.c) / kScaleA;
+    half4 rh[2][FQ], rl[2][FQ];  // R, a row of blocks ahead
+    auto read_r = [&](int i) {
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+      for (int j = 0; j < FQ; ++j) {  // R is symmetric
+        const int64_t from = L::at(min(q0 + j * 16, r - 1), min(p0 + i * 16, ld - 4), ld);
+        rh[i & 1][j] = *reinterpret_cast<const half4*>(r_hi + from);
+        rl[i & 1][j] = *reinterpret_cast<const half4*>(r_lo + from);
+      }
+    };
+    if constexpr (PRODUCT == kProductSquare) read_r(0);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const int n = n0 + j * 16;
-        if (n >= r) continue;
-        half4 hi, lo;
+    for (int i = 0; i < FP; ++i) {
+      const int pp = p0 + i * 16;
+      if constexpr (PRODUCT == kProductSquare)
+        if (i + 1 < FP) read_r(i + 1);
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) {
+        const int qq = q0 + j * 16;
+        uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int m = m0 + i * 16 + e;
-          float v = 0.f;
-          if (m < r) {
-            if constexpr (PRODUCT == kProductGram) {
-              v = acc[i][j][e] * (kScaleA / (kScaleX * kScaleX));
-              if (m == n) v -= shift;
-            } else {
-              // R is symmetric: read along the row that is stored contiguously
-              const int64_t at = n * ldr + m;
-              v = lin * (static_cast<float>(mt.g[0][at]) + static_cast<float>(mt.g[1][at])) + quad * acc[i][j][e];
-            }
-          }
-          _Float16 h, l;
-          split(v, h, l);
-          hi[e] = h, lo[e] = l;
-          if (m < r && t.m != t.n) {
-            dst_hi[m * ldr + n] = h;
-            if constexpr (kLow) dst_lo[m * ldr + n] = l;
-          }
+          float v;
+          if constexpr (PRODUCT == kProductGram)
+            v = acc[i][j][e] * (kScaleA / (kScaleX * kScaleX));
+          else
+            v = lin * join(rh[i & 1][j], rl[i & 1][j], e) + quadratic * acc[i][j][e];
+          if (pp + e == qq) v += diag;
+          w[e] = pack_split(pp + e < r && qq < r ? v : 0.f);
         }
-        const int m = m0 + i * 16;
-        if (m + 3 < r) {
-          *reinterpret_cast<half4*>(dst_hi + n * ldr + m) = hi;
-          if constexpr (kLow) *reinterpret_cast<half4*>(dst_lo + n * ldr + m) = lo;
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (m + e < r) {
-              dst_hi[n * ldr + m + e] = hi[e];
-              if constexpr (kLow) dst_lo[n * ldr + m + e] = lo[e];
-            }
+        if (qq < r && pp < r) store_split<kStoreLow>(dst_hi, dst_lo, L::at(qq, pp, ld), w);
+        if (t.m != t.n) {
+          quad_transpose(w, lane);  // C[p + l mod 4][q - l mod 4 .. + 3]
+          if (pp + quad < r && qq - quad < r) store_split<kStoreLow>(dst_hi, dst_lo, L::at(pp + quad, qq - quad, ld), w);
         }
       }
+    }
   } else {
-    const int r = mt.r, c = mt.c;
-    const int64_t ldr = mt.ldr, ldc = mt.ldc;
-    _Float16* to_hi = mt.t[args.from ^ 1][0];
-    _Float16* to_lo = mt.t[args.from ^ 1][1];
-    const float keep = static_cast<float>(args.a + args.b * s + args.c * s * s);
     float sq = 0.f;
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int j = 0; j < FQ; ++j) {
+      const int qq = q0 + j * 16;
 #pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const int n = n0 + j * 16, m = m0 + i * 16;  // X[n][m .. m+3]
-        if (n >= r) continue;
-        const int64_t at = n * ldc + m;
-        half4 hi, lo;
-        float v[4];
-        const bool whole = m + 3 < c;
-        if (whole) {
-          hi = *reinterpret_cast<const half4*>(mt.x[0] + at);
-          lo = *reinterpret_cast<const half4*>(mt.x[1] + at);
+      for (int i = 0; i < FP; i += 2) {
+        const int pp = p8 + i * 16;  // X^T[q][p .. p+7]
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[e] = acc[i + (e >> 2)][j][e & 3] * (1.f / kScaleA);
+          if constexpr (!FULL) v[e] += keep_lo * static_cast<float>(xl[i / 2][j][e]);
+          if (!(pp + e < r && qq < c)) v[e] = 0.f;
         }
+        if constexpr (LAST) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = 0.f;
-          if (m + e < c) {
-            const float x = whole ? static_cast<float>(hi[e]) + static_cast<float>(lo[e])
-                                  : static_cast<float>(mt.x[0][at + e]) + static_cast<float>(mt.x[1][at + e]);
-            v[e] = keep * x + acc[i][j][e] * (1.f / kScaleA);
-          }
-        }
-        if (args.last) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (m + e < c) {
-              const int64_t o = mt.tall ? static_cast<int64_t>(m + e) * mt.cols + n
-                                        : static_cast<int64_t>(n) * mt.cols + m + e;
+          for (int e = 0; e < 8; ++e)
+            if (pp + e < r && qq < c) {
+              const int64_t o = mt.tall ? static_cast<int64_t>(qq) * mt.cols + pp + e
+                                        : static_cast<int64_t>(pp + e) * mt.cols + qq;
               out[mt.offset + o] = v[e] * (1.f / kScaleX);
             }
         } else {
+          half8 hi, lo;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < 8; ++e) {
             sq += v[e] * v[e];
             _Float16 h, l;
             split(v[e], h, l);
             hi[e] = h, lo[e] = l;
-            if (m + e < c) {
-              to_hi[(m + e) * ldr + n] = h;
-              if constexpr (FULL) to_lo[(m + e) * ldr + n] = l;
-              if (!whole) mt.x[0][at + e] = h, mt.x[1][at + e] = l;
-            }
           }
-          if (whole) {
-            *reinterpret_cast<half4*>(mt.x[0] + at) = hi;
-            *reinterpret_cast<half4*>(mt.x[1] + at) = lo;
+          if (qq < c && pp < r) {
+            const int64_t at = L::at(qq, pp, ld);
+            *reinterpret_cast<half8*>(to_hi + at) = hi;
+            *reinterpret_cast<half8*>(to_lo + at) = lo;
           }
         }
       }
-    if (!args.last) {
+    }
+    if constexpr (!LAST) {
       const double sum = block_sum<S::kThreads>(static_cast<double>(sq) / (static_cast<double>(kScaleX) * kScaleX));
-      if (threadIdx.x == 0) mt.x_part[t.slot] = sum;
+      if (threadIdx.x == 0) as_global(mt.x_part)[t.slot] = sum;
     }
   }
 }
@@ -625,20 +820,24 @@ RepPtrs reps_of(const OrthoCall& c) {
   return r;
 }
 
-template <int PRODUCT, bool FULL, int BM, int BN, int WM, int WN, int BK>
+template <int PRODUCT, bool FULL, int BP, int BQ, int WP, int WQ>
 hipError_t launch_product(const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args, float* out,
                           hipStream_t stream) {
-  using S = ProductShape<PRODUCT, FULL, BM, BN, WM, WN, BK>;
-  ortho_product_kernel<PRODUCT, FULL, BM, BN, WM, WN, BK>
-      <<<tiles.count, S::kThreads, 0, stream>>>(mats, tiles.tile, args, out);
+  using S = ProductShape<FULL, BP, BQ, WP, WQ>;
+  if (PRODUCT == kProductUpdate && args.last)
+    ortho_product_kernel<PRODUCT, FULL, PRODUCT == kProductUpdate, BP, BQ, WP, WQ>
+        <<<tiles.count, S::kThreads, 0, stream>>>(mats, tiles.tile, args, out);
+  else
+    ortho_product_kernel<PRODUCT, FULL, false, BP, BQ, WP, WQ>
+        <<<tiles.count, S::kThreads, 0, stream>>>(mats, tiles.tile, args, out);
   return hipGetLastError();
 }
 
 template <int PRODUCT>
 hipError_t launch_product_of(bool full, const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args,
                              float* out, hipStream_t stream) {
-  if (full) return launch_product<PRODUCT, true, 128, 128, 64, 64, 32>(mats, tiles, args, out, stream);
-  return launch_product<PRODUCT, false, 128, 128, 64, 64, 64>(mats, tiles, args, out, stream);
+  if (full) return launch_product<PRODUCT, true, 128, 128, 64, 64>(mats, tiles, args, out, stream);
+  return launch_product<PRODUCT, false, 128, 128, 64, 64>(mats, tiles, args, out, stream);
 }
 
 }  // namespace

@@ -36,9 +36,14 @@ int64_t oround_up(int64_t a, int64_t b) { return oceil_div(a, b) * b; }
 
 constexpr double kDefaultCoef[3] = {3.4445, -4.7750, 2.0315};
 constexpr int64_t kMaxSide = int64_t(1) << 24;
-constexpr int64_t kMaxMatrix = int64_t(1) << 30;
+constexpr int64_t kMaxMatrix = int64_t(1) << 29;
 constexpr int kXcds = 8;                          // workgroups go to the XCDs in turn
 constexpr int kProductSide = 128;
+// Side, in tiles, of the groups that tiles are taken in.  Products of a 1B
+// layer and of a 4096 x 11008 matrix, us with groups of 1, 2, 4 and 8: update
+// (FAST) 294, 259, 255, 260 and 465, 410, 373, 375; gram 164, 149, 148, 149
+// and 286, 265, 265, 263.
+constexpr int32_t kGroup = 4;
 
 struct Tables {
   std::vector<OrthoMat> mats;
@@ -106,8 +111,8 @@ edit_status_t check_layout(const edit_ortho_config_t* cfg) {
     if (m.rows < 0 || m.cols < 0) return ofail(EDIT_EINVAL, where + ": rows and cols must be >= 0");
     if (m.rows > kMaxSide || m.cols > kMaxSide) return ofail(EDIT_EINVAL, where + ": rows and cols must be at most 2^24");
     const int64_t n = static_cast<int64_t>(m.rows) * m.cols;
-    // Padding to multiples of 64 at most doubles a side above 64, and 64 sides
-    // of 2^24 are 2^30: byte offsets within a matrix stay below 2^32.
+    // Padding the short side to a multiple of 64 at most doubles it from 32 on,
+    // and 64 sides of 2^24 are 2^30: at four bytes, offsets stay below 2^32.
     if (n > kMaxMatrix) return ofail(EDIT_EINVAL, where + " is too large");
     if (m.offset < 0 || m.offset > cfg->numel || n > cfg->numel - m.offset)
       return ofail(EDIT_EINVAL, where + " reaches beyond the unit");
@@ -121,7 +126,7 @@ edit_status_t check_layout(const edit_ortho_config_t* cfg) {
 }
 
 // The tiles of all matrices, so that the workgroups of an XCD (every eighth)
-// take neighbouring tiles of a matrix, whose operands they share in its L2;
+// take neighbouring ones of a matrix, whose operands they share in its L2;
 // matrices with the longest sums first, so that short ones fill the end.
 std::vector<OrthoTile> spread(const std::vector<std::vector<OrthoTile>>& of_matrix, const std::vector<int>& order) {
   std::vector<OrthoTile> list[kXcds];
@@ -170,7 +175,7 @@ Tables make_tables(const edit_ortho_config_t* cfg) {
     m.scale = in.scale;
     m.rows = in.rows, m.cols = in.cols;
     m.r = std::min(in.rows, in.cols), m.c = std::max(in.rows, in.cols);
-    m.ldr = static_cast<int32_t>(oround_up(m.r, kOrthoPad)), m.ldc = static_cast<int32_t>(oround_up(m.c, kOrthoPad));
+    m.ldr = static_cast<int32_t>(oround_up(m.r, kOrthoPad));
     m.tall = in.rows > in.cols;
     const int64_t end = in.offset + static_cast<int64_t>(in.rows) * in.cols;
     used.push_back({in.offset, end});
@@ -178,12 +183,17 @@ Tables make_tables(const edit_ortho_config_t* cfg) {
     for (int32_t a = 0; a < oceil_div(in.rows, kOrthoLoadTile); ++a)
       for (int32_t b = 0; b < oceil_div(in.cols, kOrthoLoadTile); ++b) t.load.push_back({k, a, b, 0});
     const int32_t tr = static_cast<int32_t>(oceil_div(m.r, kProductSide)), tc = static_cast<int32_t>(oceil_div(m.c, kProductSide));
+    // in groups of kGroup x kGroup tiles, which share operands while they run
     gram.emplace_back();
-    for (int32_t a = 0; a < tr; ++a)
-      for (int32_t b = 0; b <= a; ++b) gram.back().push_back({k, a, b, 0});
+    for (int32_t p = 0; p < tr; p += kGroup)
+      for (int32_t q = 0; q <= p; q += kGroup)
+        for (int32_t a = p; a < std::min(tr, p + kGroup); ++a)
+          for (int32_t b = q; b <= std::min(a, q + kGroup - 1); ++b) gram.back().push_back({k, a, b, 0});
     update.emplace_back();
-    for (int32_t a = 0; a < tc; ++a)
-      for (int32_t b = 0; b < tr; ++b) update.back().push_back({k, a, b, m.x_tiles++});
+    for (int32_t q = 0; q < tc; q += kGroup)
+      for (int32_t p = 0; p < tr; p += kGroup)
+        for (int32_t b = q; b < std::min(tc, q + kGroup); ++b)
+          for (int32_t a = p; a < std::min(tr, p + kGroup); ++a) update.back().push_back({k, a, b, m.x_tiles++});
     t.mats.push_back(m);
   }
   t.matrix_chunks = static_cast<int>(t.chunks.size());
@@ -218,16 +228,15 @@ struct Carver {
 size_t lay_out(edit_ortho* h, Tables& t, char* base) {
   Carver c{base};
   for (OrthoMat& m : t.mats) {
-    const size_t x = static_cast<size_t>(m.r) * m.ldc, xt = static_cast<size_t>(m.c) * m.ldr,
-                 a = static_cast<size_t>(m.r) * m.ldr;
-    for (auto& p : m.x) p = c.take<_Float16>(x);
-    for (auto& b : m.t) {
-      b[0] = c.take<_Float16>(xt);
-      b[1] = h->full ? c.take<_Float16>(xt) : nullptr;
+    const size_t xt = static_cast<size_t>(oround_up(m.c, kOrthoPad)) * m.ldr, a = static_cast<size_t>(m.r) * m.ldr;
+    if (h->full) {
+      m.t[0][0] = c.take<_Float16>(2 * xt), m.t[1][0] = c.take<_Float16>(2 * xt);
+      m.g[0] = c.take<_Float16>(2 * a), m.q[0] = c.take<_Float16>(2 * a);
+    } else {  // X's low half is read and written in place
+      m.t[0][0] = c.take<_Float16>(xt), m.t[1][0] = c.take<_Float16>(xt);
+      m.t[0][1] = m.t[1][1] = c.take<_Float16>(xt);
+      m.g[0] = c.take<_Float16>(a), m.g[1] = c.take<_Float16>(a), m.q[0] = c.take<_Float16>(a);
     }
-    for (auto& p : m.g) p = c.take<_Float16>(a);
-    m.q[0] = c.take<_Float16>(a);
-    m.q[1] = h->full ? c.take<_Float16>(a) : nullptr;
     m.norm_part = c.take<double>(m.chunks);
     m.x_part = c.take<double>(m.x_tiles);
     m.shift = c.take<double>(1);

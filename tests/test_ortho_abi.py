@@ -68,7 +68,7 @@ BIG = 2 ** 40
     (dict(matrices=((0, 8, 8, math.nan),)), "scale"),
     (dict(matrices=((0, 8, 8, math.inf),)), "scale"),
     (dict(numel=BIG, matrices=((0, 2 ** 24 + 1, 1, 1.0),)), "2^24"),
-    (dict(numel=BIG, matrices=((0, 2 ** 15 + 1, 2 ** 15, 1.0),)), "too large"),
+    (dict(numel=BIG, matrices=((0, 2 ** 15 + 1, 2 ** 14, 1.0),)), "too large"),
     (dict(numel=BIG, matrices=((0, 2 ** 31 - 1, 2 ** 31 - 1, 1.0),)), "2^24"),
     (dict(steps=1, coefficients=(math.nan, 0, 0)), "finite"),
     (dict(steps=2, coefficients=(1, 0, 0, 1, math.inf, 0)), "step 1"),
@@ -90,8 +90,8 @@ def test_init_refuses(over, needle):
     dict(matrices=((64, 0, 8, 1.0), (3, 5, 0, 0.0))),
     dict(matrices=((0, 4, 8, 1.0), (32, 8, 4, -1.0))),
     dict(steps=1, coefficients=(8.2, -23.0, 16.8)),
-    dict(numel=2 ** 30, matrices=((0, 2 ** 15, 2 ** 15, 1.0),)),
-    dict(numel=BIG, matrices=((0, 40, 2 ** 24, 1.0),)),
+    dict(numel=2 ** 29, matrices=((0, 2 ** 15, 2 ** 14, 1.0),)),
+    dict(numel=BIG, matrices=((0, 32, 2 ** 24, 1.0),)),
 ])
 def test_init_accepts_up_to_the_device(over):
     rc, msg = _init(**over)
