@@ -28,6 +28,18 @@ constexpr int kOrthoStreamThreads = 256;
 constexpr int kOrthoMaxChunks = 512;    // chunks (norm partials) of one matrix
 constexpr int kOrthoLoadTile = 64;      // side of the load pass's tiles
 
+// Matrices that one block takes whole: X^T and A, high and low halves, in LDS,
+// rows of r rounded up to 32 values and eight more.
+constexpr int kOrthoSmallThreads = 512;
+constexpr int kOrthoSmallSide = 128;   // of A
+constexpr int kOrthoSmallRows = 256;   // of X^T
+constexpr int kOrthoSmallLds = 152 * 1024;
+inline bool ortho_is_small(int64_t r, int64_t c) {
+  if (r > kOrthoSmallSide || c > kOrthoSmallRows) return false;
+  const int64_t rp = (r + 31) / 32 * 32, cp = (c + 31) / 32 * 32;
+  return (cp + rp) * (rp + 8) * 4 <= kOrthoSmallLds;
+}
+
 // One matrix of a unit: r = min(rows, cols), c = max(rows, cols).  The
 // working matrix X is r x c: the stored one, or its transpose where rows >
 // cols.  Every array is zero behind its r columns.
@@ -98,6 +110,9 @@ hipError_t launch_ortho_load(bool full, const OrthoCall& call, const OrthoMat* m
 // One product of an iteration; `side`: of its tiles, `from`: the X^T buffer read, `last`: O to `u` instead of X^T.
 hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const OrthoMat* mats, const OrthoTiles& tiles,
                                 const OrthoCoef& coef, int from, bool first, bool last, float* u, hipStream_t stream);
+// The whole call but the outer step's source pass, for small matrices only, one per block.
+hipError_t launch_ortho_small(bool full, const OrthoCall& call, const OrthoMat* mats, int count, const OrthoCoef* coef,
+                              int steps, hipStream_t stream);
 // The call's outputs from O.
 hipError_t launch_ortho_apply(const OrthoCall& call, const OrthoMat* mats, const OrthoChunk* chunks, int count,
                               hipStream_t stream);

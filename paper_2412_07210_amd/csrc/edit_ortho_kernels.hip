@@ -810,6 +810,261 @@ __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_apply_kernel(OrthoA
   }
 }
 
+// ----------------------------------------------------------- small matrices
+
+// The whole call for one matrix per block, where X and A fit into LDS
+// (ortho_is_small): no launch between the products, whose latency bounds
+// matrices of this size.  LDS holds X^T [c][r] and R, then F, [r][r], high and
+// low halves apart, in rows of r rounded up to 32 values and eight more (rows
+// then begin in different banks); what pads them is zero.  Wave w takes the
+// 16 rows 16 w .. of the symmetric products, all columns, so that R and F stay
+// in its registers as well, and rows 16 w + 128 t of X^T.
+struct SmallCoef {
+  double v[EDIT_ORTHO_MAX_STEPS][3];
+};
+
+// O of one element into the call's outputs.
+template <int SOURCE, bool BF16>
+__device__ __forceinline__ void apply_one(const OrthoArgs& a, const RepPtrs& reps, double step, bool rollback, int64_t i,
+                                          float o) {
+  if constexpr (SOURCE == kSourcePlain) {
+    store_one<BF16>(a.out, i, o);
+  } else if constexpr (SOURCE == kSourceLocal) {
+    const double p = load_one<BF16>(a.out, i);
+    store_one<BF16>(a.out, i, static_cast<float>(fma(a.keep, p, -step * static_cast<double>(o))));
+  } else {
+    float th = a.theta[i];
+    if (!rollback) {
+      th = static_cast<float>(fma(-step, static_cast<double>(o), static_cast<double>(th)));
+      a.theta[i] = th;
+    }
+    for (int j = 0; j < a.workers; ++j) store_one<BF16>(reps.p[j], i, th);
+  }
+}
+
+template <int SOURCE, bool BF16, bool FULL>
+__global__ __launch_bounds__(kOrthoSmallThreads) void ortho_small_kernel(OrthoArgs a, RepPtrs reps,
+                                                                        const OrthoMat* __restrict__ mats,
+                                                                        SmallCoef coef, int steps) {
+  constexpr int kThreads = kOrthoSmallThreads;
+  constexpr int kBlocks = kOrthoSmallSide / 16;                // of a row of A
+  constexpr int kRows = kOrthoSmallRows / 16 / (kThreads / 64);  // blocks of X^T's rows per wave
+  __shared__ __align__(256) char smem[kOrthoSmallLds];
+  const OrthoMat mt = mats[blockIdx.x];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = mt.r, c = mt.c, rp = (r + 31) & ~31, cp = (c + 31) & ~31;
+  const int pitch = rp + 8;
+  _Float16* x_hi = reinterpret_cast<_Float16*>(smem);
+  _Float16* x_lo = x_hi + cp * pitch;
+  _Float16* g_hi = x_lo + cp * pitch;
+  _Float16* g_lo = g_hi + rp * pitch;
+  const int64_t n = static_cast<int64_t>(r) * c;
+
+  // u, its norm, and X^T = u / ||u||
+  auto update_of = [&](int64_t i) -> double {
+    if constexpr (SOURCE == kSourcePlain) return load_one<BF16>(a.x, i);
+    if constexpr (SOURCE == kSourceOuter) return a.u[i];
+    const double m = a.momentum[i];
+    return a.nesterov ? fma(a.mu, m, static_cast<double>(load_one<BF16>(a.x, i))) : m;
+  };
+  for (int i = threadIdx.x; i < 2 * (cp + rp) * pitch / 8; i += kThreads)
+    reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
+  double sum = 0.0;
+  for (int64_t e = threadIdx.x; e < n; e += kThreads) {
+    const int64_t i = mt.offset + e;
+    if constexpr (SOURCE == kSourceLocal)
+      a.momentum[i] = static_cast<float>(fma(a.mu, static_cast<double>(a.momentum[i]), static_cast<double>(load_one<BF16>(a.x, i))));
+    const double u = update_of(i);
+    sum = fma(u, u, sum);
+  }
+  sum = block_sum<kThreads>(sum);
+  const double inv = sum > 0.0 ? kScaleX / sqrt(sum) : (sum == 0.0 ? 0.0 : sum);
+  for (int e = threadIdx.x; e < n; e += kThreads) {
+    const int row = e / mt.cols, col = e - row * mt.cols;
+    _Float16 hi, lo;
+    split(static_cast<float>(update_of(mt.offset + e) * inv), hi, lo);
+    const int at = mt.tall ? row * pitch + col : col * pitch + row;
+    x_hi[at] = hi, x_lo[at] = lo;
+  }
+  __syncthreads();
+
+  const int blocks = rp / 16;
+  const int l16 = lane & 15, l4 = lane >> 4;
+  // eight values along k of row `row0` + l16
+  auto along = [&](const _Float16* m, int row0, int k) {
+    return *reinterpret_cast<const half8*>(m + (row0 + l16) * pitch + k + 8 * l4);
+  };
+  // eight rows from `k` + 8 l4 on of column `col0` + l16
+  auto across = [&](const _Float16* m, int col0, int k) {
+    half8 out;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const _Float16* at = m + (k + 8 * l4 + 4 * h + (l16 >> 2)) * pitch + col0 + 4 * (l16 & 3);
+      const half4 v = __builtin_bit_cast(
+          half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) fp16x4*)(at)));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[4 * h + e] = v[e];
+    }
+    return out;
+  };
+  auto mul = [&](const half8& x, const half8& y, f32x4& to) {
+    to = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, to, 0, 0, 0);
+  };
+  // four neighbours of row `row`, high and low halves
+  auto put = [&](_Float16* hi, _Float16* lo, int row, int col, const f32x4& v) {
+    half4 h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      _Float16 x, y;
+      split(v[e], x, y);
+      h[e] = x, l[e] = y;
+    }
+    *reinterpret_cast<half4*>(hi + row * pitch + col) = h;
+    *reinterpret_cast<half4*>(lo + row * pitch + col) = l;
+  };
+
+  float* o = reinterpret_cast<float*>(smem);  // [c][pitch], over both halves of X^T
+  double s = 1.0 / r;
+  for (int k = 0; k < steps; ++k) {
+    const double ca = coef.v[k][0], cb = coef.v[k][1], cc = coef.v[k][2];
+    const double keep = ca + cb * s + cc * s * s;
+    const int p0 = 16 * wave;
+    f32x4 g[kBlocks];  // lane l: [p0 + l16][16 j + 4 l4 ..], R and then F
+#pragma unroll
+    for (int j = 0; j < kBlocks; ++j) g[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (wave < blocks) {
+      for (int t = 0; t < cp; t += 32) {
+        const half8 q = across(x_hi, p0, t);
+        half8 ql;
+        if constexpr (FULL) ql = across(x_lo, p0, t);
+#pragma unroll
+        for (int j = 0; j < kBlocks; ++j) {
+          if (j >= blocks) continue;
+          const half8 p = across(x_hi, 16 * j, t);
+          mul(p, q, g[j]);
+          if constexpr (FULL) {
+            mul(p, ql, g[j]);
+            mul(across(x_lo, 16 * j, t), q, g[j]);
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kBlocks; ++j) {
+        if (j >= blocks) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int p = 16 * j + 4 * l4 + e;
+          g[j][e] *= kScaleA / (kScaleX * kScaleX);
+          // behind the matrix R stays zero, and F with it
+          if (p == p0 + l16 && p < r) g[j][e] -= static_cast<float>(s * kScaleA);
+        }
+        put(g_hi, g_lo, p0 + l16, 16 * j + 4 * l4, g[j]);
+      }
+    }
+    __syncthreads();
+    f32x4 f[kBlocks];
+#pragma unroll
+    for (int j = 0; j < kBlocks; ++j) f[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (wave < blocks)
+      for (int t = 0; t < rp; t += 32) {
+        const half8 q = along(g_hi, p0, t);
+        half8 ql;
+        if constexpr (FULL) ql = along(g_lo, p0, t);
+#pragma unroll
+        for (int j = 0; j < kBlocks; ++j) {
+          if (j >= blocks) continue;
+          const half8 p = along(g_hi, 16 * j, t);
+          mul(p, q, f[j]);
+          if constexpr (FULL) {
+            mul(p, ql, f[j]);
+            mul(along(g_lo, 16 * j, t), q, f[j]);
+          }
+        }
+      }
+    __syncthreads();
+    if (wave < blocks) {
+      const float lin = static_cast<float>(cb + 2.0 * cc * s), quadratic = static_cast<float>(cc) / kScaleA;
+#pragma unroll
+      for (int j = 0; j < kBlocks; ++j) {
+        if (j >= blocks) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f[j][e] = lin * g[j][e] + quadratic * f[j][e];
+          if (FULL && 16 * j + 4 * l4 + e == p0 + l16) f[j][e] += static_cast<float>(keep * kScaleA);
+        }
+        put(g_hi, g_lo, p0 + l16, 16 * j + 4 * l4, f[j]);
+      }
+    }
+    __syncthreads();
+    f32x4 x[kRows][kBlocks];  // lane l: X^T[16 (wave + 8 t) + l16][16 j + 4 l4 ..]
+    const float keep_x = static_cast<float>(keep) * kScaleA;
+#pragma unroll
+    for (int t = 0; t < kRows; ++t) {
+      const int q0 = 16 * (wave + t * (kThreads / 64));
+      if (q0 >= cp) continue;
+#pragma unroll
+      for (int j = 0; j < kBlocks; ++j) {
+        x[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (j >= blocks || FULL) continue;
+        // with FAST the term (a + bs + cs^2) X is taken from both halves as they are
+        const int at = (q0 + l16) * pitch + 16 * j + 4 * l4;
+        const half4 h = *reinterpret_cast<const half4*>(x_hi + at), l = *reinterpret_cast<const half4*>(x_lo + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[t][j][e] = keep_x * join(h, l, e);
+      }
+      for (int kk = 0; kk < rp; kk += 32) {
+        const half8 q = along(x_hi, q0, kk);
+        half8 ql;
+        if constexpr (FULL) ql = along(x_lo, q0, kk);
+#pragma unroll
+        for (int j = 0; j < kBlocks; ++j) {
+          if (j >= blocks) continue;
+          const half8 p = along(g_hi, 16 * j, kk);
+          mul(p, q, x[t][j]);
+          if constexpr (FULL) {
+            mul(p, ql, x[t][j]);
+            mul(along(g_lo, 16 * j, kk), q, x[t][j]);
+          }
+        }
+      }
+    }
+    __syncthreads();
+    float sq = 0.f;
+#pragma unroll
+    for (int t = 0; t < kRows; ++t) {
+      const int q0 = 16 * (wave + t * (kThreads / 64));
+      if (q0 >= cp) continue;
+#pragma unroll
+      for (int j = 0; j < kBlocks; ++j) {
+        if (j >= blocks) continue;
+        const int q = q0 + l16, p = 16 * j + 4 * l4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[t][j][e] *= 1.f / kScaleA;
+          if (!(p + e < r && q < c)) x[t][j][e] = 0.f;  // a NaN in the matrix would reach the padding
+          sq += x[t][j][e] * x[t][j][e];
+        }
+        if (k + 1 < steps)
+          put(x_hi, x_lo, q, p, x[t][j]);
+        else  // O, where X^T was
+          *reinterpret_cast<f32x4*>(o + q * pitch + p) = x[t][j];
+      }
+    }
+    if (k + 1 < steps)
+      s = block_sum<kThreads>(static_cast<double>(sq) / (static_cast<double>(kScaleX) * kScaleX)) / r;
+  }
+  __syncthreads();
+  bool rollback = false;
+  if constexpr (SOURCE == kSourceOuter) rollback = a.rec->rollback;
+  const double step = a.lr * mt.scale;
+  for (int e = threadIdx.x; e < n; e += kThreads) {
+    const int row = e / mt.cols, col = e - row * mt.cols;
+    apply_one<SOURCE, BF16>(a, reps, step, rollback, mt.offset + e,
+                            o[mt.tall ? row * pitch + col : col * pitch + row] * (1.f / kScaleX));
+  }
+}
+
 OrthoArgs args_of(const OrthoCall& c) {
   return {c.x, c.out, c.momentum, c.theta, c.u, c.rec, c.workers, c.nesterov, c.mu, c.keep, c.lr};
 }
@@ -833,11 +1088,12 @@ hipError_t launch_product(const OrthoMat* mats, const OrthoTiles& tiles, const P
   return hipGetLastError();
 }
 
-template <int PRODUCT>
-hipError_t launch_product_of(bool full, const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args,
+template <int PRODUCT, bool FULL>
+hipError_t launch_product_of(int side, const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args,
                              float* out, hipStream_t stream) {
-  if (full) return launch_product<PRODUCT, true, 128, 128, 64, 64>(mats, tiles, args, out, stream);
-  return launch_product<PRODUCT, false, 128, 128, 64, 64>(mats, tiles, args, out, stream);
+  if (side == 128) return launch_product<PRODUCT, FULL, 128, 128, 64, 64>(mats, tiles, args, out, stream);
+  if (side == 64) return launch_product<PRODUCT, FULL, 64, 64, 32, 32>(mats, tiles, args, out, stream);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -876,14 +1132,36 @@ hipError_t launch_ortho_load(bool full, const OrthoCall& call, const OrthoMat* m
 hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const OrthoMat* mats, const OrthoTiles& tiles,
                                 const OrthoCoef& coef, int from, bool first, bool last, float* u, hipStream_t stream) {
   if (tiles.count == 0) return hipSuccess;
-  if (side != 128) return hipErrorInvalidValue;
   const ProductArgs args = {coef.a, coef.b, coef.c, from, first, last};
+#define EDIT_PRODUCT(P)                                                        \
+  (full ? launch_product_of<P, true>(side, mats, tiles, args, u, stream) \
+        : launch_product_of<P, false>(side, mats, tiles, args, u, stream))
   switch (product) {
-    case kProductGram: return launch_product_of<kProductGram>(full, mats, tiles, args, u, stream);
-    case kProductSquare: return launch_product_of<kProductSquare>(full, mats, tiles, args, u, stream);
-    case kProductUpdate: return launch_product_of<kProductUpdate>(full, mats, tiles, args, u, stream);
+    case kProductGram: return EDIT_PRODUCT(kProductGram);
+    case kProductSquare: return EDIT_PRODUCT(kProductSquare);
+    case kProductUpdate: return EDIT_PRODUCT(kProductUpdate);
   }
+#undef EDIT_PRODUCT
   return hipErrorInvalidValue;
+}
+
+hipError_t launch_ortho_small(bool full, const OrthoCall& call, const OrthoMat* mats, int count, const OrthoCoef* coef,
+                              int steps, hipStream_t stream) {
+  if (count == 0) return hipSuccess;
+  const OrthoArgs a = args_of(call);
+  const RepPtrs r = reps_of(call);
+  SmallCoef sc = {};
+  for (int k = 0; k < steps; ++k) sc.v[k][0] = coef[k].a, sc.v[k][1] = coef[k].b, sc.v[k][2] = coef[k].c;
+#define EDIT_SMALL(S, B)                                                                                  \
+  (full ? ortho_small_kernel<S, B, true><<<count, kOrthoSmallThreads, 0, stream>>>(a, r, mats, sc, steps) \
+        : ortho_small_kernel<S, B, false><<<count, kOrthoSmallThreads, 0, stream>>>(a, r, mats, sc, steps))
+  switch (call.source) {
+    case kSourcePlain: call.bf16 ? EDIT_SMALL(kSourcePlain, true) : EDIT_SMALL(kSourcePlain, false); break;
+    case kSourceLocal: call.bf16 ? EDIT_SMALL(kSourceLocal, true) : EDIT_SMALL(kSourceLocal, false); break;
+    case kSourceOuter: call.bf16 ? EDIT_SMALL(kSourceOuter, true) : EDIT_SMALL(kSourceOuter, false); break;
+  }
+#undef EDIT_SMALL
+  return hipGetLastError();
 }
 
 hipError_t launch_ortho_apply(const OrthoCall& call, const OrthoMat* mats, const OrthoChunk* chunks, int count,

@@ -38,7 +38,16 @@ constexpr double kDefaultCoef[3] = {3.4445, -4.7750, 2.0315};
 constexpr int64_t kMaxSide = int64_t(1) << 24;
 constexpr int64_t kMaxMatrix = int64_t(1) << 29;
 constexpr int kXcds = 8;                          // workgroups go to the XCDs in turn
-constexpr int kProductSide = 128;
+// Sides of the products' tiles.  A CU runs two 128 x 128 tiles side by side at
+// about the time of one, and 64 x 64 tiles take up to 1.4 times the time per
+// operation but fill the GPU with a quarter of the work.  us at 128 and 64, n
+// matrices of 1024 x 1024 (FAST): symmetric products of 40 tiles (of 128 x
+// 128) 19 and 8, 160: 22 and 18, 240: 23 and 24, 280: 33 and 25, 400: 34 and
+// 33, 480: 35 and 39; update product of 64 tiles 14 and 8, 192: 18 and 15, 256:
+// 19 and 20, 512: 29 and 35.
+constexpr int kLargeSide = 128, kSmallSide = 64;
+int symmetric_side(int64_t large_tiles, int num_cu) { return 2 * large_tiles <= 3 * num_cu ? kSmallSide : kLargeSide; }
+int update_side(int64_t large_tiles, int num_cu) { return large_tiles < num_cu ? kSmallSide : kLargeSide; }
 // Side, in tiles, of the groups that tiles are taken in.  Products of a 1B
 // layer and of a 4096 x 11008 matrix, us with groups of 1, 2, 4 and 8: update
 // (FAST) 294, 259, 255, 260 and 465, 410, 373, 375; gram 164, 149, 148, 149
@@ -50,6 +59,8 @@ struct Tables {
   std::vector<OrthoChunk> chunks;
   int matrix_chunks = 0;  // the first ones belong to matrices
   std::vector<OrthoTile> load, gram, update;
+  int gram_side = kLargeSide, update_side = kLargeSide;
+  bool small = false;  // one block takes each matrix whole
 };
 
 }  // namespace
@@ -66,6 +77,9 @@ struct edit_ortho {
   OrthoTile* load = nullptr;
   int load_tiles = 0;
   OrthoTiles gram{}, update{};
+  int gram_side = 0, update_side = 0;
+  bool small = false;
+  int matrices = 0;
   float* u = nullptr;
 };
 
@@ -162,7 +176,7 @@ void add_chunks(std::vector<OrthoChunk>& out, int64_t begin, int64_t end, int ma
   if (count) *count = slot;
 }
 
-Tables make_tables(const edit_ortho_config_t* cfg) {
+Tables make_tables(const edit_ortho_config_t* cfg, int num_cu) {
   Tables t;
   std::vector<std::pair<int64_t, int64_t>> used;
   std::vector<std::vector<OrthoTile>> gram, update;
@@ -182,19 +196,35 @@ Tables make_tables(const edit_ortho_config_t* cfg) {
     add_chunks(t.chunks, in.offset, end, k, kOrthoMaxChunks, &m.chunks);
     for (int32_t a = 0; a < oceil_div(in.rows, kOrthoLoadTile); ++a)
       for (int32_t b = 0; b < oceil_div(in.cols, kOrthoLoadTile); ++b) t.load.push_back({k, a, b, 0});
-    const int32_t tr = static_cast<int32_t>(oceil_div(m.r, kProductSide)), tc = static_cast<int32_t>(oceil_div(m.c, kProductSide));
+    t.mats.push_back(m);
+  }
+  int64_t symmetric = 0, whole = 0;  // tiles at the large side
+  for (const OrthoMat& m : t.mats) {
+    const int64_t tr = oceil_div(m.r, kLargeSide), tc = oceil_div(m.c, kLargeSide);
+    symmetric += tr * (tr + 1) / 2;
+    whole += tr * tc;
+  }
+  t.small = !t.mats.empty() && std::all_of(t.mats.begin(), t.mats.end(),
+                                           [](const OrthoMat& m) { return ortho_is_small(m.r, m.c); });
+  t.gram_side = symmetric_side(symmetric, num_cu);
+  t.update_side = update_side(whole, num_cu);
+  for (size_t k = 0; k < t.mats.size(); ++k) {
+    OrthoMat& m = t.mats[k];
+    const int32_t id = static_cast<int32_t>(k);
     // in groups of kGroup x kGroup tiles, which share operands while they run
+    const int32_t ts = static_cast<int32_t>(oceil_div(m.r, t.gram_side));
     gram.emplace_back();
-    for (int32_t p = 0; p < tr; p += kGroup)
+    for (int32_t p = 0; p < ts; p += kGroup)
       for (int32_t q = 0; q <= p; q += kGroup)
-        for (int32_t a = p; a < std::min(tr, p + kGroup); ++a)
-          for (int32_t b = q; b <= std::min(a, q + kGroup - 1); ++b) gram.back().push_back({k, a, b, 0});
+        for (int32_t a = p; a < std::min(ts, p + kGroup); ++a)
+          for (int32_t b = q; b <= std::min(a, q + kGroup - 1); ++b) gram.back().push_back({id, a, b, 0});
+    const int32_t tr = static_cast<int32_t>(oceil_div(m.r, t.update_side));
+    const int32_t tc = static_cast<int32_t>(oceil_div(m.c, t.update_side));
     update.emplace_back();
     for (int32_t q = 0; q < tc; q += kGroup)
       for (int32_t p = 0; p < tr; p += kGroup)
         for (int32_t b = q; b < std::min(tc, q + kGroup); ++b)
-          for (int32_t a = p; a < std::min(tr, p + kGroup); ++a) update.back().push_back({k, a, b, m.x_tiles++});
-    t.mats.push_back(m);
+          for (int32_t a = p; a < std::min(tr, p + kGroup); ++a) update.back().push_back({id, a, b, m.x_tiles++});
   }
   t.matrix_chunks = static_cast<int>(t.chunks.size());
   std::sort(used.begin(), used.end());
@@ -249,6 +279,9 @@ size_t lay_out(edit_ortho* h, Tables& t, char* base) {
   OrthoTile* update = c.take<OrthoTile>(t.update.size());
   h->gram = {gram, static_cast<int32_t>(t.gram.size())};
   h->update = {update, static_cast<int32_t>(t.update.size())};
+  h->gram_side = t.gram_side, h->update_side = t.update_side;
+  h->small = t.small;
+  h->matrices = static_cast<int>(t.mats.size());
   h->matrix_chunks = t.matrix_chunks;
   h->all_chunks = static_cast<int>(t.chunks.size());
   h->load_tiles = static_cast<int>(t.load.size());
@@ -284,20 +317,26 @@ bool buffers_overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_by
 
 edit_status_t enqueue(edit_ortho* h, OrthoCall call, hipStream_t s) {
   call.u = h->u;
-  hipError_t e = launch_ortho_source(call, h->mats, h->chunks,
+  const int steps = static_cast<int>(h->coef.size());
+  hipError_t e = hipSuccess;
+  if (h->small) {
+    if (call.source == kSourceOuter) e = launch_ortho_source(call, h->mats, h->chunks, h->all_chunks, s);
+    if (e == hipSuccess) e = launch_ortho_small(h->full, call, h->mats, h->matrices, h->coef.data(), steps, s);
+    return e == hipSuccess ? EDIT_OK : ofail_hip(e, "small matrices launch");
+  }
+  e = launch_ortho_source(call, h->mats, h->chunks,
                                      call.source == kSourceOuter ? h->all_chunks : h->matrix_chunks, s);
   if (e != hipSuccess) return ofail_hip(e, "source pass launch");
   if (h->matrix_chunks == 0) return EDIT_OK;
   if ((e = launch_ortho_load(h->full, call, h->mats, h->load, h->load_tiles, s)) != hipSuccess)
     return ofail_hip(e, "load pass launch");
-  const int steps = static_cast<int>(h->coef.size());
   for (int k = 0; k < steps; ++k) {
     const bool first = k == 0, last = k == steps - 1;
-    e = launch_ortho_product(kProductGram, h->full, kProductSide, h->mats, h->gram, h->coef[k], k & 1, first, last, h->u, s);
+    e = launch_ortho_product(kProductGram, h->full, h->gram_side, h->mats, h->gram, h->coef[k], k & 1, first, last, h->u, s);
     if (e == hipSuccess)
-      e = launch_ortho_product(kProductSquare, h->full, kProductSide, h->mats, h->gram, h->coef[k], k & 1, first, last, h->u, s);
+      e = launch_ortho_product(kProductSquare, h->full, h->gram_side, h->mats, h->gram, h->coef[k], k & 1, first, last, h->u, s);
     if (e == hipSuccess)
-      e = launch_ortho_product(kProductUpdate, h->full, kProductSide, h->mats, h->update, h->coef[k], k & 1, first, last, h->u, s);
+      e = launch_ortho_product(kProductUpdate, h->full, h->update_side, h->mats, h->update, h->coef[k], k & 1, first, last, h->u, s);
     if (e != hipSuccess) return ofail_hip(e, "product launch");
   }
   if ((e = launch_ortho_apply(call, h->mats, h->chunks, h->matrix_chunks, s)) != hipSuccess)
@@ -358,7 +397,7 @@ edit_status_t edit_ortho_init(const edit_ortho_config_t* cfg, edit_ortho_t* out)
     h->full = cfg->precision == EDIT_ORTHO_FULL;
     h->device = dev;
     h->coef = coef;
-    Tables t = make_tables(cfg);
+    Tables t = make_tables(cfg, num_cu);
     const size_t total = std::max<size_t>(lay_out(h, t, nullptr), 256);
     hipError_t e = hipMalloc(reinterpret_cast<void**>(&h->arena), total);
     if (e != hipSuccess) {
