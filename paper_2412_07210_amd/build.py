@@ -22,7 +22,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(PKG, "_build")
 LIBRARY = os.path.join(PKG, "libedit_outer.so")
 SOURCES = ["edit_outer_dispatch.hip", "edit_outer_runtime.hip", "edit_group_kernels.hip", "edit_group_runtime.hip",
-           "edit_ortho_kernels.hip", "edit_ortho_runtime.hip"]
+           "edit_ortho_kernels.hip", "edit_ortho_small.hip", "edit_ortho_runtime.hip"]
 # Compiled once per range of worker counts K (EDIT_K_RANGES in
 # edit_outer_internal.h), so its template instantiations build in parallel.
 KERNELS = "edit_outer_kernels.hip"

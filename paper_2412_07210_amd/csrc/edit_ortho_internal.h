@@ -33,9 +33,11 @@ constexpr int kOrthoLoadTile = 64;      // side of the load pass's tiles
 constexpr int kOrthoSmallThreads = 512;
 constexpr int kOrthoSmallSide = 128;   // of A
 constexpr int kOrthoSmallRows = 256;   // of X^T
-constexpr int kOrthoSmallLds = 152 * 1024;
+constexpr int kOrthoSmallLds = 148 * 1024;
+constexpr int kOrthoSmallSlack = 10 * 1024;  // behind: reads of 128 columns or rows where there are fewer
+constexpr int kOrthoSmallPer = 48;     // elements per thread, at most
 inline bool ortho_is_small(int64_t r, int64_t c) {
-  if (r > kOrthoSmallSide || c > kOrthoSmallRows) return false;
+  if (r > kOrthoSmallSide || c > kOrthoSmallRows || r * c > kOrthoSmallPer * kOrthoSmallThreads) return false;
   const int64_t rp = (r + 31) / 32 * 32, cp = (c + 31) / 32 * 32;
   return (cp + rp) * (rp + 8) * 4 <= kOrthoSmallLds;
 }
@@ -68,7 +70,9 @@ struct OrthoChunk {
 
 // Tile (m, n) of a matrix: of its rows and columns (load), of C's p and q (products); mat = -1: none.
 struct OrthoTile {
-  int32_t mat, m, n, slot;
+  int32_t mat, m, n;
+  int32_t slot;        // update: of x_part;  gram: of `pieces` (-1: a whole sum)
+  int32_t begin, end;  // products: slabs of the sum;  join: pieces
 };
 
 // What the update of a call is made from.
@@ -94,7 +98,9 @@ struct OrthoCoef {
 };
 
 // Products of an iteration.
-enum OrthoProduct { kProductGram = 0, kProductSquare = 1, kProductUpdate = 2 };
+enum OrthoProduct { kProductGram = 0, kProductSquare = 1, kProductUpdate = 2, kProductJoin = 3 };
+// Values of k that a product takes a step.
+inline int ortho_slab(bool full) { return full ? 32 : 64; }
 
 struct OrthoTiles {
   const OrthoTile* tile;  // device
@@ -107,12 +113,14 @@ hipError_t launch_ortho_source(const OrthoCall& call, const OrthoMat* mats, cons
 // X^T of the update over its norm.
 hipError_t launch_ortho_load(bool full, const OrthoCall& call, const OrthoMat* mats, const OrthoTile* tiles, int count,
                              hipStream_t stream);
-// One product of an iteration; `side`: of its tiles, `from`: the X^T buffer read, `last`: O to `u` instead of X^T.
+// One product of an iteration, or the join of the gram product's pieces; `side`: of its tiles, `from`: the X^T buffer read, `last`: O to `u` instead of X^T.
 hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const OrthoMat* mats, const OrthoTiles& tiles,
-                                const OrthoCoef& coef, int from, bool first, bool last, float* u, hipStream_t stream);
-// The whole call but the outer step's source pass, for small matrices only, one per block.
-hipError_t launch_ortho_small(bool full, const OrthoCall& call, const OrthoMat* mats, int count, const OrthoCoef* coef,
-                              int steps, hipStream_t stream);
+                                const OrthoCoef& coef, int from, bool first, bool last, float* u, float* pieces,
+                                hipStream_t stream);
+// The whole call but the outer step's source pass, for small matrices only, one
+// per block; `widest`: the largest r.
+hipError_t launch_ortho_small(bool full, const OrthoCall& call, const OrthoMat* mats, int count, int widest,
+                              const OrthoCoef* coef, int steps, hipStream_t stream);
 // The call's outputs from O.
 hipError_t launch_ortho_apply(const OrthoCall& call, const OrthoMat* mats, const OrthoChunk* chunks, int count,
                               hipStream_t stream);

@@ -26,118 +26,12 @@
 // Error of O against 64 bits: 1e-4 to 1e-3 with FAST over Gaussian, low-rank
 // and power-law spectra (1e-3 to 4e-2 if X itself were rounded to fp16, 1e-2
 // to 9e-2 in bf16), and that of a 32-bit iteration with FULL.
-#include "edit_ortho_internal.h"
+#include "edit_ortho_device.h"
 
 namespace edit {
 namespace {
 
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef float float2_t __attribute__((ext_vector_type(2)));
-
-// ------------------------------------------------------- elements of a unit
-
-constexpr int kVec = 8;  // elements per thread and step of the streaming passes
-
-__device__ __forceinline__ float widen_bf16(uint32_t h) { return __uint_as_float(h << 16); }
-
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  const float2_t f = {a, b};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));  // RNE
-}
-
-template <bool BF16>
-__device__ __forceinline__ float load_one(const void* p, int64_t i) {
-  if constexpr (BF16)
-    return widen_bf16(static_cast<const uint16_t*>(p)[i]);
-  else
-    return static_cast<const float*>(p)[i];
-}
-
-template <bool BF16>
-__device__ __forceinline__ void store_one(void* p, int64_t i, float x) {
-  if constexpr (BF16)
-    static_cast<uint16_t*>(p)[i] = static_cast<uint16_t>(pack_bf16(x, 0.f));
-  else
-    static_cast<float*>(p)[i] = x;
-}
-
-// Elements i .. i+7 (i a multiple of 8, the unit 16-byte aligned) of which
-// [lo, hi) are in range.
-template <bool BF16>
-__device__ __forceinline__ void load_vec(const void* p, int64_t i, int lo, int hi, float (&x)[kVec]) {
-  if (lo == 0 && hi == kVec) {
-    if constexpr (BF16) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p) + i);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) x[e] = __uint_as_float((e & 1) ? (w[e >> 1] & 0xffff0000u) : (w[e >> 1] << 16));
-    } else {
-      const f32x4* q = reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
-      const f32x4 a = q[0], b = q[1];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = a[e], x[e + 4] = b[e];
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) x[e] = e >= lo && e < hi ? load_one<BF16>(p, i + e) : 0.f;
-  }
-}
-
-template <bool BF16>
-__device__ __forceinline__ void store_vec(void* p, int64_t i, int lo, int hi, const float (&x)[kVec]) {
-  if (lo == 0 && hi == kVec) {
-    if constexpr (BF16) {
-      u32x4 w;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
-      *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p) + i) = w;
-    } else {
-      f32x4* q = reinterpret_cast<f32x4*>(static_cast<float*>(p) + i);
-      q[0] = f32x4{x[0], x[1], x[2], x[3]};
-      q[1] = f32x4{x[4], x[5], x[6], x[7]};
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < kVec; ++e)
-      if (e >= lo && e < hi) store_one<BF16>(p, i + e, x[e]);
-  }
-}
-
-// Sum over a block in a fixed order; every thread calls it and gets the sum.
-template <int kThreads>
-__device__ __forceinline__ double block_sum(double x) {
-  __shared__ double red[kThreads / 64];
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-  __syncthreads();
-  double s = red[0];
-#pragma unroll
-  for (int w = 1; w < kThreads / 64; ++w) s += red[w];
-  return s;
-}
-
 // ------------------------------------------------------------- source pass
-
-struct RepPtrs {
-  void* p[EDIT_MAX_K];
-};
-
-struct OrthoArgs {
-  const void* x;
-  void* out;
-  float* momentum;
-  float* theta;
-  float* u;
-  const UnitRecord* rec;
-  int32_t workers;
-  int32_t nesterov;
-  double mu, keep, lr;
-};
 
 // One chunk per block: the call's update u, its sum of squares, and what the
 // call stores on the way (the momentum; the outer step's u, and the whole
@@ -222,11 +116,6 @@ __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_source_kernel(Ortho
 }
 
 // --------------------------------------------------------------- load pass
-
-__device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
-  hi = static_cast<_Float16>(v);
-  lo = static_cast<_Float16>(v - static_cast<float>(hi));
-}
 
 // How the halves of a matrix lie in memory.  The 128 bytes of a cache line are
 // what one row of a slab takes, so that a load asks the L2 for whole lines:
@@ -325,6 +214,7 @@ __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_load_kernel(OrthoAr
 struct ProductArgs {
   double a, b, c;
   int32_t from, first, last;
+  float* pieces;  // unfinished sums of the gram product
 };
 
 // LDS holds two slabs of both operands: 64 values of k (FAST), or 32 with both
@@ -394,8 +284,6 @@ __device__ __forceinline__ void tile_offsets(uint32_t (&off)[LOADS], int side0, 
     off[i] = (static_cast<uint32_t>(g) * static_cast<uint32_t>(pitch) + static_cast<uint32_t>(col)) * 2u;
   }
 }
-
-typedef __fp16 fp16x4 __attribute__((__vector_size__(8)));
 
 // A lane's eight values of its row of a slab's operand: of FAST's k = 32 part +
 // 8 (lane / 16) .., of FULL's k = 8 (lane / 16) .. and half `part`.
@@ -474,8 +362,79 @@ __device__ __forceinline__ void store_split(_Float16* hi, _Float16* lo, int64_t 
     *reinterpret_cast<u32x2*>(lo + at) =
         u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x07060302), __builtin_amdgcn_perm(v[3], v[2], 0x07060302)};
 }
-__device__ __forceinline__ float join(const half4& hi, const half4& lo, int e) {
-  return static_cast<float>(hi[e]) + static_cast<float>(lo[e]);
+// s of an iteration: the mean of A's diagonal, ||X||^2 / r (1 / r at first);
+// kept for the products that follow.
+template <int kThreads>
+__device__ __forceinline__ double shift_of(const OrthoMat& mt, const OrthoTile& t, bool first) {
+  double s = 1.0;
+  if (!first) {
+    s = 0.0;
+    for (int i = threadIdx.x; i < mt.x_tiles; i += kThreads) s += as_global(mt.x_part)[i];
+    s = block_sum<kThreads>(s);
+  }
+  s /= mt.r;
+  if (t.m == 0 && t.n == 0 && threadIdx.x == 0) *as_global(mt.shift) = s;
+  return s;
+}
+
+// The results of a symmetric product, from the sums of one wave.
+template <int PRODUCT, bool FULL, int BP, int BQ, int FP, int FQ>
+__device__ __forceinline__ void store_symmetric(const f32x4 (&acc)[FP][FQ], const OrthoMat& mt, const OrthoTile& t,
+                                                const ProductArgs& args, double s, int wp, int wq, int lane) {
+  using L = Layout<FULL>;
+  const int r = mt.r, ld = mt.ldr;
+  const double keep = args.a + args.b * s + args.c * s * s;
+  // Lane l holds C[p .. p+3][q] of each 16 x 16 block, p = 4 (l / 16), q = l mod 16.
+  const int p0 = t.m * BP + wp + 4 * (lane >> 4), q0 = t.n * BQ + wq + (lane & 15);
+  const int quad = lane & 3;
+  const _Float16* r_hi = as_global(mt.g[0]);
+  const _Float16* r_lo = L::low(r_hi, as_global<const _Float16>(mt.g[1]));
+  _Float16* dst_hi = as_global(PRODUCT == kProductGram ? mt.g[0] : mt.q[0]);
+  _Float16* dst_lo = L::low(dst_hi, as_global(mt.g[1]));  // the square product's only with FULL
+  // F's low half goes into products only, R's into F as well
+  constexpr bool kStoreLow = PRODUCT == kProductGram || FULL;
+  // with FAST the update product adds the diagonal term itself, unrounded
+  const float diag = PRODUCT == kProductGram ? static_cast<float>(-s * kScaleA)
+                     : FULL                  ? static_cast<float>(keep * kScaleA)
+                                             : 0.f;
+  const float lin = static_cast<float>(args.b + 2.0 * args.c * s);
+  const float quadratic = static_cast<float>(args.c) / kScaleA;
+  half4 rh[2][FQ], rl[2][FQ];  // R, a row of blocks ahead
+  auto read_r = [&](int i) {
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {  // R is symmetric
+      const int64_t from = L::at(min(q0 + j * 16, r - 1), min(p0 + i * 16, ld - 4), ld);
+      rh[i & 1][j] = *reinterpret_cast<const half4*>(r_hi + from);
+      rl[i & 1][j] = *reinterpret_cast<const half4*>(r_lo + from);
+    }
+  };
+  if constexpr (PRODUCT == kProductSquare) read_r(0);
+#pragma unroll
+  for (int i = 0; i < FP; ++i) {
+    const int pp = p0 + i * 16;
+    if constexpr (PRODUCT == kProductSquare)
+      if (i + 1 < FP) read_r(i + 1);
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {
+      const int qq = q0 + j * 16;
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float v;
+        if constexpr (PRODUCT == kProductGram)
+          v = acc[i][j][e] * (kScaleA / (kScaleX * kScaleX));
+        else
+          v = lin * join(rh[i & 1][j], rl[i & 1][j], e) + quadratic * acc[i][j][e];
+        if (pp + e == qq) v += diag;
+        w[e] = pack_split(pp + e < r && qq < r ? v : 0.f);
+      }
+      if (qq < r && pp < r) store_split<kStoreLow>(dst_hi, dst_lo, L::at(qq, pp, ld), w);
+      if (t.m != t.n) {
+        quad_transpose(w, lane);  // C[p + l mod 4][q - l mod 4 .. + 3]
+        if (pp + quad < r && qq - quad < r) store_split<kStoreLow>(dst_hi, dst_lo, L::at(pp + quad, qq - quad, ld), w);
+      }
+    }
+  }
 }
 
 // One tile of a product per block.  While one slab is multiplied, the loads of
@@ -510,7 +469,8 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
   const uint32_t lds0 = static_cast<uint32_t>(
       reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)(smem)));  // byte offset in LDS
   const int64_t step = PRODUCT == kProductGram ? S::kSlabK * L::pitch(ld) : 64;
-  const int slabs = (PRODUCT == kProductGram ? (c + kOrthoPad - 1) / kOrthoPad * kOrthoPad : ld) / S::kSlabK;
+  const int slabs = t.end - t.begin;
+  p += t.begin * step, q += t.begin * step;
   // Slab n, or of its loads those with number part mod parts.
   auto fetch = [&](int n, int part = 0, int parts = 1) {
     const uint32_t at = lds0 + (n & 1) * S::kSlab;
@@ -525,21 +485,8 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
   };
   fetch(0);
 
-  // s of this iteration: the mean of A's diagonal, ||X||^2 / r (1 / r at first)
-  double s;
-  if constexpr (PRODUCT == kProductGram) {
-    if (args.first) {
-      s = 1.0;
-    } else {
-      s = 0.0;
-      for (int i = threadIdx.x; i < mt.x_tiles; i += S::kThreads) s += as_global(mt.x_part)[i];
-      s = block_sum<S::kThreads>(s);
-    }
-    s /= r;
-    if (t.m == 0 && t.n == 0 && threadIdx.x == 0) *as_global(mt.shift) = s;
-  } else {
-    s = *as_global(mt.shift);
-  }
+  const bool piece = PRODUCT == kProductGram && t.slot >= 0;  // of a sum that the join pass finishes
+  const double s = PRODUCT != kProductGram ? *as_global(mt.shift) : piece ? 0.0 : shift_of<S::kThreads>(mt, t, args.first);
   const double keep = args.a + args.b * s + args.c * s * s;
 
   constexpr int FP = WP / 16, FQ = WQ / 16;
@@ -670,57 +617,15 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
 
   // Values behind the matrix become the zeros that its padding holds anyway.
   if constexpr (PRODUCT != kProductUpdate) {
-    // Lane l holds C[p .. p+3][q] of each 16 x 16 block, p = 4 (l / 16), q = l mod 16.
-    const int p0 = t.m * BP + wp + 4 * (lane >> 4);
-    const int quad = lane & 3;
-    const _Float16* r_hi = as_global(mt.g[0]);
-    const _Float16* r_lo = L::low(r_hi, as_global<const _Float16>(mt.g[1]));
-    _Float16* dst_hi = as_global(PRODUCT == kProductGram ? mt.g[0] : mt.q[0]);
-    _Float16* dst_lo = L::low(dst_hi, as_global(mt.g[1]));  // the square product's only with FULL
-    // F's low half goes into products only, R's into F as well
-    constexpr bool kStoreLow = PRODUCT == kProductGram || FULL;
-    // with FAST the update product adds the diagonal term itself, unrounded
-    const float diag = PRODUCT == kProductGram ? static_cast<float>(-s * kScaleA)
-                       : FULL                  ? static_cast<float>(keep * kScaleA)
-                                               : 0.f;
-    const float lin = static_cast<float>(args.b + 2.0 * args.c * s);
-    const float quadratic = static_cast<float>(args.c) / kScaleA;
-    half4 rh[2][FQ], rl[2][FQ];  // R, a row of blocks ahead
-    auto read_r = [&](int i) {
+    if (piece) {
+      f32x4* to = reinterpret_cast<f32x4*>(as_global(args.pieces)) + static_cast<int64_t>(t.slot) * (BP * BQ / 4);
 #pragma unroll
-      for (int j = 0; j < FQ; ++j) {  // R is symmetric
-        const int64_t from = L::at(min(q0 + j * 16, r - 1), min(p0 + i * 16, ld - 4), ld);
-        rh[i & 1][j] = *reinterpret_cast<const half4*>(r_hi + from);
-        rl[i & 1][j] = *reinterpret_cast<const half4*>(r_lo + from);
-      }
-    };
-    if constexpr (PRODUCT == kProductSquare) read_r(0);
+      for (int i = 0; i < FP; ++i)
 #pragma unroll
-    for (int i = 0; i < FP; ++i) {
-      const int pp = p0 + i * 16;
-      if constexpr (PRODUCT == kProductSquare)
-        if (i + 1 < FP) read_r(i + 1);
-#pragma unroll
-      for (int j = 0; j < FQ; ++j) {
-        const int qq = q0 + j * 16;
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float v;
-          if constexpr (PRODUCT == kProductGram)
-            v = acc[i][j][e] * (kScaleA / (kScaleX * kScaleX));
-          else
-            v = lin * join(rh[i & 1][j], rl[i & 1][j], e) + quadratic * acc[i][j][e];
-          if (pp + e == qq) v += diag;
-          w[e] = pack_split(pp + e < r && qq < r ? v : 0.f);
-        }
-        if (qq < r && pp < r) store_split<kStoreLow>(dst_hi, dst_lo, L::at(qq, pp, ld), w);
-        if (t.m != t.n) {
-          quad_transpose(w, lane);  // C[p + l mod 4][q - l mod 4 .. + 3]
-          if (pp + quad < r && qq - quad < r) store_split<kStoreLow>(dst_hi, dst_lo, L::at(pp + quad, qq - quad, ld), w);
-        }
-      }
+        for (int j = 0; j < FQ; ++j) to[(i * FQ + j) * S::kThreads + threadIdx.x] = acc[i][j];
+      return;
     }
+    store_symmetric<PRODUCT, FULL, BP, BQ, FP, FQ>(acc, mt, t, args, s, wp, wq, lane);
   } else {
     float sq = 0.f;
 #pragma unroll
@@ -768,6 +673,34 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
   }
 }
 
+// The gram product's tiles whose sums were cut into pieces (few tiles with
+// long sums): the pieces added up in order, then R as from a whole sum.
+template <bool FULL, int BP, int BQ, int WP, int WQ>
+__global__ __launch_bounds__((ProductShape<FULL, BP, BQ, WP, WQ>::kThreads)) void ortho_join_kernel(
+    const OrthoMat* __restrict__ mats, const OrthoTile* __restrict__ tiles, ProductArgs args) {
+  constexpr int kThreads = ProductShape<FULL, BP, BQ, WP, WQ>::kThreads;
+  const OrthoTile t = tiles[blockIdx.x];
+  if (t.mat < 0) return;
+  const OrthoMat mt = mats[t.mat];
+  constexpr int FP = WP / 16, FQ = WQ / 16;
+  f32x4 acc[FP][FQ];
+#pragma unroll
+  for (int i = 0; i < FP; ++i)
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const f32x4* from = reinterpret_cast<const f32x4*>(as_global(args.pieces));
+  for (int k = t.begin; k < t.end; ++k)
+#pragma unroll
+    for (int i = 0; i < FP; ++i)
+#pragma unroll
+      for (int j = 0; j < FQ; ++j)
+        acc[i][j] += from[static_cast<int64_t>(k) * (BP * BQ / 4) + (i * FQ + j) * kThreads + threadIdx.x];
+  const double s = shift_of<kThreads>(mt, t, args.first);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  store_symmetric<kProductGram, FULL, BP, BQ, FP, FQ>(acc, mt, t, args, s, (wave % (BP / WP)) * WP,
+                                                      (wave / (BP / WP)) * WQ, lane);
+}
+
 // -------------------------------------------------------------- apply pass
 
 // One chunk of a matrix per block: the call's outputs from O, which is fp32 in
@@ -810,271 +743,6 @@ __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_apply_kernel(OrthoA
   }
 }
 
-// ----------------------------------------------------------- small matrices
-
-// The whole call for one matrix per block, where X and A fit into LDS
-// (ortho_is_small): no launch between the products, whose latency bounds
-// matrices of this size.  LDS holds X^T [c][r] and R, then F, [r][r], high and
-// low halves apart, in rows of r rounded up to 32 values and eight more (rows
-// then begin in different banks); what pads them is zero.  Wave w takes the
-// 16 rows 16 w .. of the symmetric products, all columns, so that R and F stay
-// in its registers as well, and rows 16 w + 128 t of X^T.
-struct SmallCoef {
-  double v[EDIT_ORTHO_MAX_STEPS][3];
-};
-
-// O of one element into the call's outputs.
-template <int SOURCE, bool BF16>
-__device__ __forceinline__ void apply_one(const OrthoArgs& a, const RepPtrs& reps, double step, bool rollback, int64_t i,
-                                          float o) {
-  if constexpr (SOURCE == kSourcePlain) {
-    store_one<BF16>(a.out, i, o);
-  } else if constexpr (SOURCE == kSourceLocal) {
-    const double p = load_one<BF16>(a.out, i);
-    store_one<BF16>(a.out, i, static_cast<float>(fma(a.keep, p, -step * static_cast<double>(o))));
-  } else {
-    float th = a.theta[i];
-    if (!rollback) {
-      th = static_cast<float>(fma(-step, static_cast<double>(o), static_cast<double>(th)));
-      a.theta[i] = th;
-    }
-    for (int j = 0; j < a.workers; ++j) store_one<BF16>(reps.p[j], i, th);
-  }
-}
-
-template <int SOURCE, bool BF16, bool FULL>
-__global__ __launch_bounds__(kOrthoSmallThreads) void ortho_small_kernel(OrthoArgs a, RepPtrs reps,
-                                                                        const OrthoMat* __restrict__ mats,
-                                                                        SmallCoef coef, int steps) {
-  constexpr int kThreads = kOrthoSmallThreads;
-  constexpr int kBlocks = kOrthoSmallSide / 16;                // of a row of A
-  constexpr int kRows = kOrthoSmallRows / 16 / (kThreads / 64);  // blocks of X^T's rows per wave
-  __shared__ __align__(256) char smem[kOrthoSmallLds];
-  const OrthoMat mt = mats[blockIdx.x];
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = mt.r, c = mt.c, rp = (r + 31) & ~31, cp = (c + 31) & ~31;
-  const int pitch = rp + 8;
-  _Float16* x_hi = reinterpret_cast<_Float16*>(smem);
-  _Float16* x_lo = x_hi + cp * pitch;
-  _Float16* g_hi = x_lo + cp * pitch;
-  _Float16* g_lo = g_hi + rp * pitch;
-  const int64_t n = static_cast<int64_t>(r) * c;
-
-  // u, its norm, and X^T = u / ||u||
-  auto update_of = [&](int64_t i) -> double {
-    if constexpr (SOURCE == kSourcePlain) return load_one<BF16>(a.x, i);
-    if constexpr (SOURCE == kSourceOuter) return a.u[i];
-    const double m = a.momentum[i];
-    return a.nesterov ? fma(a.mu, m, static_cast<double>(load_one<BF16>(a.x, i))) : m;
-  };
-  for (int i = threadIdx.x; i < 2 * (cp + rp) * pitch / 8; i += kThreads)
-    reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
-  double sum = 0.0;
-  for (int64_t e = threadIdx.x; e < n; e += kThreads) {
-    const int64_t i = mt.offset + e;
-    if constexpr (SOURCE == kSourceLocal)
-      a.momentum[i] = static_cast<float>(fma(a.mu, static_cast<double>(a.momentum[i]), static_cast<double>(load_one<BF16>(a.x, i))));
-    const double u = update_of(i);
-    sum = fma(u, u, sum);
-  }
-  sum = block_sum<kThreads>(sum);
-  const double inv = sum > 0.0 ? kScaleX / sqrt(sum) : (sum == 0.0 ? 0.0 : sum);
-  for (int e = threadIdx.x; e < n; e += kThreads) {
-    const int row = e / mt.cols, col = e - row * mt.cols;
-    _Float16 hi, lo;
-    split(static_cast<float>(update_of(mt.offset + e) * inv), hi, lo);
-    const int at = mt.tall ? row * pitch + col : col * pitch + row;
-    x_hi[at] = hi, x_lo[at] = lo;
-  }
-  __syncthreads();
-
-  const int blocks = rp / 16;
-  const int l16 = lane & 15, l4 = lane >> 4;
-  // eight values along k of row `row0` + l16
-  auto along = [&](const _Float16* m, int row0, int k) {
-    return *reinterpret_cast<const half8*>(m + (row0 + l16) * pitch + k + 8 * l4);
-  };
-  // eight rows from `k` + 8 l4 on of column `col0` + l16
-  auto across = [&](const _Float16* m, int col0, int k) {
-    half8 out;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const _Float16* at = m + (k + 8 * l4 + 4 * h + (l16 >> 2)) * pitch + col0 + 4 * (l16 & 3);
-      const half4 v = __builtin_bit_cast(
-          half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) fp16x4*)(at)));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) out[4 * h + e] = v[e];
-    }
-    return out;
-  };
-  auto mul = [&](const half8& x, const half8& y, f32x4& to) {
-    to = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, to, 0, 0, 0);
-  };
-  // four neighbours of row `row`, high and low halves
-  auto put = [&](_Float16* hi, _Float16* lo, int row, int col, const f32x4& v) {
-    half4 h, l;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      _Float16 x, y;
-      split(v[e], x, y);
-      h[e] = x, l[e] = y;
-    }
-    *reinterpret_cast<half4*>(hi + row * pitch + col) = h;
-    *reinterpret_cast<half4*>(lo + row * pitch + col) = l;
-  };
-
-  float* o = reinterpret_cast<float*>(smem);  // [c][pitch], over both halves of X^T
-  double s = 1.0 / r;
-  for (int k = 0; k < steps; ++k) {
-    const double ca = coef.v[k][0], cb = coef.v[k][1], cc = coef.v[k][2];
-    const double keep = ca + cb * s + cc * s * s;
-    const int p0 = 16 * wave;
-    f32x4 g[kBlocks];  // lane l: [p0 + l16][16 j + 4 l4 ..], R and then F
-#pragma unroll
-    for (int j = 0; j < kBlocks; ++j) g[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (wave < blocks) {
-      for (int t = 0; t < cp; t += 32) {
-        const half8 q = across(x_hi, p0, t);
-        half8 ql;
-        if constexpr (FULL) ql = across(x_lo, p0, t);
-#pragma unroll
-        for (int j = 0; j < kBlocks; ++j) {
-          if (j >= blocks) continue;
-          const half8 p = across(x_hi, 16 * j, t);
-          mul(p, q, g[j]);
-          if constexpr (FULL) {
-            mul(p, ql, g[j]);
-            mul(across(x_lo, 16 * j, t), q, g[j]);
-          }
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < kBlocks; ++j) {
-        if (j >= blocks) continue;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int p = 16 * j + 4 * l4 + e;
-          g[j][e] *= kScaleA / (kScaleX * kScaleX);
-          // behind the matrix R stays zero, and F with it
-          if (p == p0 + l16 && p < r) g[j][e] -= static_cast<float>(s * kScaleA);
-        }
-        put(g_hi, g_lo, p0 + l16, 16 * j + 4 * l4, g[j]);
-      }
-    }
-    __syncthreads();
-    f32x4 f[kBlocks];
-#pragma unroll
-    for (int j = 0; j < kBlocks; ++j) f[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (wave < blocks)
-      for (int t = 0; t < rp; t += 32) {
-        const half8 q = along(g_hi, p0, t);
-        half8 ql;
-        if constexpr (FULL) ql = along(g_lo, p0, t);
-#pragma unroll
-        for (int j = 0; j < kBlocks; ++j) {
-          if (j >= blocks) continue;
-          const half8 p = along(g_hi, 16 * j, t);
-          mul(p, q, f[j]);
-          if constexpr (FULL) {
-            mul(p, ql, f[j]);
-            mul(along(g_lo, 16 * j, t), q, f[j]);
-          }
-        }
-      }
-    __syncthreads();
-    if (wave < blocks) {
-      const float lin = static_cast<float>(cb + 2.0 * cc * s), quadratic = static_cast<float>(cc) / kScaleA;
-#pragma unroll
-      for (int j = 0; j < kBlocks; ++j) {
-        if (j >= blocks) continue;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          f[j][e] = lin * g[j][e] + quadratic * f[j][e];
-          if (FULL && 16 * j + 4 * l4 + e == p0 + l16) f[j][e] += static_cast<float>(keep * kScaleA);
-        }
-        put(g_hi, g_lo, p0 + l16, 16 * j + 4 * l4, f[j]);
-      }
-    }
-    __syncthreads();
-    f32x4 x[kRows][kBlocks];  // lane l: X^T[16 (wave + 8 t) + l16][16 j + 4 l4 ..]
-    const float keep_x = static_cast<float>(keep) * kScaleA;
-#pragma unroll
-    for (int t = 0; t < kRows; ++t) {
-      const int q0 = 16 * (wave + t * (kThreads / 64));
-      if (q0 >= cp) continue;
-#pragma unroll
-      for (int j = 0; j < kBlocks; ++j) {
-        x[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (j >= blocks || FULL) continue;
-        // with FAST the term (a + bs + cs^2) X is taken from both halves as they are
-        const int at = (q0 + l16) * pitch + 16 * j + 4 * l4;
-        const half4 h = *reinterpret_cast<const half4*>(x_hi + at), l = *reinterpret_cast<const half4*>(x_lo + at);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[t][j][e] = keep_x * join(h, l, e);
-      }
-      for (int kk = 0; kk < rp; kk += 32) {
-        const half8 q = along(x_hi, q0, kk);
-        half8 ql;
-        if constexpr (FULL) ql = along(x_lo, q0, kk);
-#pragma unroll
-        for (int j = 0; j < kBlocks; ++j) {
-          if (j >= blocks) continue;
-          const half8 p = along(g_hi, 16 * j, kk);
-          mul(p, q, x[t][j]);
-          if constexpr (FULL) {
-            mul(p, ql, x[t][j]);
-            mul(along(g_lo, 16 * j, kk), q, x[t][j]);
-          }
-        }
-      }
-    }
-    __syncthreads();
-    float sq = 0.f;
-#pragma unroll
-    for (int t = 0; t < kRows; ++t) {
-      const int q0 = 16 * (wave + t * (kThreads / 64));
-      if (q0 >= cp) continue;
-#pragma unroll
-      for (int j = 0; j < kBlocks; ++j) {
-        if (j >= blocks) continue;
-        const int q = q0 + l16, p = 16 * j + 4 * l4;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[t][j][e] *= 1.f / kScaleA;
-          if (!(p + e < r && q < c)) x[t][j][e] = 0.f;  // a NaN in the matrix would reach the padding
-          sq += x[t][j][e] * x[t][j][e];
-        }
-        if (k + 1 < steps)
-          put(x_hi, x_lo, q, p, x[t][j]);
-        else  // O, where X^T was
-          *reinterpret_cast<f32x4*>(o + q * pitch + p) = x[t][j];
-      }
-    }
-    if (k + 1 < steps)
-      s = block_sum<kThreads>(static_cast<double>(sq) / (static_cast<double>(kScaleX) * kScaleX)) / r;
-  }
-  __syncthreads();
-  bool rollback = false;
-  if constexpr (SOURCE == kSourceOuter) rollback = a.rec->rollback;
-  const double step = a.lr * mt.scale;
-  for (int e = threadIdx.x; e < n; e += kThreads) {
-    const int row = e / mt.cols, col = e - row * mt.cols;
-    apply_one<SOURCE, BF16>(a, reps, step, rollback, mt.offset + e,
-                            o[mt.tall ? row * pitch + col : col * pitch + row] * (1.f / kScaleX));
-  }
-}
-
-OrthoArgs args_of(const OrthoCall& c) {
-  return {c.x, c.out, c.momentum, c.theta, c.u, c.rec, c.workers, c.nesterov, c.mu, c.keep, c.lr};
-}
-
-RepPtrs reps_of(const OrthoCall& c) {
-  RepPtrs r = {};
-  for (int j = 0; j < c.workers; ++j) r.p[j] = c.reps[j];
-  return r;
-}
-
 template <int PRODUCT, bool FULL, int BP, int BQ, int WP, int WQ>
 hipError_t launch_product(const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args, float* out,
                           hipStream_t stream) {
@@ -1085,6 +753,13 @@ hipError_t launch_product(const OrthoMat* mats, const OrthoTiles& tiles, const P
   else
     ortho_product_kernel<PRODUCT, FULL, false, BP, BQ, WP, WQ>
         <<<tiles.count, S::kThreads, 0, stream>>>(mats, tiles.tile, args, out);
+  return hipGetLastError();
+}
+
+template <bool FULL, int BP, int BQ, int WP, int WQ>
+hipError_t launch_join(const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args, hipStream_t stream) {
+  ortho_join_kernel<FULL, BP, BQ, WP, WQ>
+      <<<tiles.count, ProductShape<FULL, BP, BQ, WP, WQ>::kThreads, 0, stream>>>(mats, tiles.tile, args);
   return hipGetLastError();
 }
 
@@ -1130,9 +805,10 @@ hipError_t launch_ortho_load(bool full, const OrthoCall& call, const OrthoMat* m
 }
 
 hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const OrthoMat* mats, const OrthoTiles& tiles,
-                                const OrthoCoef& coef, int from, bool first, bool last, float* u, hipStream_t stream) {
+                                const OrthoCoef& coef, int from, bool first, bool last, float* u, float* pieces,
+                                hipStream_t stream) {
   if (tiles.count == 0) return hipSuccess;
-  const ProductArgs args = {coef.a, coef.b, coef.c, from, first, last};
+  const ProductArgs args = {coef.a, coef.b, coef.c, from, first, last, pieces};
 #define EDIT_PRODUCT(P)                                                        \
   (full ? launch_product_of<P, true>(side, mats, tiles, args, u, stream) \
         : launch_product_of<P, false>(side, mats, tiles, args, u, stream))
@@ -1140,28 +816,13 @@ hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const
     case kProductGram: return EDIT_PRODUCT(kProductGram);
     case kProductSquare: return EDIT_PRODUCT(kProductSquare);
     case kProductUpdate: return EDIT_PRODUCT(kProductUpdate);
+    case kProductJoin:
+      if (side != 64) return hipErrorInvalidValue;
+      return full ? launch_join<true, 64, 64, 32, 32>(mats, tiles, args, stream)
+                  : launch_join<false, 64, 64, 32, 32>(mats, tiles, args, stream);
   }
 #undef EDIT_PRODUCT
   return hipErrorInvalidValue;
-}
-
-hipError_t launch_ortho_small(bool full, const OrthoCall& call, const OrthoMat* mats, int count, const OrthoCoef* coef,
-                              int steps, hipStream_t stream) {
-  if (count == 0) return hipSuccess;
-  const OrthoArgs a = args_of(call);
-  const RepPtrs r = reps_of(call);
-  SmallCoef sc = {};
-  for (int k = 0; k < steps; ++k) sc.v[k][0] = coef[k].a, sc.v[k][1] = coef[k].b, sc.v[k][2] = coef[k].c;
-#define EDIT_SMALL(S, B)                                                                                  \
-  (full ? ortho_small_kernel<S, B, true><<<count, kOrthoSmallThreads, 0, stream>>>(a, r, mats, sc, steps) \
-        : ortho_small_kernel<S, B, false><<<count, kOrthoSmallThreads, 0, stream>>>(a, r, mats, sc, steps))
-  switch (call.source) {
-    case kSourcePlain: call.bf16 ? EDIT_SMALL(kSourcePlain, true) : EDIT_SMALL(kSourcePlain, false); break;
-    case kSourceLocal: call.bf16 ? EDIT_SMALL(kSourceLocal, true) : EDIT_SMALL(kSourceLocal, false); break;
-    case kSourceOuter: call.bf16 ? EDIT_SMALL(kSourceOuter, true) : EDIT_SMALL(kSourceOuter, false); break;
-  }
-#undef EDIT_SMALL
-  return hipGetLastError();
 }
 
 hipError_t launch_ortho_apply(const OrthoCall& call, const OrthoMat* mats, const OrthoChunk* chunks, int count,

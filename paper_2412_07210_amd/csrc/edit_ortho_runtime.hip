@@ -46,6 +46,9 @@ constexpr int kXcds = 8;                          // workgroups go to the XCDs i
 // 33, 480: 35 and 39; update product of 64 tiles 14 and 8, 192: 18 and 15, 256:
 // 19 and 20, 512: 29 and 35.
 constexpr int kLargeSide = 128, kSmallSide = 64;
+// A gram tile whose sum is kCutFrom times as long as a CU's share of all of
+// them (and kPieceSlabs slabs at least) is cut into pieces of about that.
+constexpr int64_t kPieceSlabs = 8, kCutFrom = 2;
 int symmetric_side(int64_t large_tiles, int num_cu) { return 2 * large_tiles <= 3 * num_cu ? kSmallSide : kLargeSide; }
 int update_side(int64_t large_tiles, int num_cu) { return large_tiles < num_cu ? kSmallSide : kLargeSide; }
 // Side, in tiles, of the groups that tiles are taken in.  Products of a 1B
@@ -58,7 +61,8 @@ struct Tables {
   std::vector<OrthoMat> mats;
   std::vector<OrthoChunk> chunks;
   int matrix_chunks = 0;  // the first ones belong to matrices
-  std::vector<OrthoTile> load, gram, update;
+  std::vector<OrthoTile> load, gram, join, square, update;
+  int pieces = 0;
   int gram_side = kLargeSide, update_side = kLargeSide;
   bool small = false;  // one block takes each matrix whole
 };
@@ -76,10 +80,11 @@ struct edit_ortho {
   int matrix_chunks = 0, all_chunks = 0;
   OrthoTile* load = nullptr;
   int load_tiles = 0;
-  OrthoTiles gram{}, update{};
+  OrthoTiles gram{}, join{}, square{}, update{};
+  float* pieces = nullptr;
   int gram_side = 0, update_side = 0;
   bool small = false;
-  int matrices = 0;
+  int matrices = 0, widest = 0;  // widest: the largest r
   float* u = nullptr;
 };
 
@@ -158,7 +163,7 @@ std::vector<OrthoTile> spread(const std::vector<std::vector<OrthoTile>>& of_matr
   for (const auto& l : list) longest = std::max(longest, l.size());
   std::vector<OrthoTile> out;
   for (size_t i = 0; i < longest; ++i)
-    for (const auto& l : list) out.push_back(i < l.size() ? l[i] : OrthoTile{-1, 0, 0, 0});
+    for (const auto& l : list) out.push_back(i < l.size() ? l[i] : OrthoTile{-1, 0, 0, 0, 0, 0});
   while (!out.empty() && out.back().mat < 0) out.pop_back();
   return out;
 }
@@ -179,7 +184,7 @@ void add_chunks(std::vector<OrthoChunk>& out, int64_t begin, int64_t end, int ma
 Tables make_tables(const edit_ortho_config_t* cfg, int num_cu) {
   Tables t;
   std::vector<std::pair<int64_t, int64_t>> used;
-  std::vector<std::vector<OrthoTile>> gram, update;
+  std::vector<std::vector<OrthoTile>> gram, square, update;
   for (int i = 0; i < cfg->num_matrices; ++i) {
     const edit_ortho_matrix_t& in = cfg->matrices[i];
     if (in.rows == 0 || in.cols == 0) continue;
@@ -195,7 +200,7 @@ Tables make_tables(const edit_ortho_config_t* cfg, int num_cu) {
     used.push_back({in.offset, end});
     add_chunks(t.chunks, in.offset, end, k, kOrthoMaxChunks, &m.chunks);
     for (int32_t a = 0; a < oceil_div(in.rows, kOrthoLoadTile); ++a)
-      for (int32_t b = 0; b < oceil_div(in.cols, kOrthoLoadTile); ++b) t.load.push_back({k, a, b, 0});
+      for (int32_t b = 0; b < oceil_div(in.cols, kOrthoLoadTile); ++b) t.load.push_back({k, a, b, 0, 0, 0});
     t.mats.push_back(m);
   }
   int64_t symmetric = 0, whole = 0;  // tiles at the large side
@@ -208,23 +213,42 @@ Tables make_tables(const edit_ortho_config_t* cfg, int num_cu) {
                                            [](const OrthoMat& m) { return ortho_is_small(m.r, m.c); });
   t.gram_side = symmetric_side(symmetric, num_cu);
   t.update_side = update_side(whole, num_cu);
+  const int slab = ortho_slab(cfg->precision == EDIT_ORTHO_FULL);
+  int64_t work = 0;  // slabs of all symmetric tiles
+  for (const OrthoMat& m : t.mats) {
+    const int64_t ts = oceil_div(m.r, t.gram_side);
+    work += ts * (ts + 1) / 2 * oceil_div(m.c, slab);
+  }
+  const int64_t piece = std::max<int64_t>(kPieceSlabs, oceil_div(work, 2 * num_cu));
   for (size_t k = 0; k < t.mats.size(); ++k) {
     OrthoMat& m = t.mats[k];
     const int32_t id = static_cast<int32_t>(k);
     // in groups of kGroup x kGroup tiles, which share operands while they run
     const int32_t ts = static_cast<int32_t>(oceil_div(m.r, t.gram_side));
+    const int32_t slabs_r = m.ldr / slab, slabs_c = static_cast<int32_t>(oround_up(m.c, kOrthoPad)) / slab;
+    const int32_t pieces = t.gram_side == kSmallSide && slabs_c >= kCutFrom * piece ? static_cast<int32_t>(oceil_div(slabs_c, piece)) : 1;
     gram.emplace_back();
+    square.emplace_back();
     for (int32_t p = 0; p < ts; p += kGroup)
       for (int32_t q = 0; q <= p; q += kGroup)
         for (int32_t a = p; a < std::min(ts, p + kGroup); ++a)
-          for (int32_t b = q; b <= std::min(a, q + kGroup - 1); ++b) gram.back().push_back({id, a, b, 0});
+          for (int32_t b = q; b <= std::min(a, q + kGroup - 1); ++b) {
+            square.back().push_back({id, a, b, -1, 0, slabs_r});
+            if (pieces == 1) {
+              gram.back().push_back({id, a, b, -1, 0, slabs_c});
+              continue;
+            }
+            t.join.push_back({id, a, b, 0, t.pieces, t.pieces + pieces});
+            for (int32_t k = 0; k < pieces; ++k)
+              gram.back().push_back({id, a, b, t.pieces++, slabs_c * k / pieces, slabs_c * (k + 1) / pieces});
+          }
     const int32_t tr = static_cast<int32_t>(oceil_div(m.r, t.update_side));
     const int32_t tc = static_cast<int32_t>(oceil_div(m.c, t.update_side));
     update.emplace_back();
     for (int32_t q = 0; q < tc; q += kGroup)
       for (int32_t p = 0; p < tr; p += kGroup)
         for (int32_t b = q; b < std::min(tc, q + kGroup); ++b)
-          for (int32_t a = p; a < std::min(tr, p + kGroup); ++a) update.back().push_back({id, a, b, m.x_tiles++});
+          for (int32_t a = p; a < std::min(tr, p + kGroup); ++a) update.back().push_back({id, a, b, m.x_tiles++, 0, slabs_r});
   }
   t.matrix_chunks = static_cast<int>(t.chunks.size());
   std::sort(used.begin(), used.end());
@@ -238,6 +262,7 @@ Tables make_tables(const edit_ortho_config_t* cfg, int num_cu) {
   for (size_t i = 0; i < order.size(); ++i) order[i] = static_cast<int>(i);
   std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return t.mats[a].c > t.mats[b].c; });
   t.gram = spread(gram, order);
+  t.square = spread(square, order);
   std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return t.mats[a].r > t.mats[b].r; });
   t.update = spread(update, order);
   return t;
@@ -277,11 +302,17 @@ size_t lay_out(edit_ortho* h, Tables& t, char* base) {
   h->load = c.take<OrthoTile>(t.load.size());
   OrthoTile* gram = c.take<OrthoTile>(t.gram.size());
   OrthoTile* update = c.take<OrthoTile>(t.update.size());
+  OrthoTile* join = c.take<OrthoTile>(t.join.size());
+  OrthoTile* square = c.take<OrthoTile>(t.square.size());
+  h->pieces = c.take<float>(static_cast<size_t>(t.pieces) * kSmallSide * kSmallSide);
+  h->join = {join, static_cast<int32_t>(t.join.size())};
+  h->square = {square, static_cast<int32_t>(t.square.size())};
   h->gram = {gram, static_cast<int32_t>(t.gram.size())};
   h->update = {update, static_cast<int32_t>(t.update.size())};
   h->gram_side = t.gram_side, h->update_side = t.update_side;
   h->small = t.small;
   h->matrices = static_cast<int>(t.mats.size());
+  for (const OrthoMat& m : t.mats) h->widest = std::max(h->widest, m.r);
   h->matrix_chunks = t.matrix_chunks;
   h->all_chunks = static_cast<int>(t.chunks.size());
   h->load_tiles = static_cast<int>(t.load.size());
@@ -321,7 +352,7 @@ edit_status_t enqueue(edit_ortho* h, OrthoCall call, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (h->small) {
     if (call.source == kSourceOuter) e = launch_ortho_source(call, h->mats, h->chunks, h->all_chunks, s);
-    if (e == hipSuccess) e = launch_ortho_small(h->full, call, h->mats, h->matrices, h->coef.data(), steps, s);
+    if (e == hipSuccess) e = launch_ortho_small(h->full, call, h->mats, h->matrices, h->widest, h->coef.data(), steps, s);
     return e == hipSuccess ? EDIT_OK : ofail_hip(e, "small matrices launch");
   }
   e = launch_ortho_source(call, h->mats, h->chunks,
@@ -331,12 +362,15 @@ edit_status_t enqueue(edit_ortho* h, OrthoCall call, hipStream_t s) {
   if ((e = launch_ortho_load(h->full, call, h->mats, h->load, h->load_tiles, s)) != hipSuccess)
     return ofail_hip(e, "load pass launch");
   for (int k = 0; k < steps; ++k) {
-    const bool first = k == 0, last = k == steps - 1;
-    e = launch_ortho_product(kProductGram, h->full, h->gram_side, h->mats, h->gram, h->coef[k], k & 1, first, last, h->u, s);
-    if (e == hipSuccess)
-      e = launch_ortho_product(kProductSquare, h->full, h->gram_side, h->mats, h->gram, h->coef[k], k & 1, first, last, h->u, s);
-    if (e == hipSuccess)
-      e = launch_ortho_product(kProductUpdate, h->full, h->update_side, h->mats, h->update, h->coef[k], k & 1, first, last, h->u, s);
+    auto product = [&](OrthoProduct p, int side, const OrthoTiles& tiles) {
+      if (e == hipSuccess)
+        e = launch_ortho_product(p, h->full, side, h->mats, tiles, h->coef[k], k & 1, k == 0, k == steps - 1, h->u,
+                                 h->pieces, s);
+    };
+    product(kProductGram, h->gram_side, h->gram);
+    product(kProductJoin, h->gram_side, h->join);
+    product(kProductSquare, h->gram_side, h->square);
+    product(kProductUpdate, h->update_side, h->update);
     if (e != hipSuccess) return ofail_hip(e, "product launch");
   }
   if ((e = launch_ortho_apply(call, h->mats, h->chunks, h->matrix_chunks, s)) != hipSuccess)
@@ -411,6 +445,8 @@ edit_status_t edit_ortho_init(const edit_ortho_config_t* cfg, edit_ortho_t* out)
     if (e == hipSuccess) e = upload(h->load, t.load);
     if (e == hipSuccess) e = upload(h->gram.tile, t.gram);
     if (e == hipSuccess) e = upload(h->update.tile, t.update);
+    if (e == hipSuccess) e = upload(h->join.tile, t.join);
+    if (e == hipSuccess) e = upload(h->square.tile, t.square);
     if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e != hipSuccess) {
       (void)hipFree(h->arena);

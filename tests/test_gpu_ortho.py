@@ -33,7 +33,8 @@ def _ortho(numel, matrices, dtype, precision=None, **more):
 SHAPES = [
     [(1, 1)], [(1, 7), (5, 1), (3, 3)], [(16, 16)], [(64, 64), (65, 63), (63, 65)], [(127, 129), (129, 127)],
     [(128, 128)], [(256, 31), (31, 256)], [(100, 300), (300, 100), (129, 257)], [(513, 1000)], [(1000, 513)],
-    [(8, 3000), (3000, 8)], [(640, 640)] * 3, [(1, 4097), (4097, 1)], [(384, 700), (700, 384)] * 2, [(1300, 1290)],
+    [(8, 3000), (3000, 8)], [(96, 7129), (5001, 70)], [(128, 128), (1, 256), (96, 250), (256, 64), (17, 33)], [(250, 96)] * 3,
+    [(60, 60), (2, 2)], [(30, 9), (32, 32)], [(640, 640)] * 3, [(1, 4097), (4097, 1)], [(384, 700), (700, 384)] * 2, [(1300, 1290)],
 ]
 
 
