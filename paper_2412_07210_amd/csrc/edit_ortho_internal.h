@@ -47,9 +47,9 @@ inline bool ortho_is_small(int64_t r, int64_t c) {
 // cols.  Every array is zero behind its r columns.
 struct OrthoMat {
   // High and low halves; with FULL they share the first array (Layout in the
-  // kernels) and there is no second.
+  // kernels) and there is no second.  R and F have low halves with FULL only.
   _Float16* t[2][2];  // X^T, [buffer][half]: [c][ldr], and rows of zeros to a multiple of kOrthoPad
-  _Float16* g[2];     // R = A - sI                            [r][ldr]
+  _Float16* g[1];     // R = A - sI                            [r][ldr]
   _Float16* q[1];     // the update product's polynomial F     [r][ldr]
   double* norm_part;  // sums of squares of the update's chunks
   double* x_part;     // sums of squares of the X tiles of the last product

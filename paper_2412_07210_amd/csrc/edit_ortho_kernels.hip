@@ -323,45 +323,6 @@ __device__ __forceinline__ void slab_barrier() {
   asm volatile("" : : : "memory");
 }
 
-// The 4 x 4 transpose of what four neighbouring lanes hold: lane q of each
-// quad gives v[e] = element (e, q) and gets (q, e).
-template <int CTRL>
-__device__ __forceinline__ uint32_t quad_move(uint32_t x) {
-  return static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), CTRL, 0xf, 0xf, true));
-}
-__device__ __forceinline__ void quad_transpose(uint32_t (&v)[4], int lane) {
-  constexpr int kSwap1 = 1 | 0 << 2 | 3 << 4 | 2 << 6;  // lanes 1 0 3 2
-  constexpr int kSwap2 = 2 | 3 << 2 | 0 << 4 | 1 << 6;  // lanes 2 3 0 1
-  const bool odd = lane & 1, high = lane & 2;
-#pragma unroll
-  for (int e = 0; e < 4; e += 2) {
-    const uint32_t got = quad_move<kSwap1>(odd ? v[e] : v[e + 1]);
-    v[e] = odd ? got : v[e];
-    v[e + 1] = odd ? v[e + 1] : got;
-  }
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const uint32_t got = quad_move<kSwap2>(high ? v[e] : v[e + 2]);
-    v[e] = high ? got : v[e];
-    v[e + 2] = high ? v[e + 2] : got;
-  }
-}
-
-// A value as its (high, low) halves in 32 bits, and four of them in two rows.
-__device__ __forceinline__ uint32_t pack_split(float v) {
-  _Float16 hi, lo;
-  split(v, hi, lo);
-  return __builtin_bit_cast(uint16_t, hi) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, lo)) << 16;
-}
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-template <bool LOW>
-__device__ __forceinline__ void store_split(_Float16* hi, _Float16* lo, int64_t at, const uint32_t (&v)[4]) {
-  *reinterpret_cast<u32x2*>(hi + at) =
-      u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x05040100), __builtin_amdgcn_perm(v[3], v[2], 0x05040100)};
-  if constexpr (LOW)
-    *reinterpret_cast<u32x2*>(lo + at) =
-        u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x07060302), __builtin_amdgcn_perm(v[3], v[2], 0x07060302)};
-}
 // s of an iteration: the mean of A's diagonal, ||X||^2 / r (1 / r at first);
 // kept for the products that follow.
 template <int kThreads>
@@ -377,62 +338,110 @@ __device__ __forceinline__ double shift_of(const OrthoMat& mt, const OrthoTile& 
   return s;
 }
 
-// The results of a symmetric product, from the sums of one wave.
-template <int PRODUCT, bool FULL, int BP, int BQ, int FP, int FQ>
-__device__ __forceinline__ void store_symmetric(const f32x4 (&acc)[FP][FQ], const OrthoMat& mt, const OrthoTile& t,
-                                                const ProductArgs& args, double s, int wp, int wq, int lane) {
+// The results of a symmetric product from its sums: lane l of a wave holds
+// C[p .. p+3][q] of each 16 x 16 block, p = 4 (l / 16), q = l mod 16.  They go
+// through LDS, so that both the tile and its mirror image leave in whole rows
+// (eight bytes a lane, straight from the registers, cost a 1B layer's gram
+// product a quarter of its time).  Values behind the matrix become the zeros
+// that its padding holds anyway.
+template <int PRODUCT, bool FULL, int BP, int BQ, int WP, int WQ>
+__device__ __forceinline__ void store_symmetric(f32x4 (&acc)[WP / 16][WQ / 16], char* smem, const OrthoMat& mt,
+                                                const OrthoTile& t, const ProductArgs& args, double s, int wave,
+                                                int lane) {
   using L = Layout<FULL>;
+  constexpr int FP = WP / 16, FQ = WQ / 16, kWaves = (BP / WP) * (BQ / WQ), kThreads = kWaves * 64;
+  constexpr int kPitch = BP + 8;  // halves of a row in LDS: rows begin in different banks
+  static_assert(BQ * kPitch * 2 <= 2 * ProductShape<FULL, BP, BQ, WP, WQ>::kSlab, "LDS");
   const int r = mt.r, ld = mt.ldr;
-  const double keep = args.a + args.b * s + args.c * s * s;
-  // Lane l holds C[p .. p+3][q] of each 16 x 16 block, p = 4 (l / 16), q = l mod 16.
-  const int p0 = t.m * BP + wp + 4 * (lane >> 4), q0 = t.n * BQ + wq + (lane & 15);
-  const int quad = lane & 3;
-  const _Float16* r_hi = as_global(mt.g[0]);
-  const _Float16* r_lo = L::low(r_hi, as_global<const _Float16>(mt.g[1]));
-  _Float16* dst_hi = as_global(PRODUCT == kProductGram ? mt.g[0] : mt.q[0]);
-  _Float16* dst_lo = L::low(dst_hi, as_global(mt.g[1]));  // the square product's only with FULL
-  // F's low half goes into products only, R's into F as well
-  constexpr bool kStoreLow = PRODUCT == kProductGram || FULL;
-  // with FAST the update product adds the diagonal term itself, unrounded
-  const float diag = PRODUCT == kProductGram ? static_cast<float>(-s * kScaleA)
-                     : FULL                  ? static_cast<float>(keep * kScaleA)
-                                             : 0.f;
-  const float lin = static_cast<float>(args.b + 2.0 * args.c * s);
-  const float quadratic = static_cast<float>(args.c) / kScaleA;
-  half4 rh[2][FQ], rl[2][FQ];  // R, a row of blocks ahead
-  auto read_r = [&](int i) {
+  const int wp = (wave % (BP / WP)) * WP, wq = (wave / (BP / WP)) * WQ;
+  const int p_tile = t.m * BP, q_tile = t.n * BQ;
+  const int p0 = wp + 4 * (lane >> 4), q0 = wq + (lane & 15);  // in the tile
+  if constexpr (PRODUCT == kProductGram) {
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) {  // R is symmetric
-      const int64_t from = L::at(min(q0 + j * 16, r - 1), min(p0 + i * 16, ld - 4), ld);
-      rh[i & 1][j] = *reinterpret_cast<const half4*>(r_hi + from);
-      rl[i & 1][j] = *reinterpret_cast<const half4*>(r_lo + from);
+    for (int i = 0; i < FP; ++i)
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) acc[i][j] *= kScaleA / (kScaleX * kScaleX);
+  } else {
+    const _Float16* r_hi = as_global(mt.g[0]);
+    const float lin = static_cast<float>(args.b + 2.0 * args.c * s);
+    const float quadratic = static_cast<float>(args.c) / kScaleA;
+#pragma unroll
+    for (int i = 0; i < FP; ++i) {
+      half4 rh[FQ], rl[FULL ? FQ : 1];
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) {  // R is symmetric
+        const int64_t from = L::at(min(q_tile + q0 + j * 16, r - 1), min(p_tile + p0 + i * 16, ld - 4), ld);
+        rh[j] = *reinterpret_cast<const half4*>(r_hi + from);
+        if constexpr (FULL) rl[j] = *reinterpret_cast<const half4*>(r_hi + 32 + from);
+      }
+#pragma unroll
+      for (int j = 0; j < FQ; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = FULL ? join(rh[j], rl[FULL ? j : 0], e) : static_cast<float>(rh[j][e]);
+          acc[i][j][e] = lin * x + quadratic * acc[i][j][e];
+        }
     }
-  };
-  if constexpr (PRODUCT == kProductSquare) read_r(0);
+  }
+  // the gram product's shift; with FULL F's term (a + bs + cs^2) I, which with
+  // FAST the update product adds itself, unrounded
+  const bool diagonal = (PRODUCT == kProductGram || FULL) && t.m == t.n;
+  const bool edge = p_tile + BP > r || q_tile + BQ > r;
+  if (diagonal || edge) {
+    const double keep = args.a + args.b * s + args.c * s * s;
+    const float diag = diagonal ? static_cast<float>((PRODUCT == kProductGram ? -s : keep) * kScaleA) : 0.f;
 #pragma unroll
-  for (int i = 0; i < FP; ++i) {
-    const int pp = p0 + i * 16;
-    if constexpr (PRODUCT == kProductSquare)
-      if (i + 1 < FP) read_r(i + 1);
+    for (int i = 0; i < FP; ++i)
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) {
-      const int qq = q0 + j * 16;
-      uint32_t w[4];
+      for (int j = 0; j < FQ; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float v;
-        if constexpr (PRODUCT == kProductGram)
-          v = acc[i][j][e] * (kScaleA / (kScaleX * kScaleX));
-        else
-          v = lin * join(rh[i & 1][j], rl[i & 1][j], e) + quadratic * acc[i][j][e];
-        if (pp + e == qq) v += diag;
-        w[e] = pack_split(pp + e < r && qq < r ? v : 0.f);
+        for (int e = 0; e < 4; ++e) {
+          const int p = p_tile + p0 + i * 16 + e, q = q_tile + q0 + j * 16;
+          if (p == q) acc[i][j][e] += diag;
+          if (!(p < r && q < r)) acc[i][j][e] = 0.f;
+        }
+  }
+  _Float16* tile = reinterpret_cast<_Float16*>(smem);
+  _Float16* dst = as_global(PRODUCT == kProductGram ? mt.g[0] : mt.q[0]);
+#pragma unroll
+  for (int h = 0; h < (FULL ? 2 : 1); ++h) {  // the high halves, and with FULL the low ones
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < FP; ++i)
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) {
+        half4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = static_cast<_Float16>(acc[i][j][e]);
+          if (FULL && h == 0) acc[i][j][e] -= static_cast<float>(v[e]);
+        }
+        *reinterpret_cast<half4*>(tile + (q0 + j * 16) * kPitch + p0 + i * 16) = v;
       }
-      if (qq < r && pp < r) store_split<kStoreLow>(dst_hi, dst_lo, L::at(qq, pp, ld), w);
-      if (t.m != t.n) {
-        quad_transpose(w, lane);  // C[p + l mod 4][q - l mod 4 .. + 3]
-        if (pp + quad < r && qq - quad < r) store_split<kStoreLow>(dst_hi, dst_lo, L::at(pp + quad, qq - quad, ld), w);
+    __syncthreads();
+    constexpr int kRowThreads = BP / 8;
+#pragma unroll
+    for (int row0 = 0; row0 < BQ; row0 += kThreads / kRowThreads) {
+      const int q = row0 + threadIdx.x / kRowThreads, p = 8 * (threadIdx.x % kRowThreads);
+      if (q_tile + q < r && p_tile + p < r)
+        *reinterpret_cast<half8*>(dst + 32 * h + L::at(q_tile + q, p_tile + p, ld)) =
+            *reinterpret_cast<const half8*>(tile + q * kPitch + p);
+    }
+    if (t.m == t.n) continue;
+#pragma unroll
+    for (int b = 0; b < BP / 16 * (BQ / 32); b += kWaves) {
+      const int block = b + wave, p = 16 * (block % (BP / 16)), q = 32 * (block / (BP / 16)) + 8 * (lane >> 4);
+      half8 v;  // eight rows q of column p + l mod 16
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const half4 x = __builtin_bit_cast(
+            half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) fp16x4*)(
+                       tile + (q + 4 * k + ((lane & 15) >> 2)) * kPitch + p + 4 * (lane & 3))));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * k + e] = x[e];
       }
+      const int row = p_tile + p + (lane & 15);
+      if (row < r && q_tile + q < r) *reinterpret_cast<half8*>(dst + 32 * h + L::at(row, q_tile + q, ld)) = v;
     }
   }
 }
@@ -615,7 +624,6 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
     }
   }
 
-  // Values behind the matrix become the zeros that its padding holds anyway.
   if constexpr (PRODUCT != kProductUpdate) {
     if (piece) {
       f32x4* to = reinterpret_cast<f32x4*>(as_global(args.pieces)) + static_cast<int64_t>(t.slot) * (BP * BQ / 4);
@@ -625,7 +633,7 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
         for (int j = 0; j < FQ; ++j) to[(i * FQ + j) * S::kThreads + threadIdx.x] = acc[i][j];
       return;
     }
-    store_symmetric<PRODUCT, FULL, BP, BQ, FP, FQ>(acc, mt, t, args, s, wp, wq, lane);
+    store_symmetric<PRODUCT, FULL, BP, BQ, WP, WQ>(acc, smem, mt, t, args, s, wave, lane);
   } else {
     float sq = 0.f;
 #pragma unroll
@@ -696,9 +704,8 @@ __global__ __launch_bounds__((ProductShape<FULL, BP, BQ, WP, WQ>::kThreads)) voi
       for (int j = 0; j < FQ; ++j)
         acc[i][j] += from[static_cast<int64_t>(k) * (BP * BQ / 4) + (i * FQ + j) * kThreads + threadIdx.x];
   const double s = shift_of<kThreads>(mt, t, args.first);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  store_symmetric<kProductGram, FULL, BP, BQ, FP, FQ>(acc, mt, t, args, s, (wave % (BP / WP)) * WP,
-                                                      (wave / (BP / WP)) * WQ, lane);
+  __shared__ __align__(256) char smem[2 * ProductShape<FULL, BP, BQ, WP, WQ>::kSlab];
+  store_symmetric<kProductGram, FULL, BP, BQ, WP, WQ>(acc, smem, mt, t, args, s, threadIdx.x >> 6, threadIdx.x & 63);
 }
 
 // -------------------------------------------------------------- apply pass

@@ -290,7 +290,7 @@ size_t lay_out(edit_ortho* h, Tables& t, char* base) {
     } else {  // X's low half is read and written in place
       m.t[0][0] = c.take<_Float16>(xt), m.t[1][0] = c.take<_Float16>(xt);
       m.t[0][1] = m.t[1][1] = c.take<_Float16>(xt);
-      m.g[0] = c.take<_Float16>(a), m.g[1] = c.take<_Float16>(a), m.q[0] = c.take<_Float16>(a);
+      m.g[0] = c.take<_Float16>(a), m.q[0] = c.take<_Float16>(a);
     }
     m.norm_part = c.take<double>(m.chunks);
     m.x_part = c.take<double>(m.x_tiles);
