@@ -113,9 +113,10 @@ hipError_t launch_ortho_source(const OrthoCall& call, const OrthoMat* mats, cons
 // X^T of the update over its norm.
 hipError_t launch_ortho_load(bool full, const OrthoCall& call, const OrthoMat* mats, const OrthoTile* tiles, int count,
                              hipStream_t stream);
-// One product of an iteration, or the join of the gram product's pieces; `side`: of its tiles, `from`: the X^T buffer read, `last`: O to `u` instead of X^T.
+// One product of an iteration, or the join of the gram product's pieces; `side`: of its tiles; the
+// last step's update product writes O to `u` instead of X^T.
 hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const OrthoMat* mats, const OrthoTiles& tiles,
-                                const OrthoCoef& coef, int from, bool first, bool last, float* u, float* pieces,
+                                const OrthoCoef& coef, int step, int steps, float* u, float* pieces,
                                 hipStream_t stream);
 // The whole call but the outer step's source pass, for small matrices only, one
 // per block; `widest`: the largest r.

@@ -26,6 +26,8 @@
 // Error of O against 64 bits: 1e-4 to 1e-3 with FAST over Gaussian, low-rank
 // and power-law spectra (1e-3 to 4e-2 if X itself were rounded to fp16, 1e-2
 // to 9e-2 in bf16), and that of a 32-bit iteration with FULL.
+#include <type_traits>
+
 #include "edit_ortho_device.h"
 
 namespace edit {
@@ -141,60 +143,91 @@ __device__ __forceinline__ T* as_global(T* p) {
 }
 
 // One 64 x 64 tile of a stored matrix per block: X^T = u / ||u|| at kScaleX,
-// through LDS where that transposes.
+// through LDS where that transposes.  Eight elements a thread and access, also
+// where matrices begin at odd places (then element by element).
 template <int SOURCE, bool BF16, bool FULL>
 __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_load_kernel(OrthoArgs a, const OrthoMat* __restrict__ mats,
                                                                         const OrthoTile* __restrict__ tiles) {
+  using L = Layout<FULL>;
   constexpr int T = kOrthoLoadTile;
+  constexpr int kRuns = T / kVec;                          // of a row
+  constexpr int kPasses = T * kRuns / kOrthoStreamThreads;
   __shared__ uint32_t lds[T][T + 1];  // high half in the low 16 bits
   const OrthoTile t = tiles[blockIdx.x];
-  const OrthoMat& mt = mats[t.mat];
+  const OrthoMat mt = mats[t.mat];
+  const int run = threadIdx.x % kRuns, line = threadIdx.x / kRuns;
+  const int row0 = t.m * T, col0 = t.n * T;
+  const bool vectors = (mt.offset | mt.cols) % kVec == 0;
+
+  float x[kPasses][kVec], m[SOURCE == kSourceLocal ? kPasses : 1][kVec];
+#pragma unroll
+  for (int k = 0; k < kPasses; ++k) {
+    const int row = row0 + line + k * (kOrthoStreamThreads / kRuns), col = col0 + run * kVec;
+    const int count = row < mt.rows ? min(mt.cols - col, kVec) : 0;
+    const int64_t i = mt.offset + static_cast<int64_t>(row) * mt.cols + col;
+    auto read = [&](const void* from, auto bf16, float (&to)[kVec]) {
+      constexpr bool B = decltype(bf16)::value;
+      if (vectors && count > 0) {
+        load_vec<B>(from, i, 0, kVec, to);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) to[e] = e < count ? load_one<B>(from, i + e) : 0.f;
+      }
+    };
+    if constexpr (SOURCE == kSourceOuter)
+      read(a.u, std::false_type(), x[k]);
+    else
+      read(a.x, std::integral_constant<bool, BF16>(), x[k]);
+    if constexpr (SOURCE == kSourceLocal) read(a.momentum, std::false_type(), m[k]);
+  }
+
   double sum = 0.0;
-  for (int i = threadIdx.x; i < mt.chunks; i += kOrthoStreamThreads) sum += mt.norm_part[i];
+  for (int i = threadIdx.x; i < mt.chunks; i += kOrthoStreamThreads) sum += as_global(mt.norm_part)[i];
   sum = block_sum<kOrthoStreamThreads>(sum);
   // sums of squares of fp32 values neither overflow nor vanish in fp64, nor does their root's inverse
   const double inv = sum > 0.0 ? kScaleX / sqrt(sum) : (sum == 0.0 ? 0.0 : sum);
-  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-  const int row0 = t.m * T, col0 = t.n * T;
-  using L = Layout<FULL>;
   _Float16* x_hi = as_global(mt.t[0][0]);
   _Float16* x_lo = L::low(x_hi, as_global(mt.t[0][1]));
-  for (int y = ty; y < T; y += kOrthoStreamThreads / 64) {
-    const int row = row0 + y, col = col0 + tx;
-    float v = 0.f;
-    if (row < mt.rows && col < mt.cols) {
-      const int64_t i = mt.offset + static_cast<int64_t>(row) * mt.cols + col;
-      double u;
-      if constexpr (SOURCE == kSourcePlain) {
-        u = load_one<BF16>(a.x, i);
-      } else if constexpr (SOURCE == kSourceLocal) {
-        const double m = a.momentum[i];
-        u = a.nesterov ? fma(a.mu, m, static_cast<double>(load_one<BF16>(a.x, i))) : m;
-      } else {
-        u = a.u[i];
-      }
-      v = static_cast<float>(u * inv);
-      _Float16 hi, lo;
-      split(v, hi, lo);
-      if (mt.tall) {  // X^T is the stored matrix
-        const int64_t at = L::at(row, col, mt.ldr);
-        x_hi[at] = hi;
-        x_lo[at] = lo;
-      } else {
-        lds[y][tx] = __builtin_bit_cast(uint16_t, hi) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, lo)) << 16;
-      }
+  // eight neighbours of a row of X^T; zeros behind r, as its padding
+  auto write = [&](int q, int p, const half8& hi, const half8& lo) {
+    if (q >= mt.c || p >= mt.ldr) return;
+    const int64_t at = L::at(q, p, mt.ldr);
+    *reinterpret_cast<half8*>(x_hi + at) = hi;
+    *reinterpret_cast<half8*>(x_lo + at) = lo;
+  };
+#pragma unroll
+  for (int k = 0; k < kPasses; ++k) {
+    const int y = line + k * (kOrthoStreamThreads / kRuns);
+    half8 hi, lo;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      double u = x[k][e];
+      if constexpr (SOURCE == kSourceLocal)
+        u = a.nesterov ? fma(a.mu, static_cast<double>(m[k][e]), u) : static_cast<double>(m[k][e]);
+      _Float16 h, l;
+      split(static_cast<float>(u * inv), h, l);
+      // a NaN of the norm stays out of the padding
+      const bool in = row0 + y < mt.rows && col0 + run * kVec + e < mt.cols;
+      hi[e] = in ? h : _Float16(0), lo[e] = in ? l : _Float16(0);
+      if (!mt.tall)
+        lds[y][run * kVec + e] = __builtin_bit_cast(uint16_t, _Float16(hi[e])) |
+                                 static_cast<uint32_t>(__builtin_bit_cast(uint16_t, _Float16(lo[e]))) << 16;
     }
+    if (mt.tall) write(row0 + y, col0 + run * kVec, hi, lo);  // X^T is the stored matrix
   }
   if (mt.tall) return;
   __syncthreads();
-  for (int y = ty; y < T; y += kOrthoStreamThreads / 64) {
-    const int col = col0 + y, row = row0 + tx;
-    if (row < mt.rows && col < mt.cols) {
-      const uint32_t w = lds[tx][y];
-      const int64_t at = L::at(col, row, mt.ldr);
-      x_hi[at] = __builtin_bit_cast(_Float16, static_cast<uint16_t>(w));
-      x_lo[at] = __builtin_bit_cast(_Float16, static_cast<uint16_t>(w >> 16));
+#pragma unroll
+  for (int k = 0; k < kPasses; ++k) {
+    const int y = line + k * (kOrthoStreamThreads / kRuns);
+    half8 hi, lo;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      const uint32_t w = lds[run * kVec + e][y];
+      hi[e] = __builtin_bit_cast(_Float16, static_cast<uint16_t>(w));
+      lo[e] = __builtin_bit_cast(_Float16, static_cast<uint16_t>(w >> 16));
     }
+    write(col0 + y, row0 + run * kVec, hi, lo);
   }
 }
 
@@ -214,6 +247,7 @@ __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_load_kernel(OrthoAr
 struct ProductArgs {
   double a, b, c;
   int32_t from, first, last;
+  int32_t low;    // the update product writes X's low half
   float* pieces;  // unfinished sums of the gram product
 };
 
@@ -513,7 +547,7 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
   const int p8 = t.m * BP + wp + 8 * (lane >> 4), q0 = t.n * BQ + wq + (lane & 15);
   _Float16* to_hi = as_global(args.from ? mt.t[0][0] : mt.t[1][0]);
   _Float16* to_lo = L::low(to_hi, as_global(mt.t[0][1]));  // FAST: read and written in place
-  constexpr bool kLow = PRODUCT == kProductUpdate && !FULL;
+  constexpr bool kLow = PRODUCT == kProductUpdate && !FULL && !LAST;
   const float keep_lo = static_cast<float>(keep);
   half8 xl[kLow ? FP / 2 : 1][kLow ? FQ : 1];
   if constexpr (kLow) {
@@ -646,7 +680,7 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           v[e] = acc[i + (e >> 2)][j][e & 3] * (1.f / kScaleA);
-          if constexpr (!FULL) v[e] += keep_lo * static_cast<float>(xl[i / 2][j][e]);
+          if constexpr (kLow) v[e] += keep_lo * static_cast<float>(xl[i / 2][j][e]);
           if (!(pp + e < r && qq < c)) v[e] = 0.f;
         }
         if constexpr (LAST) {
@@ -669,7 +703,7 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
           if (qq < c && pp < r) {
             const int64_t at = L::at(qq, pp, ld);
             *reinterpret_cast<half8*>(to_hi + at) = hi;
-            *reinterpret_cast<half8*>(to_lo + at) = lo;
+            if (FULL || args.low) *reinterpret_cast<half8*>(to_lo + at) = lo;
           }
         }
       }
@@ -812,10 +846,10 @@ hipError_t launch_ortho_load(bool full, const OrthoCall& call, const OrthoMat* m
 }
 
 hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const OrthoMat* mats, const OrthoTiles& tiles,
-                                const OrthoCoef& coef, int from, bool first, bool last, float* u, float* pieces,
+                                const OrthoCoef& coef, int step, int steps, float* u, float* pieces,
                                 hipStream_t stream) {
   if (tiles.count == 0) return hipSuccess;
-  const ProductArgs args = {coef.a, coef.b, coef.c, from, first, last, pieces};
+  const ProductArgs args = {coef.a, coef.b, coef.c, step & 1, step == 0, step == steps - 1, step < steps - 2, pieces};
 #define EDIT_PRODUCT(P)                                                        \
   (full ? launch_product_of<P, true>(side, mats, tiles, args, u, stream) \
         : launch_product_of<P, false>(side, mats, tiles, args, u, stream))

@@ -364,8 +364,7 @@ edit_status_t enqueue(edit_ortho* h, OrthoCall call, hipStream_t s) {
   for (int k = 0; k < steps; ++k) {
     auto product = [&](OrthoProduct p, int side, const OrthoTiles& tiles) {
       if (e == hipSuccess)
-        e = launch_ortho_product(p, h->full, side, h->mats, tiles, h->coef[k], k & 1, k == 0, k == steps - 1, h->u,
-                                 h->pieces, s);
+        e = launch_ortho_product(p, h->full, side, h->mats, tiles, h->coef[k], k, steps, h->u, h->pieces, s);
     };
     product(kProductGram, h->gram_side, h->gram);
     product(kProductJoin, h->gram_side, h->join);
