@@ -85,7 +85,7 @@ struct OrthoCall {
   void* out;            // plain: the result;  local: the parameters
   float* momentum;      // local, outer
   float* theta;         // outer
-  float* u;             // [numel] scratch: outer's update, and every call's O in the end
+  float* u;             // [numel] scratch: outer's update
   void* const* reps;    // outer: K replicas (host array)
   const UnitRecord* rec;
   int32_t workers;
@@ -113,19 +113,15 @@ hipError_t launch_ortho_source(const OrthoCall& call, const OrthoMat* mats, cons
 // X^T of the update over its norm.
 hipError_t launch_ortho_load(bool full, const OrthoCall& call, const OrthoMat* mats, const OrthoTile* tiles, int count,
                              hipStream_t stream);
-// One product of an iteration, or the join of the gram product's pieces; `side`: of its tiles; the
-// last step's update product writes O to `u` instead of X^T.
+// One product of an iteration, or the join of the gram product's pieces;
+// `side`: of its tiles.  The last step's update product makes the call's outputs.
 hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const OrthoMat* mats, const OrthoTiles& tiles,
-                                const OrthoCoef& coef, int step, int steps, float* u, float* pieces,
+                                const OrthoCoef& coef, int step, int steps, const OrthoCall& call, float* pieces,
                                 hipStream_t stream);
 // The whole call but the outer step's source pass, for small matrices only, one
 // per block; `widest`: the largest r.
 hipError_t launch_ortho_small(bool full, const OrthoCall& call, const OrthoMat* mats, int count, int widest,
                               const OrthoCoef* coef, int steps, hipStream_t stream);
-// The call's outputs from O.
-hipError_t launch_ortho_apply(const OrthoCall& call, const OrthoMat* mats, const OrthoChunk* chunks, int count,
-                              hipStream_t stream);
-
 // The outer step's part of a handle: its argument check and, after the
 // decision has been enqueued, the orthogonalised update (edit_ortho_runtime.hip).
 edit_status_t check_ortho_unit(const edit_ortho* h, int64_t numel, int device);

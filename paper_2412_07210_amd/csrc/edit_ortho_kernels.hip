@@ -9,7 +9,8 @@
 //   gram     A = X X^T               } steps times, each a launch over the
 //   square   F = a I + b A + c A^2   } tiles of all matrices
 //   update   X <- F X                }
-//   apply    the call's outputs from O = X
+//
+// The last step's update product makes the call's outputs from O = X.
 //
 // Numerics.  The products run on the fp16 matrix cores with fp32 sums.  Two
 // things keep them near 32 bits of X at that price:
@@ -246,7 +247,8 @@ __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_load_kernel(OrthoAr
 // p >= q and store each twice.
 struct ProductArgs {
   double a, b, c;
-  int32_t from, first, last;
+  int32_t from;   // the X^T buffer read
+  int32_t first;  // step
   int32_t low;    // the update product writes X's low half
   float* pieces;  // unfinished sums of the gram product
 };
@@ -480,16 +482,139 @@ __device__ __forceinline__ void store_symmetric(f32x4 (&acc)[WP / 16][WQ / 16], 
   }
 }
 
+// ------------------------------------------------------------ the call's end
+
+// What a call does with O: its source, and the type of its parameters or replicas.
+constexpr int kNoApply = -1;
+constexpr int apply_of(int source, bool bf16) { return 2 * source + (bf16 ? 1 : 0); }
+
+// The first `count` of the elements i + e stride, e < 8, of the call's outputs
+// from O; VECTORS: there are eight, side by side at a multiple of eight.
+template <int SOURCE, bool BF16, bool VECTORS>
+__device__ __forceinline__ void apply_run(const OrthoArgs& a, const RepPtrs& reps, double step, bool rollback, int64_t i,
+                                          int stride, int count, const float (&o)[kVec]) {
+  auto read = [&](const void* from, auto bf16, float (&to)[kVec]) {
+    constexpr bool B = decltype(bf16)::value;
+    if constexpr (VECTORS) {
+      load_vec<B>(from, i, 0, kVec, to);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) to[e] = e < count ? load_one<B>(from, i + static_cast<int64_t>(e) * stride) : 0.f;
+    }
+  };
+  auto write = [&](void* to, auto bf16, const float (&from)[kVec]) {
+    constexpr bool B = decltype(bf16)::value;
+    if constexpr (VECTORS) {
+      store_vec<B>(to, i, 0, kVec, from);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e)
+        if (e < count) store_one<B>(to, i + static_cast<int64_t>(e) * stride, from[e]);
+    }
+  };
+  const std::integral_constant<bool, BF16> type;
+  if constexpr (SOURCE == kSourcePlain) {
+    write(a.out, type, o);
+  } else if constexpr (SOURCE == kSourceLocal) {
+    float p[kVec];
+    read(a.out, type, p);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e)
+      p[e] = static_cast<float>(fma(a.keep, static_cast<double>(p[e]), -step * static_cast<double>(o[e])));
+    write(a.out, type, p);
+  } else {
+    float th[kVec];
+    read(a.theta, std::false_type(), th);
+    if (!rollback) {  // otherwise theta stays, to the sign of its zeros
+#pragma unroll
+      for (int e = 0; e < kVec; ++e)
+        th[e] = static_cast<float>(fma(-step, static_cast<double>(o[e]), static_cast<double>(th[e])));
+      write(a.theta, std::false_type(), th);
+    }
+    for (int j = 0; j < a.workers; ++j) write(reps.p[j], type, th);
+  }
+}
+
+// The last step's tile of O (in the registers of the update product) into the
+// call's outputs: through LDS, 64 stored rows at a time, so that each row's
+// elements are read and written side by side.
+template <int APPLY, int BP, int BQ, int WP, int WQ>
+__device__ __forceinline__ void apply_tile(const f32x4 (&acc)[WP / 16][WQ / 16], char* smem, const OrthoMat& mt,
+                                           const OrthoTile& t, const OrthoArgs& a, const RepPtrs& reps, int wave,
+                                           int lane) {
+  constexpr int SOURCE = APPLY / 2;
+  constexpr int kRows = 64, kThreads = (BP / WP) * (BQ / WQ) * 64;
+  constexpr int kCols = BP;  // of a stored row
+  constexpr int kPitch = kCols + 4;
+  static_assert(BP == BQ && kRows % WP == 0 && kRows % WQ == 0, "whole waves a pass");
+  static_assert(kRows * kPitch * 4 <= 2 * (BP + BQ) * 128, "LDS");
+  float* tile = reinterpret_cast<float*>(smem);
+  const int wp = (wave % (BP / WP)) * WP, wq = (wave / (BP / WP)) * WQ;
+  const int p0 = wp + 8 * (lane >> 4), q0 = wq + (lane & 15);
+  const double step = a.lr * mt.scale;
+  bool rollback = false;
+  if constexpr (SOURCE == kSourceOuter) rollback = a.rec->rollback;
+  const bool aligned = (mt.offset | mt.cols) % kVec == 0;
+  const int row0 = mt.tall ? t.n * BQ : t.m * BP, col0 = mt.tall ? t.m * BP : t.n * BQ;
+  for (int pass = 0; pass < BP; pass += kRows) {
+    __syncthreads();
+    if ((mt.tall ? wq : wp) / kRows * kRows == pass) {
+#pragma unroll
+      for (int i = 0; i < WP / 16; i += 2)
+#pragma unroll
+        for (int j = 0; j < WQ / 16; ++j) {
+          const int p = p0 + 16 * i, q = q0 + 16 * j;  // O[p .. p+7][q]
+          if (mt.tall) {
+            float* to = tile + (q - pass) * kPitch + p;
+            *reinterpret_cast<f32x4*>(to) = acc[i][j];
+            *reinterpret_cast<f32x4*>(to + 4) = acc[i + 1][j];
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) tile[(p + e - pass) * kPitch + q] = acc[i + (e >> 2)][j][e & 3];
+          }
+        }
+    }
+    __syncthreads();
+    constexpr bool BF16 = (APPLY & 1) != 0;
+    if (aligned) {  // eight elements of a row a thread
+      for (int k = threadIdx.x; k < kRows * kCols / kVec; k += kThreads) {
+        const int y = k / (kCols / kVec), x = k % (kCols / kVec) * kVec;
+        const int row = row0 + pass + y, col = col0 + x;
+        if (row >= mt.rows || col >= mt.cols) continue;
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(tile + y * kPitch + x);
+        const f32x4 hi = *reinterpret_cast<const f32x4*>(tile + y * kPitch + x + 4);
+        const float o[kVec] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        apply_run<SOURCE, BF16, true>(a, reps, step, rollback,
+                                      mt.offset + static_cast<int64_t>(row) * mt.cols + col, 1, kVec, o);
+      }
+    } else {  // rows that begin anywhere: eight rows a thread, a row's elements lane by lane
+      constexpr int kStep = kThreads / kCols;
+      const int x = threadIdx.x % kCols, col = col0 + x;
+      if (col < mt.cols)
+        for (int y = threadIdx.x / kCols; y < kRows; y += kVec * kStep) {
+          const int row = row0 + pass + y;
+          float o[kVec];
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) o[e] = tile[(y + e * kStep) * kPitch + x];
+          apply_run<SOURCE, BF16, false>(a, reps, step, rollback,
+                                         mt.offset + static_cast<int64_t>(row) * mt.cols + col, kStep * mt.cols,
+                                         (mt.rows - row + kStep - 1) / kStep, o);
+        }
+    }
+  }
+}
+
 // One tile of a product per block.  While one slab is multiplied, the loads of
 // the next are under way.  A wave's operands are read a step ahead of their
 // use: each register is read anew right after its last use, and the barrier
 // between slabs stands before the last step of a slab, so that the first reads
 // of the next one run under that step's products.
-template <int PRODUCT, bool FULL, bool LAST, int BP, int BQ, int WP, int WQ>
+template <int PRODUCT, bool FULL, int APPLY, int BP, int BQ, int WP, int WQ>
 __global__ __launch_bounds__((ProductShape<FULL, BP, BQ, WP, WQ>::kThreads),
                              2)  // waves per SIMD that the registers are budgeted for
 void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __restrict__ tiles, ProductArgs args,
-                          float* __restrict__ out) {
+                          OrthoArgs call, RepPtrs reps) {
+  constexpr bool LAST = APPLY != kNoApply;
   using S = ProductShape<FULL, BP, BQ, WP, WQ>;
   constexpr Reading kReadP = PRODUCT == kProductGram ? kAcross : PRODUCT == kProductUpdate ? kBlocks : kAlong;
   constexpr Reading kReadQ = PRODUCT == kProductGram ? kAcross : kAlong;
@@ -681,16 +806,11 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
         for (int e = 0; e < 8; ++e) {
           v[e] = acc[i + (e >> 2)][j][e & 3] * (1.f / kScaleA);
           if constexpr (kLow) v[e] += keep_lo * static_cast<float>(xl[i / 2][j][e]);
-          if (!(pp + e < r && qq < c)) v[e] = 0.f;
+          if (!LAST && !(pp + e < r && qq < c)) v[e] = 0.f;
         }
         if constexpr (LAST) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (pp + e < r && qq < c) {
-              const int64_t o = mt.tall ? static_cast<int64_t>(qq) * mt.cols + pp + e
-                                        : static_cast<int64_t>(pp + e) * mt.cols + qq;
-              out[mt.offset + o] = v[e] * (1.f / kScaleX);
-            }
+          for (int e = 0; e < 8; ++e) acc[i + (e >> 2)][j][e & 3] = v[e] * (1.f / kScaleX);
         } else {
           half8 hi, lo;
 #pragma unroll
@@ -708,7 +828,9 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
         }
       }
     }
-    if constexpr (!LAST) {
+    if constexpr (LAST) {
+      apply_tile<APPLY, BP, BQ, WP, WQ>(acc, smem, mt, t, call, reps, wave, lane);
+    } else {
       const double sum = block_sum<S::kThreads>(static_cast<double>(sq) / (static_cast<double>(kScaleX) * kScaleX));
       if (threadIdx.x == 0) as_global(mt.x_part)[t.slot] = sum;
     }
@@ -742,58 +864,11 @@ __global__ __launch_bounds__((ProductShape<FULL, BP, BQ, WP, WQ>::kThreads)) voi
   store_symmetric<kProductGram, FULL, BP, BQ, WP, WQ>(acc, smem, mt, t, args, s, threadIdx.x >> 6, threadIdx.x & 63);
 }
 
-// -------------------------------------------------------------- apply pass
-
-// One chunk of a matrix per block: the call's outputs from O, which is fp32 in
-// the stored order.  Bound by memory.
-template <int SOURCE, bool BF16>
-__global__ __launch_bounds__(kOrthoStreamThreads) void ortho_apply_kernel(OrthoArgs a, RepPtrs reps,
-                                                                         const OrthoMat* __restrict__ mats,
-                                                                         const OrthoChunk* __restrict__ chunks) {
-  const OrthoChunk ch = chunks[blockIdx.x];
-  if (ch.mat < 0) return;
-  const double step = a.lr * mats[ch.mat].scale;
-  const int64_t first = ch.begin / kVec;
-  const int64_t last = (ch.end + kVec - 1) / kVec;
-  for (int64_t v = first + threadIdx.x; v < last; v += kOrthoStreamThreads) {
-    const int64_t i = v * kVec;
-    const int lo = ch.begin > i ? static_cast<int>(ch.begin - i) : 0;
-    const int hi = ch.end < i + kVec ? static_cast<int>(ch.end - i) : kVec;
-    float o[kVec];
-    load_vec<false>(a.u, i, lo, hi, o);
-    if constexpr (SOURCE == kSourcePlain) {
-      store_vec<BF16>(a.out, i, lo, hi, o);
-    } else if constexpr (SOURCE == kSourceLocal) {
-      float p[kVec];
-      load_vec<BF16>(a.out, i, lo, hi, p);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e)
-        p[e] = static_cast<float>(fma(a.keep, static_cast<double>(p[e]), -step * static_cast<double>(o[e])));
-      store_vec<BF16>(a.out, i, lo, hi, p);
-    } else {
-      float th[kVec];
-      load_vec<false>(a.theta, i, lo, hi, th);
-      if (!a.rec->rollback) {
-#pragma unroll
-        for (int e = 0; e < kVec; ++e)
-          th[e] = static_cast<float>(fma(-step, static_cast<double>(o[e]), static_cast<double>(th[e])));
-        store_vec<false>(a.theta, i, lo, hi, th);
-      }
-      for (int j = 0; j < a.workers; ++j) store_vec<BF16>(reps.p[j], i, lo, hi, th);
-    }
-  }
-}
-
-template <int PRODUCT, bool FULL, int BP, int BQ, int WP, int WQ>
-hipError_t launch_product(const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args, float* out,
-                          hipStream_t stream) {
-  using S = ProductShape<FULL, BP, BQ, WP, WQ>;
-  if (PRODUCT == kProductUpdate && args.last)
-    ortho_product_kernel<PRODUCT, FULL, PRODUCT == kProductUpdate, BP, BQ, WP, WQ>
-        <<<tiles.count, S::kThreads, 0, stream>>>(mats, tiles.tile, args, out);
-  else
-    ortho_product_kernel<PRODUCT, FULL, false, BP, BQ, WP, WQ>
-        <<<tiles.count, S::kThreads, 0, stream>>>(mats, tiles.tile, args, out);
+template <int PRODUCT, bool FULL, int APPLY, int BP, int BQ, int WP, int WQ>
+hipError_t launch_product(const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args, const OrthoArgs& call,
+                          const RepPtrs& reps, hipStream_t stream) {
+  ortho_product_kernel<PRODUCT, FULL, APPLY, BP, BQ, WP, WQ>
+      <<<tiles.count, ProductShape<FULL, BP, BQ, WP, WQ>::kThreads, 0, stream>>>(mats, tiles.tile, args, call, reps);
   return hipGetLastError();
 }
 
@@ -804,11 +879,11 @@ hipError_t launch_join(const OrthoMat* mats, const OrthoTiles& tiles, const Prod
   return hipGetLastError();
 }
 
-template <int PRODUCT, bool FULL>
+template <int PRODUCT, bool FULL, int APPLY = kNoApply>
 hipError_t launch_product_of(int side, const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args,
-                             float* out, hipStream_t stream) {
-  if (side == 128) return launch_product<PRODUCT, FULL, 128, 128, 64, 64>(mats, tiles, args, out, stream);
-  if (side == 64) return launch_product<PRODUCT, FULL, 64, 64, 32, 32>(mats, tiles, args, out, stream);
+                             const OrthoArgs& call, const RepPtrs& reps, hipStream_t stream) {
+  if (side == 128) return launch_product<PRODUCT, FULL, APPLY, 128, 128, 64, 64>(mats, tiles, args, call, reps, stream);
+  if (side == 64) return launch_product<PRODUCT, FULL, APPLY, 64, 64, 32, 32>(mats, tiles, args, call, reps, stream);
   return hipErrorInvalidValue;
 }
 
@@ -846,39 +921,35 @@ hipError_t launch_ortho_load(bool full, const OrthoCall& call, const OrthoMat* m
 }
 
 hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const OrthoMat* mats, const OrthoTiles& tiles,
-                                const OrthoCoef& coef, int step, int steps, float* u, float* pieces,
+                                const OrthoCoef& coef, int step, int steps, const OrthoCall& call, float* pieces,
                                 hipStream_t stream) {
   if (tiles.count == 0) return hipSuccess;
-  const ProductArgs args = {coef.a, coef.b, coef.c, step & 1, step == 0, step == steps - 1, step < steps - 2, pieces};
-#define EDIT_PRODUCT(P)                                                        \
-  (full ? launch_product_of<P, true>(side, mats, tiles, args, u, stream) \
-        : launch_product_of<P, false>(side, mats, tiles, args, u, stream))
+  const ProductArgs args = {coef.a, coef.b, coef.c, step & 1, step == 0, step < steps - 2, pieces};
+  const OrthoArgs a = args_of(call);
+  const RepPtrs r = reps_of(call);
+#define EDIT_PRODUCT(P, A)                                                        \
+  (full ? launch_product_of<P, true, A>(side, mats, tiles, args, a, r, stream) \
+        : launch_product_of<P, false, A>(side, mats, tiles, args, a, r, stream))
   switch (product) {
-    case kProductGram: return EDIT_PRODUCT(kProductGram);
-    case kProductSquare: return EDIT_PRODUCT(kProductSquare);
-    case kProductUpdate: return EDIT_PRODUCT(kProductUpdate);
+    case kProductGram: return EDIT_PRODUCT(kProductGram, kNoApply);
     case kProductJoin:
       if (side != 64) return hipErrorInvalidValue;
       return full ? launch_join<true, 64, 64, 32, 32>(mats, tiles, args, stream)
                   : launch_join<false, 64, 64, 32, 32>(mats, tiles, args, stream);
+    case kProductSquare: return EDIT_PRODUCT(kProductSquare, kNoApply);
+    case kProductUpdate:
+      if (step < steps - 1) return EDIT_PRODUCT(kProductUpdate, kNoApply);
+      switch (apply_of(call.source, call.bf16)) {
+        case apply_of(kSourcePlain, false): return EDIT_PRODUCT(kProductUpdate, apply_of(kSourcePlain, false));
+        case apply_of(kSourcePlain, true): return EDIT_PRODUCT(kProductUpdate, apply_of(kSourcePlain, true));
+        case apply_of(kSourceLocal, false): return EDIT_PRODUCT(kProductUpdate, apply_of(kSourceLocal, false));
+        case apply_of(kSourceLocal, true): return EDIT_PRODUCT(kProductUpdate, apply_of(kSourceLocal, true));
+        case apply_of(kSourceOuter, false): return EDIT_PRODUCT(kProductUpdate, apply_of(kSourceOuter, false));
+        case apply_of(kSourceOuter, true): return EDIT_PRODUCT(kProductUpdate, apply_of(kSourceOuter, true));
+      }
   }
 #undef EDIT_PRODUCT
   return hipErrorInvalidValue;
-}
-
-hipError_t launch_ortho_apply(const OrthoCall& call, const OrthoMat* mats, const OrthoChunk* chunks, int count,
-                              hipStream_t stream) {
-  if (count == 0) return hipSuccess;
-  const OrthoArgs a = args_of(call);
-  const RepPtrs r = reps_of(call);
-#define EDIT_APPLY(S, B) ortho_apply_kernel<S, B><<<count, kOrthoStreamThreads, 0, stream>>>(a, r, mats, chunks)
-  switch (call.source) {
-    case kSourcePlain: call.bf16 ? EDIT_APPLY(kSourcePlain, true) : EDIT_APPLY(kSourcePlain, false); break;
-    case kSourceLocal: call.bf16 ? EDIT_APPLY(kSourceLocal, true) : EDIT_APPLY(kSourceLocal, false); break;
-    case kSourceOuter: call.bf16 ? EDIT_APPLY(kSourceOuter, true) : EDIT_APPLY(kSourceOuter, false); break;
-  }
-#undef EDIT_APPLY
-  return hipGetLastError();
 }
 
 }  // namespace edit

@@ -4,7 +4,8 @@
 // A handle owns, for one unit layout, a workspace for every matrix and the
 // tables its launches run over: chunks of the unit for the streaming passes,
 // tiles of all matrices for the products.  A call enqueues source -> load ->
-// steps x (gram, square, update) -> apply on the caller's stream.
+// steps x (gram, square, update) on the caller's stream, or one launch for
+// small matrices.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -364,7 +365,7 @@ edit_status_t enqueue(edit_ortho* h, OrthoCall call, hipStream_t s) {
   for (int k = 0; k < steps; ++k) {
     auto product = [&](OrthoProduct p, int side, const OrthoTiles& tiles) {
       if (e == hipSuccess)
-        e = launch_ortho_product(p, h->full, side, h->mats, tiles, h->coef[k], k, steps, h->u, h->pieces, s);
+        e = launch_ortho_product(p, h->full, side, h->mats, tiles, h->coef[k], k, steps, call, h->pieces, s);
     };
     product(kProductGram, h->gram_side, h->gram);
     product(kProductJoin, h->gram_side, h->join);
@@ -372,8 +373,6 @@ edit_status_t enqueue(edit_ortho* h, OrthoCall call, hipStream_t s) {
     product(kProductUpdate, h->update_side, h->update);
     if (e != hipSuccess) return ofail_hip(e, "product launch");
   }
-  if ((e = launch_ortho_apply(call, h->mats, h->chunks, h->matrix_chunks, s)) != hipSuccess)
-    return ofail_hip(e, "apply pass launch");
   return EDIT_OK;
 }
 
