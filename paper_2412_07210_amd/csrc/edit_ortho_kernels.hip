@@ -546,7 +546,7 @@ __device__ __forceinline__ void apply_tile(const f32x4 (&acc)[WP / 16][WQ / 16],
   constexpr int kRows = 64, kThreads = (BP / WP) * (BQ / WQ) * 64;
   constexpr int kCols = BP;  // of a stored row
   constexpr int kPitch = kCols + 4;
-  static_assert(BP == BQ && kRows % WP == 0 && kRows % WQ == 0, "whole waves a pass");
+  static_assert(BP == BQ && BP % kRows == 0 && kRows % 32 == 0, "whole blocks of results a pass");
   static_assert(kRows * kPitch * 4 <= 2 * (BP + BQ) * 128, "LDS");
   float* tile = reinterpret_cast<float*>(smem);
   const int wp = (wave % (BP / WP)) * WP, wq = (wave / (BP / WP)) * WQ;
@@ -558,22 +558,21 @@ __device__ __forceinline__ void apply_tile(const f32x4 (&acc)[WP / 16][WQ / 16],
   const int row0 = mt.tall ? t.n * BQ : t.m * BP, col0 = mt.tall ? t.m * BP : t.n * BQ;
   for (int pass = 0; pass < BP; pass += kRows) {
     __syncthreads();
-    if ((mt.tall ? wq : wp) / kRows * kRows == pass) {
 #pragma unroll
-      for (int i = 0; i < WP / 16; i += 2)
+    for (int i = 0; i < WP / 16; i += 2)
 #pragma unroll
-        for (int j = 0; j < WQ / 16; ++j) {
-          const int p = p0 + 16 * i, q = q0 + 16 * j;  // O[p .. p+7][q]
-          if (mt.tall) {
-            float* to = tile + (q - pass) * kPitch + p;
-            *reinterpret_cast<f32x4*>(to) = acc[i][j];
-            *reinterpret_cast<f32x4*>(to + 4) = acc[i + 1][j];
-          } else {
+      for (int j = 0; j < WQ / 16; ++j) {
+        const int p = p0 + 16 * i, q = q0 + 16 * j;  // O[p .. p+7][q]
+        if ((mt.tall ? wq + 16 * j : wp + 16 * i) / kRows * kRows != pass) continue;
+        if (mt.tall) {
+          float* to = tile + (q - pass) * kPitch + p;
+          *reinterpret_cast<f32x4*>(to) = acc[i][j];
+          *reinterpret_cast<f32x4*>(to + 4) = acc[i + 1][j];
+        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) tile[(p + e - pass) * kPitch + q] = acc[i + (e >> 2)][j][e & 3];
-          }
+          for (int e = 0; e < 8; ++e) tile[(p + e - pass) * kPitch + q] = acc[i + (e >> 2)][j][e & 3];
         }
-    }
+      }
     __syncthreads();
     constexpr bool BF16 = (APPLY & 1) != 0;
     if (aligned) {  // eight elements of a row a thread
@@ -668,21 +667,25 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
 
   // The update product's results: lane l holds C^T[q][p .. p+7], q = l mod 16, p
   // = 8 (l / 16), of each pair of 16 x 16 blocks.  FAST adds X's low half to
-  // them, which is read ahead of the sums.
+  // them, which is read ahead of the sums where there are registers for it.
   const int p8 = t.m * BP + wp + 8 * (lane >> 4), q0 = t.n * BQ + wq + (lane & 15);
   _Float16* to_hi = as_global(args.from ? mt.t[0][0] : mt.t[1][0]);
   _Float16* to_lo = L::low(to_hi, as_global(mt.t[0][1]));  // FAST: read and written in place
   constexpr bool kLow = PRODUCT == kProductUpdate && !FULL && !LAST;
   const float keep_lo = static_cast<float>(keep);
   half8 xl[kLow ? FP / 2 : 1][kLow ? FQ : 1];
-  if constexpr (kLow) {
+  auto read_low = [&] {
+    if constexpr (kLow) {
 #pragma unroll
-    for (int i = 0; i < FP; i += 2)
+      for (int i = 0; i < FP; i += 2)
 #pragma unroll
-      for (int j = 0; j < FQ; ++j)
-        xl[i / 2][j] = *reinterpret_cast<const half8*>(
-            to_lo + L::at(min(q0 + j * 16, c - 1), min(p8 + i * 16, ld - 8), ld));
-  }
+        for (int j = 0; j < FQ; ++j)
+          xl[i / 2][j] = *reinterpret_cast<const half8*>(
+              to_lo + L::at(min(q0 + j * 16, c - 1), min(p8 + i * 16, ld - 8), ld));
+    }
+  };
+  constexpr bool kLowFirst = FP * FQ <= 16;
+  if constexpr (kLowFirst) read_low();
 
   auto slab = [&](int n) { return smem + (n & 1) * S::kSlab; };
   auto read_p = [&](const char* at, int part, int i) {
@@ -794,6 +797,7 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
     }
     store_symmetric<PRODUCT, FULL, BP, BQ, WP, WQ>(acc, smem, mt, t, args, s, wave, lane);
   } else {
+    if constexpr (!kLowFirst) read_low();
     float sq = 0.f;
 #pragma unroll
     for (int j = 0; j < FQ; ++j) {
@@ -882,6 +886,8 @@ hipError_t launch_join(const OrthoMat* mats, const OrthoTiles& tiles, const Prod
 template <int PRODUCT, bool FULL, int APPLY = kNoApply>
 hipError_t launch_product_of(int side, const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args,
                              const OrthoArgs& call, const RepPtrs& reps, hipStream_t stream) {
+  if constexpr (PRODUCT == kProductUpdate && !FULL)
+    if (side == 256) return launch_product<PRODUCT, FULL, APPLY, 256, 256, 128, 64>(mats, tiles, args, call, reps, stream);
   if (side == 128) return launch_product<PRODUCT, FULL, APPLY, 128, 128, 64, 64>(mats, tiles, args, call, reps, stream);
   if (side == 64) return launch_product<PRODUCT, FULL, APPLY, 64, 64, 32, 32>(mats, tiles, args, call, reps, stream);
   return hipErrorInvalidValue;

@@ -46,12 +46,26 @@ constexpr int kXcds = 8;                          // workgroups go to the XCDs i
 // 128) 19 and 8, 160: 22 and 18, 240: 23 and 24, 280: 33 and 25, 400: 34 and
 // 33, 480: 35 and 39; update product of 64 tiles 14 and 8, 192: 18 and 15, 256:
 // 19 and 20, 512: 29 and 35.
-constexpr int kLargeSide = 128, kSmallSide = 64;
+//
+// FAST's update product of much work takes 256 x 256 tiles, which load half as
+// much per operation, but a CU runs one at a time, so that the last round of
+// them has to be nearly full.  us at 128 and 256: 192 tiles (of 256 x 256) of
+// r = 1024 43 and 45, 256: 53 and 51, 384: 77 and 89, 512: 111 and 103; r =
+// 2048, 256: 80 and 71, 384: 116 and 130, 512: 163 and 145; r = 4096, 256: 138
+// and 120.  Whole calls: one 4096 x 11008 matrix (688 tiles) 3830 and 3670, a
+// 1B layer's local step (784, the last round nearly empty) 2533 and 2563.
+// FULL's is bound by its operations, and has no registers for them.
+constexpr int kLargeSide = 128, kSmallSide = 64, kHugeSide = 256;
 // A gram tile whose sum is kCutFrom times as long as a CU's share of all of
 // them (and kPieceSlabs slabs at least) is cut into pieces of about that.
 constexpr int64_t kPieceSlabs = 8, kCutFrom = 2;
 int symmetric_side(int64_t large_tiles, int num_cu) { return 2 * large_tiles <= 3 * num_cu ? kSmallSide : kLargeSide; }
-int update_side(int64_t large_tiles, int num_cu) { return large_tiles < num_cu ? kSmallSide : kLargeSide; }
+int update_side(int64_t large_tiles, int64_t huge_tiles, int num_cu, bool full) {
+  if (large_tiles < num_cu) return kSmallSide;
+  const int64_t idle = oround_up(huge_tiles, num_cu) - huge_tiles;  // CUs of the last round
+  const bool padded = 10 * 4 * huge_tiles > 11 * large_tiles;  // more work for it than it saves
+  return !full && !padded && 8 * idle <= huge_tiles ? kHugeSide : kLargeSide;
+}
 // Side, in tiles, of the groups that tiles are taken in.  Products of a 1B
 // layer and of a 4096 x 11008 matrix, us with groups of 1, 2, 4 and 8: update
 // (FAST) 294, 259, 255, 260 and 465, 410, 373, 375; gram 164, 149, 148, 149
@@ -204,17 +218,19 @@ Tables make_tables(const edit_ortho_config_t* cfg, int num_cu) {
       for (int32_t b = 0; b < oceil_div(in.cols, kOrthoLoadTile); ++b) t.load.push_back({k, a, b, 0, 0, 0});
     t.mats.push_back(m);
   }
-  int64_t symmetric = 0, whole = 0;  // tiles at the large side
+  const bool full = cfg->precision == EDIT_ORTHO_FULL;
+  int64_t symmetric = 0, whole = 0, huge = 0;  // tiles at the large side; at the huge one
   for (const OrthoMat& m : t.mats) {
     const int64_t tr = oceil_div(m.r, kLargeSide), tc = oceil_div(m.c, kLargeSide);
     symmetric += tr * (tr + 1) / 2;
     whole += tr * tc;
+    huge += oceil_div(m.r, kHugeSide) * oceil_div(m.c, kHugeSide);
   }
   t.small = !t.mats.empty() && std::all_of(t.mats.begin(), t.mats.end(),
                                            [](const OrthoMat& m) { return ortho_is_small(m.r, m.c); });
   t.gram_side = symmetric_side(symmetric, num_cu);
-  t.update_side = update_side(whole, num_cu);
-  const int slab = ortho_slab(cfg->precision == EDIT_ORTHO_FULL);
+  t.update_side = update_side(whole, huge, num_cu, full);
+  const int slab = ortho_slab(full);
   int64_t work = 0;  // slabs of all symmetric tiles
   for (const OrthoMat& m : t.mats) {
     const int64_t ts = oceil_div(m.r, t.gram_side);

@@ -51,6 +51,24 @@ def test_orthogonalize_shapes(shapes, dtype, precision):
         assert_o_close(matrix(y, m), ortho64(matrix(x, m)), precision, f"{dtype} {precision} {m}")
 
 
+@pytest.mark.parametrize("shapes,gaps", [([(500, 29201)], [3]), ([(29192, 504)], [0]), ([(1000, 7592), (7603, 1010)], [0, 8])],
+                         ids=["wide", "tall", "both"])
+def test_matrices_of_many_tiles(shapes, gaps):
+    """Work for every CU at the products' largest tiles, whose edges no side is a multiple of."""
+    numel, mats = layout(shapes, gaps)
+    x = _randn(numel, 6).to(torch.bfloat16)
+    p, m = _randn(numel, 7, 0.02).to(torch.bfloat16), torch.zeros(numel, device=DEV)
+    with _ortho(numel, mats, "bf16") as o:
+        scales = o.cfg.scales()
+        y = o.orthogonalize(x)
+        assert torch.equal(y, o.orthogonalize(x))
+        ref_p, ref_m, outs = _local_step64(p, x, m, mats, scales, 0.02, 0.9, 0.1, True)
+        o.local_step(p, x, m, lr=0.02, mu=0.9, weight_decay=0.1)
+    for spec in mats:
+        assert_o_close(matrix(y, spec), ortho64(matrix(x, spec)), "fast", f"{spec}")
+    _check_step(p, ref_p, mats, outs, [0.02 * abs(s) for s in scales], "fast", "local")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_odd_offsets_and_elements_of_no_matrix(dtype):
     """Matrices at odd offsets behind gaps of 1 to 5 elements; what lies between them stays as it was."""
