@@ -71,7 +71,7 @@ struct OrthoChunk {
 // Tile (m, n) of a matrix: of its rows and columns (load), of C's p and q (products); mat = -1: none.
 struct OrthoTile {
   int32_t mat, m, n;
-  int32_t slot;        // update: of x_part;  gram: of `pieces` (-1: a whole sum)
+  int32_t slot;        // update: of x_part;  gram, square: of `pieces` (-1: a whole sum)
   int32_t begin, end;  // products: slabs of the sum;  join: pieces
 };
 
@@ -98,7 +98,7 @@ struct OrthoCoef {
 };
 
 // Products of an iteration.
-enum OrthoProduct { kProductGram = 0, kProductSquare = 1, kProductUpdate = 2, kProductJoin = 3 };
+enum OrthoProduct { kProductGram = 0, kProductSquare = 1, kProductUpdate = 2, kProductGramJoin = 3, kProductSquareJoin = 4 };
 // Values of k that a product takes a step.
 inline int ortho_slab(bool full) { return full ? 32 : 64; }
 
@@ -113,7 +113,7 @@ hipError_t launch_ortho_source(const OrthoCall& call, const OrthoMat* mats, cons
 // X^T of the update over its norm.
 hipError_t launch_ortho_load(bool full, const OrthoCall& call, const OrthoMat* mats, const OrthoTile* tiles, int count,
                              hipStream_t stream);
-// One product of an iteration, or the join of the gram product's pieces;
+// One product of an iteration, or the join of a symmetric one's pieces;
 // `side`: of its tiles.  The last step's update product makes the call's outputs.
 hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const OrthoMat* mats, const OrthoTiles& tiles,
                                 const OrthoCoef& coef, int step, int steps, const OrthoCall& call, float* pieces,

@@ -250,7 +250,7 @@ struct ProductArgs {
   int32_t from;   // the X^T buffer read
   int32_t first;  // step
   int32_t low;    // the update product writes X's low half
-  float* pieces;  // unfinished sums of the gram product
+  float* pieces;  // unfinished sums of a symmetric product
 };
 
 // LDS holds two slabs of both operands: 64 values of k (FAST), or 32 with both
@@ -652,7 +652,7 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
   };
   fetch(0);
 
-  const bool piece = PRODUCT == kProductGram && t.slot >= 0;  // of a sum that the join pass finishes
+  const bool piece = PRODUCT != kProductUpdate && t.slot >= 0;  // of a sum that the join pass finishes
   const double s = PRODUCT != kProductGram ? *as_global(mt.shift) : piece ? 0.0 : shift_of<S::kThreads>(mt, t, args.first);
   const double keep = args.a + args.b * s + args.c * s * s;
 
@@ -841,9 +841,9 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
   }
 }
 
-// The gram product's tiles whose sums were cut into pieces (few tiles with
-// long sums): the pieces added up in order, then R as from a whole sum.
-template <bool FULL, int BP, int BQ, int WP, int WQ>
+// The tiles of a symmetric product whose sums were cut into pieces: the pieces
+// added up in order, then the results as from a whole sum.
+template <int PRODUCT, bool FULL, int BP, int BQ, int WP, int WQ>
 __global__ __launch_bounds__((ProductShape<FULL, BP, BQ, WP, WQ>::kThreads)) void ortho_join_kernel(
     const OrthoMat* __restrict__ mats, const OrthoTile* __restrict__ tiles, ProductArgs args) {
   constexpr int kThreads = ProductShape<FULL, BP, BQ, WP, WQ>::kThreads;
@@ -863,9 +863,9 @@ __global__ __launch_bounds__((ProductShape<FULL, BP, BQ, WP, WQ>::kThreads)) voi
 #pragma unroll
       for (int j = 0; j < FQ; ++j)
         acc[i][j] += from[static_cast<int64_t>(k) * (BP * BQ / 4) + (i * FQ + j) * kThreads + threadIdx.x];
-  const double s = shift_of<kThreads>(mt, t, args.first);
+  const double s = PRODUCT == kProductGram ? shift_of<kThreads>(mt, t, args.first) : *as_global(mt.shift);
   __shared__ __align__(256) char smem[2 * ProductShape<FULL, BP, BQ, WP, WQ>::kSlab];
-  store_symmetric<kProductGram, FULL, BP, BQ, WP, WQ>(acc, smem, mt, t, args, s, threadIdx.x >> 6, threadIdx.x & 63);
+  store_symmetric<PRODUCT, FULL, BP, BQ, WP, WQ>(acc, smem, mt, t, args, s, threadIdx.x >> 6, threadIdx.x & 63);
 }
 
 template <int PRODUCT, bool FULL, int APPLY, int BP, int BQ, int WP, int WQ>
@@ -876,10 +876,15 @@ hipError_t launch_product(const OrthoMat* mats, const OrthoTiles& tiles, const P
   return hipGetLastError();
 }
 
-template <bool FULL, int BP, int BQ, int WP, int WQ>
-hipError_t launch_join(const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args, hipStream_t stream) {
-  ortho_join_kernel<FULL, BP, BQ, WP, WQ>
-      <<<tiles.count, ProductShape<FULL, BP, BQ, WP, WQ>::kThreads, 0, stream>>>(mats, tiles.tile, args);
+template <int PRODUCT, bool FULL>
+hipError_t launch_join(int side, const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args,
+                       hipStream_t stream) {
+  if (side == 128)
+    ortho_join_kernel<PRODUCT, FULL, 128, 128, 64, 64><<<tiles.count, 256, 0, stream>>>(mats, tiles.tile, args);
+  else if (side == 64)
+    ortho_join_kernel<PRODUCT, FULL, 64, 64, 32, 32><<<tiles.count, 256, 0, stream>>>(mats, tiles.tile, args);
+  else
+    return hipErrorInvalidValue;
   return hipGetLastError();
 }
 
@@ -936,12 +941,13 @@ hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const
 #define EDIT_PRODUCT(P, A)                                                        \
   (full ? launch_product_of<P, true, A>(side, mats, tiles, args, a, r, stream) \
         : launch_product_of<P, false, A>(side, mats, tiles, args, a, r, stream))
+#define EDIT_JOIN(P)                                             \
+  (full ? launch_join<P, true>(side, mats, tiles, args, stream) \
+        : launch_join<P, false>(side, mats, tiles, args, stream))
   switch (product) {
     case kProductGram: return EDIT_PRODUCT(kProductGram, kNoApply);
-    case kProductJoin:
-      if (side != 64) return hipErrorInvalidValue;
-      return full ? launch_join<true, 64, 64, 32, 32>(mats, tiles, args, stream)
-                  : launch_join<false, 64, 64, 32, 32>(mats, tiles, args, stream);
+    case kProductGramJoin: return EDIT_JOIN(kProductGram);
+    case kProductSquareJoin: return EDIT_JOIN(kProductSquare);
     case kProductSquare: return EDIT_PRODUCT(kProductSquare, kNoApply);
     case kProductUpdate:
       if (step < steps - 1) return EDIT_PRODUCT(kProductUpdate, kNoApply);
@@ -954,6 +960,7 @@ hipError_t launch_ortho_product(OrthoProduct product, bool full, int side, const
         case apply_of(kSourceOuter, true): return EDIT_PRODUCT(kProductUpdate, apply_of(kSourceOuter, true));
       }
   }
+#undef EDIT_JOIN
 #undef EDIT_PRODUCT
   return hipErrorInvalidValue;
 }

@@ -9,7 +9,9 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <functional>
 #include <new>
+#include <queue>
 #include <string>
 #include <vector>
 
@@ -56,9 +58,17 @@ constexpr int kXcds = 8;                          // workgroups go to the XCDs i
 // 1B layer's local step (784, the last round nearly empty) 2533 and 2563.
 // FULL's is bound by its operations, and has no registers for them.
 constexpr int kLargeSide = 128, kSmallSide = 64, kHugeSide = 256;
-// A gram tile whose sum is kCutFrom times as long as a CU's share of all of
-// them (and kPieceSlabs slabs at least) is cut into pieces of about that.
-constexpr int64_t kPieceSlabs = 8, kCutFrom = 2;
+// Tiles of the symmetric products that would run on when most CUs are done are
+// cut into pieces of the sum, kPieceSlabs slabs at least, where that is expected
+// to save what a tile or piece by itself costs (kTileSlabs), the join pass
+// (kCutGain) and the pieces' way through memory (cut()).  Whole calls, us
+// without and with: one 4096 x 11008 matrix (528 tiles where 512 run at a time;
+// the last 16 in pieces) 3490 and 3240; one 1024 x 1024 matrix with FULL (136
+// tiles in four pieces each), the gram product cut and both cut: 254 and 242.
+// Cut without regard to the pieces' way, a 1B layer's outer step with FULL took
+// 6728 for 6624.
+constexpr int64_t kPieceSlabs = 10, kTileSlabs = 4, kCutGain = 6;
+int tiles_per_cu(int side) { return side == kLargeSide ? 2 : 4; }  // that run side by side
 int symmetric_side(int64_t large_tiles, int num_cu) { return 2 * large_tiles <= 3 * num_cu ? kSmallSide : kLargeSide; }
 int update_side(int64_t large_tiles, int64_t huge_tiles, int num_cu, bool full) {
   if (large_tiles < num_cu) return kSmallSide;
@@ -76,8 +86,8 @@ struct Tables {
   std::vector<OrthoMat> mats;
   std::vector<OrthoChunk> chunks;
   int matrix_chunks = 0;  // the first ones belong to matrices
-  std::vector<OrthoTile> load, gram, join, square, update;
-  int pieces = 0;
+  std::vector<OrthoTile> load, gram, gram_join, square, square_join, update;
+  int pieces = 0;  // of one product at most
   int gram_side = kLargeSide, update_side = kLargeSide;
   bool small = false;  // one block takes each matrix whole
 };
@@ -95,7 +105,7 @@ struct edit_ortho {
   int matrix_chunks = 0, all_chunks = 0;
   OrthoTile* load = nullptr;
   int load_tiles = 0;
-  OrthoTiles gram{}, join{}, square{}, update{};
+  OrthoTiles gram{}, gram_join{}, square{}, square_join{}, update{};
   float* pieces = nullptr;
   int gram_side = 0, update_side = 0;
   bool small = false;
@@ -183,6 +193,63 @@ std::vector<OrthoTile> spread(const std::vector<std::vector<OrthoTile>>& of_matr
   return out;
 }
 
+// A symmetric product's tiles (whole sums, in `order` of the matrices) for
+// `slots` that run at a time: `tiles` is what to launch, `join` the tiles that
+// are left in pieces.  Each tile goes to the slot that is free first; one that
+// would end behind an even share of all work is cut into pieces that fill what
+// the share leaves.  Returns the number of pieces.
+int cut(const std::vector<std::vector<OrthoTile>>& of_matrix, const std::vector<int>& order, int side,
+        int num_cu, std::vector<OrthoTile>* tiles, std::vector<OrthoTile>* join) {
+  using Ends = std::priority_queue<int64_t, std::vector<int64_t>, std::greater<int64_t>>;
+  int64_t work = 0;
+  for (const auto& l : of_matrix)
+    for (const OrthoTile& t : l) work += t.end + kTileSlabs;
+  const int slots = tiles_per_cu(side) * num_cu;
+  const int64_t share = oceil_div(work, slots);
+  std::vector<std::vector<OrthoTile>> lists = of_matrix, pieces(of_matrix.size());
+  int64_t last_whole = 0, last_cut = 0;
+  int count = 0;
+  Ends whole(std::greater<int64_t>(), std::vector<int64_t>(slots, 0)), parts = whole;
+  auto run = [](Ends& ends, int64_t slabs, int64_t* last) {
+    const int64_t end = ends.top() + slabs + kTileSlabs;
+    ends.pop();
+    ends.push(end);
+    *last = std::max(*last, end);
+  };
+  for (int m : order) {
+    lists[m].clear();
+    for (const OrthoTile& t : of_matrix[m]) {
+      run(whole, t.end, &last_whole);
+      const int64_t room = std::max(kPieceSlabs, share - parts.top() - kTileSlabs);
+      const int32_t n = t.end <= room + kPieceSlabs ? 1 : static_cast<int32_t>(oceil_div(t.end, room));
+      if (n == 1) {
+        run(parts, t.end, &last_cut);
+        lists[m].push_back(t);
+        continue;
+      }
+      join->push_back({t.mat, t.m, t.n, 0, count, count + n});
+      for (int32_t k = 0; k < n; ++k) {
+        const int32_t begin = static_cast<int32_t>(static_cast<int64_t>(t.end) * k / n);
+        const int32_t end = static_cast<int32_t>(static_cast<int64_t>(t.end) * (k + 1) / n);
+        pieces[m].push_back({t.mat, t.m, t.n, count++, begin, end});
+        run(parts, end - begin, &last_cut);
+      }
+    }
+  }
+  if (last_whole - last_cut < kCutGain + count / (side == kLargeSide ? 16 : 64)) {
+    join->clear();
+    *tiles = spread(of_matrix, order);
+    return 0;
+  }
+  std::vector<int> all = order;
+  for (int m : order) {  // a matrix's pieces behind all whole tiles
+    all.push_back(static_cast<int>(lists.size()));
+    lists.push_back(pieces[m]);
+  }
+  *tiles = spread(lists, all);
+  return count;
+}
+
 // [begin, end) in about `most` chunks at most, cut at whole vectors.
 void add_chunks(std::vector<OrthoChunk>& out, int64_t begin, int64_t end, int mat, int most, int* count) {
   constexpr int64_t kUnit = 2048;
@@ -231,19 +298,12 @@ Tables make_tables(const edit_ortho_config_t* cfg, int num_cu) {
   t.gram_side = symmetric_side(symmetric, num_cu);
   t.update_side = update_side(whole, huge, num_cu, full);
   const int slab = ortho_slab(full);
-  int64_t work = 0;  // slabs of all symmetric tiles
-  for (const OrthoMat& m : t.mats) {
-    const int64_t ts = oceil_div(m.r, t.gram_side);
-    work += ts * (ts + 1) / 2 * oceil_div(m.c, slab);
-  }
-  const int64_t piece = std::max<int64_t>(kPieceSlabs, oceil_div(work, 2 * num_cu));
   for (size_t k = 0; k < t.mats.size(); ++k) {
     OrthoMat& m = t.mats[k];
     const int32_t id = static_cast<int32_t>(k);
     // in groups of kGroup x kGroup tiles, which share operands while they run
     const int32_t ts = static_cast<int32_t>(oceil_div(m.r, t.gram_side));
     const int32_t slabs_r = m.ldr / slab, slabs_c = static_cast<int32_t>(oround_up(m.c, kOrthoPad)) / slab;
-    const int32_t pieces = t.gram_side == kSmallSide && slabs_c >= kCutFrom * piece ? static_cast<int32_t>(oceil_div(slabs_c, piece)) : 1;
     gram.emplace_back();
     square.emplace_back();
     for (int32_t p = 0; p < ts; p += kGroup)
@@ -251,13 +311,7 @@ Tables make_tables(const edit_ortho_config_t* cfg, int num_cu) {
         for (int32_t a = p; a < std::min(ts, p + kGroup); ++a)
           for (int32_t b = q; b <= std::min(a, q + kGroup - 1); ++b) {
             square.back().push_back({id, a, b, -1, 0, slabs_r});
-            if (pieces == 1) {
-              gram.back().push_back({id, a, b, -1, 0, slabs_c});
-              continue;
-            }
-            t.join.push_back({id, a, b, 0, t.pieces, t.pieces + pieces});
-            for (int32_t k = 0; k < pieces; ++k)
-              gram.back().push_back({id, a, b, t.pieces++, slabs_c * k / pieces, slabs_c * (k + 1) / pieces});
+            gram.back().push_back({id, a, b, -1, 0, slabs_c});
           }
     const int32_t tr = static_cast<int32_t>(oceil_div(m.r, t.update_side));
     const int32_t tc = static_cast<int32_t>(oceil_div(m.c, t.update_side));
@@ -278,9 +332,9 @@ Tables make_tables(const edit_ortho_config_t* cfg, int num_cu) {
   std::vector<int> order(t.mats.size());
   for (size_t i = 0; i < order.size(); ++i) order[i] = static_cast<int>(i);
   std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return t.mats[a].c > t.mats[b].c; });
-  t.gram = spread(gram, order);
-  t.square = spread(square, order);
+  t.pieces = cut(gram, order, t.gram_side, num_cu, &t.gram, &t.gram_join);
   std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return t.mats[a].r > t.mats[b].r; });
+  t.pieces = std::max(t.pieces, cut(square, order, t.gram_side, num_cu, &t.square, &t.square_join));
   t.update = spread(update, order);
   return t;
 }
@@ -319,11 +373,13 @@ size_t lay_out(edit_ortho* h, Tables& t, char* base) {
   h->load = c.take<OrthoTile>(t.load.size());
   OrthoTile* gram = c.take<OrthoTile>(t.gram.size());
   OrthoTile* update = c.take<OrthoTile>(t.update.size());
-  OrthoTile* join = c.take<OrthoTile>(t.join.size());
+  OrthoTile* gram_join = c.take<OrthoTile>(t.gram_join.size());
   OrthoTile* square = c.take<OrthoTile>(t.square.size());
-  h->pieces = c.take<float>(static_cast<size_t>(t.pieces) * kSmallSide * kSmallSide);
-  h->join = {join, static_cast<int32_t>(t.join.size())};
+  OrthoTile* square_join = c.take<OrthoTile>(t.square_join.size());
+  h->pieces = c.take<float>(static_cast<size_t>(t.pieces) * t.gram_side * t.gram_side);
+  h->gram_join = {gram_join, static_cast<int32_t>(t.gram_join.size())};
   h->square = {square, static_cast<int32_t>(t.square.size())};
+  h->square_join = {square_join, static_cast<int32_t>(t.square_join.size())};
   h->gram = {gram, static_cast<int32_t>(t.gram.size())};
   h->update = {update, static_cast<int32_t>(t.update.size())};
   h->gram_side = t.gram_side, h->update_side = t.update_side;
@@ -384,8 +440,9 @@ edit_status_t enqueue(edit_ortho* h, OrthoCall call, hipStream_t s) {
         e = launch_ortho_product(p, h->full, side, h->mats, tiles, h->coef[k], k, steps, call, h->pieces, s);
     };
     product(kProductGram, h->gram_side, h->gram);
-    product(kProductJoin, h->gram_side, h->join);
+    product(kProductGramJoin, h->gram_side, h->gram_join);
     product(kProductSquare, h->gram_side, h->square);
+    product(kProductSquareJoin, h->gram_side, h->square_join);
     product(kProductUpdate, h->update_side, h->update);
     if (e != hipSuccess) return ofail_hip(e, "product launch");
   }
@@ -459,8 +516,9 @@ edit_status_t edit_ortho_init(const edit_ortho_config_t* cfg, edit_ortho_t* out)
     if (e == hipSuccess) e = upload(h->load, t.load);
     if (e == hipSuccess) e = upload(h->gram.tile, t.gram);
     if (e == hipSuccess) e = upload(h->update.tile, t.update);
-    if (e == hipSuccess) e = upload(h->join.tile, t.join);
+    if (e == hipSuccess) e = upload(h->gram_join.tile, t.gram_join);
     if (e == hipSuccess) e = upload(h->square.tile, t.square);
+    if (e == hipSuccess) e = upload(h->square_join.tile, t.square_join);
     if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e != hipSuccess) {
       (void)hipFree(h->arena);

@@ -70,6 +70,18 @@ def test_matrices_of_many_tiles(shapes, gaps):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_last_tiles_in_pieces(dtype):
+    """A few tiles more than run at a time: the last ones' sums are taken in pieces."""
+    numel, mats = layout([(4001, 4100), (90, 70)], [5, 0])
+    x = _randn(numel, 8).to(TYPES[dtype])
+    with _ortho(numel, mats, dtype) as o:
+        y = o.orthogonalize(x)
+        assert torch.equal(y, o.orthogonalize(x))
+    for spec in mats:
+        assert_o_close(matrix(y, spec), ortho64(matrix(x, spec)), "full" if dtype == "f32" else "fast", f"{dtype} {spec}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_odd_offsets_and_elements_of_no_matrix(dtype):
     """Matrices at odd offsets behind gaps of 1 to 5 elements; what lies between them stays as it was."""
     numel, mats = layout([(33, 47), (64, 64), (5, 130), (130, 70)], gaps=[1, 3, 5, 2], tail=7)
