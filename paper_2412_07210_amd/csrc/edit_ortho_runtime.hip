@@ -250,10 +250,11 @@ int cut(const std::vector<std::vector<OrthoTile>>& of_matrix, const std::vector<
   return count;
 }
 
-// [begin, end) in about `most` chunks at most, cut at whole vectors.
+// [begin, end) in about `most` chunks at most, cut at whole vectors: one a thread
+// at least (four: 272 us for 264 of a 1024 x 1024 matrix's outer step).
 void add_chunks(std::vector<OrthoChunk>& out, int64_t begin, int64_t end, int mat, int most, int* count) {
   constexpr int64_t kUnit = 2048;
-  const int64_t size = std::max(4 * kUnit, oround_up(oceil_div(end - begin, most), kUnit));
+  const int64_t size = std::max(kUnit, oround_up(oceil_div(end - begin, most), kUnit));
   int slot = 0;
   for (int64_t at = begin; at < end;) {
     const int64_t to = std::min(end, at / kUnit * kUnit + size);
