@@ -380,15 +380,16 @@ void edit_group_destroy(edit_group_t h);
  *
  * Precision.  Products run on the fp16 matrix cores with fp32 sums.  X is held
  * to 22 bits as the sum of two fp16 values, and A is taken about its mean
- * diagonal.  EDIT_ORTHO_FAST multiplies the high halves only: O is off by 1e-4
- * to 1e-3 of its norm (an iteration rounded to bf16 is off by 1e-2 to 9e-2).
+ * diagonal.  EDIT_ORTHO_FAST multiplies the high halves only: O is off by 2e-4
+ * to 1.3e-3 of its norm (an iteration rounded to bf16: by 1e-2 to 9e-2).
  * EDIT_ORTHO_FULL takes three products (high*high, high*low, low*high) and is
- * off by as much as an fp32 iteration, at 2.2 to 2.8 times the time.
+ * off by as much as an fp32 iteration, at up to 2.3 times the time.
  * Norms are summed in fp64, steps are taken in fp64 and rounded once.  Results
  * are the same bit for bit on every run.
  *
- * The handle owns its workspace (10 bytes per element and 6 more per element
- * of A, with FULL 12 and 8), made by edit_ortho_init; the calls allocate
+ * The handle owns its workspace (10 bytes per element and 4 more per element
+ * of A, with FULL 12 and 8, short sides rounded up to multiples of 64, and up
+ * to some 50 MB for unfinished sums), made by edit_ortho_init; the calls allocate
  * nothing, do not synchronise and can be captured into HIP graphs.  Calls on
  * one handle, replays of graphs that hold them included, use the same
  * workspace and must not overlap: order them on one stream or with events. */

@@ -24,7 +24,7 @@
 //    near I, and what fp16 rounds off R is small with it; b A + c A^2 would
 //    cancel to a third of its terms.  Only s must be the same in the three
 //    products, so it is computed once per iteration and stored.
-// Error of O against 64 bits: 1e-4 to 1e-3 with FAST over Gaussian, low-rank
+// Error of O against 64 bits: 2e-4 to 1.3e-3 with FAST over Gaussian, low-rank
 // and power-law spectra (1e-3 to 4e-2 if X itself were rounded to fp16, 1e-2
 // to 9e-2 in bf16), and that of a 32-bit iteration with FULL.
 #include <type_traits>
@@ -38,7 +38,9 @@ namespace {
 
 // One chunk per block: the call's update u, its sum of squares, and what the
 // call stores on the way (the momentum; the outer step's u, and the whole
-// step of elements that belong to no matrix).  Bound by memory.
+// step of elements that belong to no matrix).  Bound by memory: a 1B layer's
+// local step in bf16 (10 bytes an element) 94 us, 5.5 TB/s; its outer step of
+// eight fp32 replicas (48 bytes) 527 us, 4.7 TB/s.
 template <int SOURCE, bool BF16>
 __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_source_kernel(OrthoArgs a, RepPtrs reps,
                                                                           const OrthoMat* __restrict__ mats,
@@ -145,7 +147,8 @@ __device__ __forceinline__ T* as_global(T* p) {
 
 // One 64 x 64 tile of a stored matrix per block: X^T = u / ||u|| at kScaleX,
 // through LDS where that transposes.  Eight elements a thread and access, also
-// where matrices begin at odd places (then element by element).
+// where matrices begin at odd places (then element by element).  Bound by memory:
+// a 1B layer's local step in bf16 (10 bytes an element) 106 us, 4.9 TB/s.
 template <int SOURCE, bool BF16, bool FULL>
 __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_load_kernel(OrthoArgs a, const OrthoMat* __restrict__ mats,
                                                                         const OrthoTile* __restrict__ tiles) {
@@ -245,6 +248,19 @@ __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_load_kernel(OrthoAr
 // update product takes it from the operand tiles as they pass through LDS, and
 // the low half of X in its epilogue.  Symmetric products take the tiles with
 // p >= q and store each twice.
+//
+// Of a 1B layer (four matrices of 2048 x 2048, three of 2048 x 5632), by the
+// operations that the symmetric products cannot do without:
+//           FAST                 FULL, three products
+//   gram    130 us,  810 TF/s    315 us, 1000 TF/s
+//   square   80 us,  756 TF/s    194 us,  930 TF/s
+//   update  264 us,  797 TF/s    533 us, 1180 TF/s
+// FULL is bound by the matrix cores (a large library product reaches 1310
+// TF/s).  FAST is bound by what the loads bring to LDS, about 34 bytes a clock
+// and CU: the update product takes 175 us without its loads, 244 without its
+// multiplications; 256 x 256 tiles, which load half as much, reach 1086 TF/s on
+// 4096 x 11008.  The tiles of 64 x 64 are bound by the launch and the loads'
+// latency: one block a CU takes about 5 us, and 0.4 a slab.
 struct ProductArgs {
   double a, b, c;
   int32_t from;   // the X^T buffer read
@@ -842,30 +858,38 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
 }
 
 // The tiles of a symmetric product whose sums were cut into pieces: the pieces
-// added up in order, then the results as from a whole sum.
-template <int PRODUCT, bool FULL, int BP, int BQ, int WP, int WQ>
-__global__ __launch_bounds__((ProductShape<FULL, BP, BQ, WP, WQ>::kThreads)) void ortho_join_kernel(
-    const OrthoMat* __restrict__ mats, const OrthoTile* __restrict__ tiles, ProductArgs args) {
-  constexpr int kThreads = ProductShape<FULL, BP, BQ, WP, WQ>::kThreads;
-  const OrthoTile t = tiles[blockIdx.x];
-  if (t.mat < 0) return;
+// added up in order, then the results as from a whole sum.  A block takes 64 x
+// 64 of a tile, which is what a wave of the product has of a 128 x 128 one (or
+// all of a 64 x 64 one), in 32 x 32 parts.  Bound by the latency of the pieces'
+// loads, hence several at a time: 16 tiles of 128 x 128 in 18 pieces each took
+// 26 us in a block a tile and 10 so; 136 of 64 x 64 in four take 5.4.
+template <int PRODUCT, bool FULL, int SIDE>
+__global__ __launch_bounds__(256) void ortho_join_kernel(const OrthoMat* __restrict__ mats,
+                                                         const OrthoTile* __restrict__ tiles, ProductArgs args) {
+  constexpr int kParts = SIDE / 64, kFrags = SIDE / 32;  // kFrags: 16 x 16 blocks along a wave of the product
+  OrthoTile t = tiles[blockIdx.x / (kParts * kParts)];
+  const int part = blockIdx.x % (kParts * kParts);
+  t.m = t.m * kParts + part % kParts, t.n = t.n * kParts + part / kParts;
+  if (t.m < t.n) return;  // the mirror image of another part
   const OrthoMat mt = mats[t.mat];
-  constexpr int FP = WP / 16, FQ = WQ / 16;
-  f32x4 acc[FP][FQ];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int from_wave = kParts == 1 ? wave : part, i0 = kParts == 1 ? 0 : 2 * (wave & 1), j0 = kParts == 1 ? 0 : 2 * (wave >> 1);
+  f32x4 acc[2][2];
 #pragma unroll
-  for (int i = 0; i < FP; ++i)
+  for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const f32x4* from = reinterpret_cast<const f32x4*>(as_global(args.pieces));
+    for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const f32x4* from = reinterpret_cast<const f32x4*>(as_global(args.pieces)) + from_wave * 64 + lane;
+#pragma unroll 4
   for (int k = t.begin; k < t.end; ++k)
 #pragma unroll
-    for (int i = 0; i < FP; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < FQ; ++j)
-        acc[i][j] += from[static_cast<int64_t>(k) * (BP * BQ / 4) + (i * FQ + j) * kThreads + threadIdx.x];
-  const double s = PRODUCT == kProductGram ? shift_of<kThreads>(mt, t, args.first) : *as_global(mt.shift);
-  __shared__ __align__(256) char smem[2 * ProductShape<FULL, BP, BQ, WP, WQ>::kSlab];
-  store_symmetric<PRODUCT, FULL, BP, BQ, WP, WQ>(acc, smem, mt, t, args, s, threadIdx.x >> 6, threadIdx.x & 63);
+      for (int j = 0; j < 2; ++j)
+        acc[i][j] += from[static_cast<int64_t>(k) * (SIDE * SIDE / 4) + ((i0 + i) * kFrags + j0 + j) * 256];
+  const double s = PRODUCT == kProductGram ? shift_of<256>(mt, t, args.first) : *as_global(mt.shift);
+  __shared__ __align__(256) char smem[2 * ProductShape<FULL, 64, 64, 32, 32>::kSlab];
+  store_symmetric<PRODUCT, FULL, 64, 64, 32, 32>(acc, smem, mt, t, args, s, wave, lane);
 }
 
 template <int PRODUCT, bool FULL, int APPLY, int BP, int BQ, int WP, int WQ>
@@ -880,9 +904,9 @@ template <int PRODUCT, bool FULL>
 hipError_t launch_join(int side, const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args,
                        hipStream_t stream) {
   if (side == 128)
-    ortho_join_kernel<PRODUCT, FULL, 128, 128, 64, 64><<<tiles.count, 256, 0, stream>>>(mats, tiles.tile, args);
+    ortho_join_kernel<PRODUCT, FULL, 128><<<4 * tiles.count, 256, 0, stream>>>(mats, tiles.tile, args);
   else if (side == 64)
-    ortho_join_kernel<PRODUCT, FULL, 64, 64, 32, 32><<<tiles.count, 256, 0, stream>>>(mats, tiles.tile, args);
+    ortho_join_kernel<PRODUCT, FULL, 64><<<tiles.count, 256, 0, stream>>>(mats, tiles.tile, args);
   else
     return hipErrorInvalidValue;
   return hipGetLastError();

@@ -4,13 +4,13 @@
 // A handle owns, for one unit layout, a workspace for every matrix and the
 // tables its launches run over: chunks of the unit for the streaming passes,
 // tiles of all matrices for the products.  A call enqueues source -> load ->
-// steps x (gram, square, update) on the caller's stream, or one launch for
+// steps x (gram, square, update; after a symmetric product the join of what was
+// cut) on the caller's stream, or one launch for
 // small matrices.
 #include <algorithm>
-#include <climits>
 #include <cmath>
 #include <functional>
-#include <new>
+#include <memory>
 #include <queue>
 #include <string>
 #include <vector>
@@ -40,6 +40,7 @@ int64_t oround_up(int64_t a, int64_t b) { return oceil_div(a, b) * b; }
 constexpr double kDefaultCoef[3] = {3.4445, -4.7750, 2.0315};
 constexpr int64_t kMaxSide = int64_t(1) << 24;
 constexpr int64_t kMaxMatrix = int64_t(1) << 29;
+constexpr int kGapChunks = 4096;                  // blocks for a run of elements of no matrix, at most
 constexpr int kXcds = 8;                          // workgroups go to the XCDs in turn
 // Sides of the products' tiles.  A CU runs two 128 x 128 tiles side by side at
 // about the time of one, and 64 x 64 tiles take up to 1.4 times the time per
@@ -327,7 +328,7 @@ Tables make_tables(const edit_ortho_config_t* cfg, int num_cu) {
   int64_t at = 0;
   used.push_back({cfg->numel, cfg->numel});
   for (const auto& [lo, hi] : used) {
-    if (lo > at) add_chunks(t.chunks, at, lo, -1, INT_MAX, nullptr);
+    if (lo > at) add_chunks(t.chunks, at, lo, -1, kGapChunks, nullptr);
     at = hi;
   }
   std::vector<int> order(t.mats.size());
@@ -496,22 +497,18 @@ edit_status_t edit_ortho_init(const edit_ortho_config_t* cfg, edit_ortho_t* out)
     ORTHO_TRY(check_coefficients(coef));
     int dev = 0, num_cu = 0;
     ORTHO_TRY(current_gfx950(&dev, &num_cu));
-    edit_ortho* h = new (std::nothrow) edit_ortho;
-    if (!h) return ofail(EDIT_ENOMEM, "host allocation failed");
+    auto h = std::make_unique<edit_ortho>();
     h->numel = cfg->numel;
     h->bf16 = cfg->dtype == EDIT_BF16;
     h->full = cfg->precision == EDIT_ORTHO_FULL;
     h->device = dev;
     h->coef = coef;
     Tables t = make_tables(cfg, num_cu);
-    const size_t total = std::max<size_t>(lay_out(h, t, nullptr), 256);
+    const size_t total = std::max<size_t>(lay_out(h.get(), t, nullptr), 256);
     hipError_t e = hipMalloc(reinterpret_cast<void**>(&h->arena), total);
-    if (e != hipSuccess) {
-      delete h;
-      return ofail(EDIT_ENOMEM, std::string("hipMalloc of the workspace: ") + hipGetErrorString(e));
-    }
+    if (e != hipSuccess) return ofail(EDIT_ENOMEM, std::string("hipMalloc of the workspace: ") + hipGetErrorString(e));
     e = hipMemset(h->arena, 0, total);  // what pads the matrices stays zero
-    lay_out(h, t, h->arena);
+    lay_out(h.get(), t, h->arena);
     if (e == hipSuccess) e = upload(h->mats, t.mats);
     if (e == hipSuccess) e = upload(h->chunks, t.chunks);
     if (e == hipSuccess) e = upload(h->load, t.load);
@@ -523,10 +520,9 @@ edit_status_t edit_ortho_init(const edit_ortho_config_t* cfg, edit_ortho_t* out)
     if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e != hipSuccess) {
       (void)hipFree(h->arena);
-      delete h;
       return ofail_hip(e, "edit_ortho_init");
     }
-    *out = h;
+    *out = h.release();
     return EDIT_OK;
   } catch (const std::exception&) {  // the tables' host memory
     return ofail(EDIT_ENOMEM, "host allocation failed");
