@@ -762,10 +762,9 @@ class Orthogonalizer:
         given one keeps what it holds there."""
         px = self._arg(x, self._torch_dtype, "x")
         if out is None:
-            out = torch.empty_like(x)
-            if not self._covered:
-                with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
-                    out.zero_()
+            # of the call's stream: memory that another one has just freed may still be in use there
+            with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+                out = torch.empty_like(x) if self._covered else torch.zeros_like(x)
         self._call(self._lib.edit_ortho_apply, "edit_ortho_apply", px, self._arg(out, self._torch_dtype, "out"),
                    _stream_handle(stream, self.device))
         return out

@@ -472,6 +472,82 @@ def test_two_handles_on_two_streams():
     assert all(torch.equal(p, q) for p, q in zip(want, got))
 
 
+def test_many_matrices():
+    """Hundreds of matrices in one unit, some whole in a block and, beside a larger one, none."""
+    shapes = [(1 + k % 13, 1 + (7 * k) % 29) for k in range(700)]
+    for more in ([], [(130, 300)]):
+        numel, mats = layout(shapes + more)
+        x = _randn(numel, 12)
+        with _ortho(numel, mats, "f32") as o:
+            y = o.orthogonalize(x)
+        for spec in mats[::23] + mats[-1:]:
+            assert_o_close(matrix(y, spec), ortho64(matrix(x, spec)), "full", f"{spec}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_longest_side(dtype):
+    """One row, and one column, of 2^24 elements: the workspace's offsets reach 2^31 bytes and, in fp32, nearly 2^32."""
+    for shape in ((1, 2 ** 24), (2 ** 24, 1)):
+        x = _randn(2 ** 24, 13).to(TYPES[dtype])
+        with _ortho(2 ** 24, [(0, *shape)], dtype) as o:
+            y = o.orthogonalize(x)
+        assert_o_close(y.view(shape), ortho64(x.view(shape)), "full" if dtype == "f32" else "fast", f"{dtype} {shape}")
+
+
+def test_matrices_behind_2_to_the_31_elements():
+    at = 2 ** 31 + 5
+    mats = [(3, 70, 90), (at, 90, 300), (at + 90 * 300, 64, 64)]
+    numel = at + 90 * 300 + 64 * 64 + 3
+    x = torch.zeros(numel, dtype=torch.bfloat16, device=DEV)
+    for k, spec in enumerate(mats):
+        matrix(x, spec).copy_(_randn(spec[1] * spec[2], 14 + k).view(spec[1], spec[2]))
+    with _ortho(numel, mats, "bf16") as o:
+        y = x.clone()
+        o.orthogonalize(y, y)
+    for spec in mats:
+        assert_o_close(matrix(y, spec), ortho64(matrix(x, spec)), "fast", f"{spec}")
+        matrix(y, spec).zero_()
+    assert int(y.count_nonzero()) == 0
+
+
+def test_result_on_another_stream():
+    """A new result belongs to the stream of the call, where memory that the
+    current one has just let go, with work pending on it, is not handed out."""
+    numel, mats = layout([(600, 700)])
+    x = _randn(numel, 15).to(torch.bfloat16)
+    side = torch.cuda.Stream(DEV)
+    with _ortho(numel, mats, "bf16") as o:
+        want = o.orthogonalize(x)
+        torch.cuda.synchronize()
+        for _ in range(3):
+            held = torch.full_like(x, 2.0)
+            for _ in range(20):
+                held.mul_(0.5).add_(1.0)  # stays 2
+            kept = held.float()
+            del held
+            got = o.orthogonalize(x, stream=side)
+            torch.cuda.synchronize()
+            assert torch.equal(got, want)
+            assert bool((kept == 2.0).all())
+
+
+def test_outer_step_is_timed_and_empty_units_pass():
+    """Kernel times of a step with matrices, and a unit of no elements."""
+    numel, mats = layout([(300, 400)], tail=9)
+    cfg = OuterConfig(2, [numel, 0], "bf16")
+    theta, b, reps = _outer_inputs(2, "bf16", numel, 70)
+    none = torch.empty(0, device=DEV)
+    with EditOuter(cfg, DEV) as h, _ortho(numel, mats, "f32", scale="rms") as o, _ortho(0, [], "f32") as empty:
+        h.set_profiling(1)
+        h.step_layer_ortho(0, o, theta, b, reps)
+        h.step_layer_ortho(1, empty, none, none.clone(), [none.to(torch.bfloat16) for _ in range(2)])
+        torch.cuda.synchronize()
+        times = h.kernel_times(0)
+        assert h.state_get(0).round == 1 and h.state_get(1).round == 1
+    assert all(torch.equal(r, theta.to(r.dtype)) for r in reps)
+    assert len(times) == 2 and min(times) > 0.0
+
+
 def test_refusals():
     numel, mats = layout([(32, 40)], tail=8)
     x = _randn(numel, 1).to(torch.bfloat16)
