@@ -105,6 +105,7 @@ inline int ortho_slab(bool full) { return full ? 32 : 64; }
 struct OrthoTiles {
   const OrthoTile* tile;  // device
   int32_t count;
+  bool few;  // of 64 x 64 tiles: four slabs in LDS
 };
 
 // Pass over the update: momentum and update of the call, and the chunks' sums of squares.

@@ -260,7 +260,8 @@ __global__ __launch_bounds__(kOrthoStreamThreads) void ortho_load_kernel(OrthoAr
 // and CU: the update product takes 175 us without its loads, 244 without its
 // multiplications; 256 x 256 tiles, which load half as much, reach 1086 TF/s on
 // 4096 x 11008.  The tiles of 64 x 64 are bound by the launch and the loads'
-// latency: one block a CU takes about 5 us, and 0.4 a slab.
+// latency: one block a CU takes about 5 us, and 0.4 a slab with two slabs in
+// LDS (0.2 with four).
 struct ProductArgs {
   double a, b, c;
   int32_t from;   // the X^T buffer read
@@ -269,9 +270,9 @@ struct ProductArgs {
   float* pieces;  // unfinished sums of a symmetric product
 };
 
-// LDS holds two slabs of both operands: 64 values of k (FAST), or 32 with both
+// LDS holds RING slabs of both operands: 64 values of k (FAST), or 32 with both
 // halves (FULL); 128 bytes for each of the operands' rows either way.
-template <bool FULL, int BP, int BQ, int WP, int WQ>
+template <bool FULL, int RING, int BP, int BQ, int WP, int WQ>
 struct ProductShape {
   static constexpr int kSlabK = FULL ? 32 : 64;
   static constexpr int kWaves = (BP / WP) * (BQ / WQ);
@@ -282,7 +283,8 @@ struct ProductShape {
   static constexpr int kLoadsQ = kBytesQ / 1024 / kWaves;
   static_assert(kLoadsP * kWaves * 1024 == kBytesP && kLoadsQ * kWaves * 1024 == kBytesQ, "whole loads");
   static_assert(kOrthoPad % kSlabK == 0, "whole slabs");
-  static_assert(2 * kSlab <= 160 * 1024 - 256, "two slabs, and the sums of block_sum");
+  static constexpr int kLoads = kLoadsP + kLoadsQ;
+  static_assert((RING & (RING - 1)) == 0 && RING * kSlab <= 160 * 1024 - 256, "the slabs, and the sums of block_sum");
   static_assert(!FULL || WP >= WQ, "the order of the reads");
 };
 
@@ -364,13 +366,15 @@ __device__ __forceinline__ half8 read_operand(const char* slab, int side, int pa
   }
 }
 
-// All of the wave's loads into LDS have landed and its reads of LDS are done,
-// for every wave of the block.  The wait is the builtin one, which the compiler
-// counts: with scalar loads outstanding it could only wait for all reads of LDS
-// at each use of one.
+// All of the wave's loads into LDS but the last OUT have landed and its reads of
+// LDS are done, for every wave of the block.  The wait is the builtin one, which
+// the compiler counts: with scalar loads outstanding it could only wait for all
+// reads of LDS at each use of one.
+template <int OUT>
 __device__ __forceinline__ void slab_barrier() {
+  static_assert(OUT < 16, "four bits of the count");
   asm volatile("" : : : "memory");
-  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  __builtin_amdgcn_s_waitcnt(0x0070 + OUT);  // vmcnt(OUT) lgkmcnt(0)
   __builtin_amdgcn_s_barrier();
   asm volatile("" : : : "memory");
 }
@@ -403,7 +407,7 @@ __device__ __forceinline__ void store_symmetric(f32x4 (&acc)[WP / 16][WQ / 16], 
   using L = Layout<FULL>;
   constexpr int FP = WP / 16, FQ = WQ / 16, kWaves = (BP / WP) * (BQ / WQ), kThreads = kWaves * 64;
   constexpr int kPitch = BP + 8;  // halves of a row in LDS: rows begin in different banks
-  static_assert(BQ * kPitch * 2 <= 2 * ProductShape<FULL, BP, BQ, WP, WQ>::kSlab, "LDS");
+  static_assert(BQ * kPitch * 2 <= 2 * ProductShape<FULL, 2, BP, BQ, WP, WQ>::kSlab, "LDS");
   const int r = mt.r, ld = mt.ldr;
   const int wp = (wave % (BP / WP)) * WP, wq = (wave / (BP / WP)) * WQ;
   const int p_tile = t.m * BP, q_tile = t.n * BQ;
@@ -620,21 +624,21 @@ __device__ __forceinline__ void apply_tile(const f32x4 (&acc)[WP / 16][WQ / 16],
 }
 
 // One tile of a product per block.  While one slab is multiplied, the loads of
-// the next are under way.  A wave's operands are read a step ahead of their
+// the RING - 1 next are under way.  A wave's operands are read a step ahead of their
 // use: each register is read anew right after its last use, and the barrier
 // between slabs stands before the last step of a slab, so that the first reads
 // of the next one run under that step's products.
-template <int PRODUCT, bool FULL, int APPLY, int BP, int BQ, int WP, int WQ>
-__global__ __launch_bounds__((ProductShape<FULL, BP, BQ, WP, WQ>::kThreads),
+template <int PRODUCT, bool FULL, int APPLY, int RING, int BP, int BQ, int WP, int WQ>
+__global__ __launch_bounds__((ProductShape<FULL, RING, BP, BQ, WP, WQ>::kThreads),
                              2)  // waves per SIMD that the registers are budgeted for
 void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __restrict__ tiles, ProductArgs args,
                           OrthoArgs call, RepPtrs reps) {
   constexpr bool LAST = APPLY != kNoApply;
-  using S = ProductShape<FULL, BP, BQ, WP, WQ>;
+  using S = ProductShape<FULL, RING, BP, BQ, WP, WQ>;
   constexpr Reading kReadP = PRODUCT == kProductGram ? kAcross : PRODUCT == kProductUpdate ? kBlocks : kAlong;
   constexpr Reading kReadQ = PRODUCT == kProductGram ? kAcross : kAlong;
   using L = Layout<FULL>;
-  __shared__ __align__(256) char smem[2 * S::kSlab];
+  __shared__ __align__(256) char smem[RING * S::kSlab];
   const OrthoTile t = tiles[blockIdx.x];
   if (t.mat < 0) return;
   const OrthoMat mt = mats[t.mat];
@@ -656,7 +660,7 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
   p += t.begin * step, q += t.begin * step;
   // Slab n, or of its loads those with number part mod parts.
   auto fetch = [&](int n, int part = 0, int parts = 1) {
-    const uint32_t at = lds0 + (n & 1) * S::kSlab;
+    const uint32_t at = lds0 + (n & (RING - 1)) * S::kSlab;
     const _Float16* from_p = p + n * step;
     const _Float16* from_q = q + n * step;
 #pragma unroll
@@ -666,7 +670,8 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
     for (int i = 0; i < S::kLoadsQ; ++i)
       if (i % parts == part) load_to_lds(at + S::kBytesP + (wave + i * S::kWaves) * 1024, from_q, off_q[i]);
   };
-  fetch(0);
+  for (int n = 0; n < RING - 1; ++n)
+    if (n < slabs) fetch(n);
 
   const bool piece = PRODUCT != kProductUpdate && t.slot >= 0;  // of a sum that the join pass finishes
   const double s = PRODUCT != kProductGram ? *as_global(mt.shift) : piece ? 0.0 : shift_of<S::kThreads>(mt, t, args.first);
@@ -703,7 +708,7 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
   constexpr bool kLowFirst = FP * FQ <= 16;
   if constexpr (kLowFirst) read_low();
 
-  auto slab = [&](int n) { return smem + (n & 1) * S::kSlab; };
+  auto slab = [&](int n) { return smem + (n & (RING - 1)) * S::kSlab; };
   auto read_p = [&](const char* at, int part, int i) {
     return read_operand<kReadP, FULL, BP>(at, wp + (kReadP == kBlocks ? 16 * (i & ~1) + 4 * (i & 1) : 16 * i), part, lane);
   };
@@ -713,14 +718,23 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
   auto mul = [&](const half8& x, const half8& y, f32x4& to) {
     to = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, to, 0, 0, 0);
   };
-  // Slab n + 1 has landed, and slab n is read: slab n + 2 takes its place.
+  // Slab n has landed.  Of the loads, which land in order, those of the RING - 2
+  // slabs behind it may be out, where there are as many; others than of slabs
+  // are older or make the wait longer.
+  auto landed = [&](int n) {
+    if (RING > 2 && n + RING - 2 < slabs)
+      slab_barrier<(RING - 2) * S::kLoads>();
+    else
+      slab_barrier<0>();
+  };
+  // Slab n + 1 has landed, and slab n is read: slab n + RING takes its place.
   auto next_slab = [&](int n) {
-    slab_barrier();
-    if (n + 2 < slabs) fetch(n + 2);
+    landed(n + 1);
+    if (n + RING < slabs) fetch(n + RING);
   };
 
-  slab_barrier();
-  if (slabs > 1) fetch(1);
+  landed(0);
+  if (RING - 1 < slabs) fetch(RING - 1);
   if constexpr (!FULL) {
     half8 pf[FP], qf[2][FQ];
 #pragma unroll
@@ -888,15 +902,15 @@ __global__ __launch_bounds__(256) void ortho_join_kernel(const OrthoMat* __restr
       for (int j = 0; j < 2; ++j)
         acc[i][j] += from[static_cast<int64_t>(k) * (SIDE * SIDE / 4) + ((i0 + i) * kFrags + j0 + j) * 256];
   const double s = PRODUCT == kProductGram ? shift_of<256>(mt, t, args.first) : *as_global(mt.shift);
-  __shared__ __align__(256) char smem[2 * ProductShape<FULL, 64, 64, 32, 32>::kSlab];
+  __shared__ __align__(256) char smem[2 * ProductShape<FULL, 2, 64, 64, 32, 32>::kSlab];
   store_symmetric<PRODUCT, FULL, 64, 64, 32, 32>(acc, smem, mt, t, args, s, wave, lane);
 }
 
-template <int PRODUCT, bool FULL, int APPLY, int BP, int BQ, int WP, int WQ>
+template <int PRODUCT, bool FULL, int APPLY, int RING, int BP, int BQ, int WP, int WQ>
 hipError_t launch_product(const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args, const OrthoArgs& call,
                           const RepPtrs& reps, hipStream_t stream) {
-  ortho_product_kernel<PRODUCT, FULL, APPLY, BP, BQ, WP, WQ>
-      <<<tiles.count, ProductShape<FULL, BP, BQ, WP, WQ>::kThreads, 0, stream>>>(mats, tiles.tile, args, call, reps);
+  ortho_product_kernel<PRODUCT, FULL, APPLY, RING, BP, BQ, WP, WQ>
+      <<<tiles.count, ProductShape<FULL, RING, BP, BQ, WP, WQ>::kThreads, 0, stream>>>(mats, tiles.tile, args, call, reps);
   return hipGetLastError();
 }
 
@@ -916,9 +930,11 @@ template <int PRODUCT, bool FULL, int APPLY = kNoApply>
 hipError_t launch_product_of(int side, const OrthoMat* mats, const OrthoTiles& tiles, const ProductArgs& args,
                              const OrthoArgs& call, const RepPtrs& reps, hipStream_t stream) {
   if constexpr (PRODUCT == kProductUpdate && !FULL)
-    if (side == 256) return launch_product<PRODUCT, FULL, APPLY, 256, 256, 128, 64>(mats, tiles, args, call, reps, stream);
-  if (side == 128) return launch_product<PRODUCT, FULL, APPLY, 128, 128, 64, 64>(mats, tiles, args, call, reps, stream);
-  if (side == 64) return launch_product<PRODUCT, FULL, APPLY, 64, 64, 32, 32>(mats, tiles, args, call, reps, stream);
+    if (side == 256) return launch_product<PRODUCT, FULL, APPLY, 2, 256, 256, 128, 64>(mats, tiles, args, call, reps, stream);
+  if (side == 128) return launch_product<PRODUCT, FULL, APPLY, 2, 128, 128, 64, 64>(mats, tiles, args, call, reps, stream);
+  if (side == 64 && tiles.few)
+    return launch_product<PRODUCT, FULL, APPLY, 4, 64, 64, 32, 32>(mats, tiles, args, call, reps, stream);
+  if (side == 64) return launch_product<PRODUCT, FULL, APPLY, 2, 64, 64, 32, 32>(mats, tiles, args, call, reps, stream);
   return hipErrorInvalidValue;
 }
 

@@ -64,12 +64,18 @@ constexpr int kLargeSide = 128, kSmallSide = 64, kHugeSide = 256;
 // to save what a tile or piece by itself costs (kTileSlabs), the join pass
 // (kCutGain) and the pieces' way through memory (cut()).  Whole calls, us
 // without and with: one 4096 x 11008 matrix (528 tiles where 512 run at a time;
-// the last 16 in pieces) 3490 and 3240; one 1024 x 1024 matrix with FULL (136
-// tiles in four pieces each), the gram product cut and both cut: 254 and 242.
-// Cut without regard to the pieces' way, a 1B layer's outer step with FULL took
-// 6728 for 6624.
-constexpr int64_t kPieceSlabs = 10, kTileSlabs = 4, kCutGain = 6;
+// the last 16 in pieces) 3490 and 3240.  Where it does not save that: one 1024 x
+// 1024 matrix with FULL (136 tiles of 32 slabs where 1024 run at a time) 197
+// whole and 214 in four pieces each; a 1B layer's outer step with FULL, the gram
+// product's last 232 of 952 cut, 6624 and 6728.
+constexpr int64_t kPieceSlabs = 10, kTileSlabs = 4, kCutGain = 20;
 int tiles_per_cu(int side) { return side == kLargeSide ? 2 : 4; }  // that run side by side
+// 64 x 64 tiles take four slabs in LDS instead of two where the blocks that
+// then fit, two a CU, are all there are.  Whole calls, us with two and four: one
+// 1024 x 1024 matrix, FULL (256 tiles) 238 and 208; a layer of hidden size 256
+// (88 and 208) 106.5 and 99.2.  With more tiles: 208 and 234 where that matrix's
+// gram product has 544; a 350M layer (952) 501 and 523.
+int few_tiles(int num_cu) { return 2 * num_cu; }
 int symmetric_side(int64_t large_tiles, int num_cu) { return 2 * large_tiles <= 3 * num_cu ? kSmallSide : kLargeSide; }
 int update_side(int64_t large_tiles, int64_t huge_tiles, int num_cu, bool full) {
   if (large_tiles < num_cu) return kSmallSide;
@@ -353,7 +359,10 @@ struct Carver {
   }
 };
 
-size_t lay_out(edit_ortho* h, Tables& t, char* base) {
+size_t lay_out(edit_ortho* h, Tables& t, char* base, int num_cu) {
+  auto tiles = [&](const OrthoTile* at, const std::vector<OrthoTile>& list) {
+    return OrthoTiles{at, static_cast<int32_t>(list.size()), static_cast<int>(list.size()) <= few_tiles(num_cu)};
+  };
   Carver c{base};
   for (OrthoMat& m : t.mats) {
     const size_t xt = static_cast<size_t>(oround_up(m.c, kOrthoPad)) * m.ldr, a = static_cast<size_t>(m.r) * m.ldr;
@@ -379,11 +388,11 @@ size_t lay_out(edit_ortho* h, Tables& t, char* base) {
   OrthoTile* square = c.take<OrthoTile>(t.square.size());
   OrthoTile* square_join = c.take<OrthoTile>(t.square_join.size());
   h->pieces = c.take<float>(static_cast<size_t>(t.pieces) * t.gram_side * t.gram_side);
-  h->gram_join = {gram_join, static_cast<int32_t>(t.gram_join.size())};
-  h->square = {square, static_cast<int32_t>(t.square.size())};
-  h->square_join = {square_join, static_cast<int32_t>(t.square_join.size())};
-  h->gram = {gram, static_cast<int32_t>(t.gram.size())};
-  h->update = {update, static_cast<int32_t>(t.update.size())};
+  h->gram_join = tiles(gram_join, t.gram_join);
+  h->square = tiles(square, t.square);
+  h->square_join = tiles(square_join, t.square_join);
+  h->gram = tiles(gram, t.gram);
+  h->update = tiles(update, t.update);
   h->gram_side = t.gram_side, h->update_side = t.update_side;
   h->small = t.small;
   h->matrices = static_cast<int>(t.mats.size());
@@ -504,11 +513,11 @@ edit_status_t edit_ortho_init(const edit_ortho_config_t* cfg, edit_ortho_t* out)
     h->device = dev;
     h->coef = coef;
     Tables t = make_tables(cfg, num_cu);
-    const size_t total = std::max<size_t>(lay_out(h.get(), t, nullptr), 256);
+    const size_t total = std::max<size_t>(lay_out(h.get(), t, nullptr, num_cu), 256);
     hipError_t e = hipMalloc(reinterpret_cast<void**>(&h->arena), total);
     if (e != hipSuccess) return ofail(EDIT_ENOMEM, std::string("hipMalloc of the workspace: ") + hipGetErrorString(e));
     e = hipMemset(h->arena, 0, total);  // what pads the matrices stays zero
-    lay_out(h.get(), t, h->arena);
+    lay_out(h.get(), t, h->arena, num_cu);
     if (e == hipSuccess) e = upload(h->mats, t.mats);
     if (e == hipSuccess) e = upload(h->chunks, t.chunks);
     if (e == hipSuccess) e = upload(h->load, t.load);

@@ -70,9 +70,10 @@ def test_matrices_of_many_tiles(shapes, gaps):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_last_tiles_in_pieces(dtype):
-    """A few tiles more than run at a time: the last ones' sums are taken in pieces."""
-    numel, mats = layout([(4001, 4100), (90, 70)], [5, 0])
+@pytest.mark.parametrize("shape", [(4001, 4100), (2900, 2850)])
+def test_last_tiles_in_pieces(shape, dtype):
+    """A few tiles more than run at a time (528 of 128, 1035 of 64): the last ones' sums are taken in pieces."""
+    numel, mats = layout([shape, (90, 70)], [5, 0])
     x = _randn(numel, 8).to(TYPES[dtype])
     with _ortho(numel, mats, dtype) as o:
         y = o.orthogonalize(x)
