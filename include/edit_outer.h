@@ -447,7 +447,9 @@ edit_status_t edit_ortho_local_step(edit_ortho_t h, void *param, const void *gra
  * and every replica set to theta'.  O has no magnitude of its own, so beta
  * acts through the momentum only, and nu is the step's size.  `ortho`'s numel
  * must be the unit's and its device the handle's; its dtype does not matter
- * here.  Not available with EDIT_ONE_PASS.  Otherwise arguments, ownership
+ * here, its precision does: theta is fp32, and FULL is what keeps it as exact
+ * as the plain step does (the Python binding takes FULL here unless FAST was
+ * named).  Not available with EDIT_ONE_PASS.  Otherwise arguments, ownership
  * and errors as in edit_outer_step_layer. */
 edit_status_t edit_outer_step_layer_ortho(edit_outer_t h, int32_t layer, edit_ortho_t ortho, float *theta,
                                           float *momentum, void *const *replicas, void *stream);

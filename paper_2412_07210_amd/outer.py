@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
-from dataclasses import dataclass
+from dataclasses import dataclass, replace
 from typing import List, Optional, Sequence, Union
 
 import numpy as np
@@ -395,12 +395,13 @@ class EditOuter:
                          replicas: Sequence[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> None:
         """Enqueue one outer step of unit `layer` whose matrices, as `ortho`
         names them, move along their orthogonalised Nesterov direction
-        (edit_outer_step_layer_ortho); in place on all tensors."""
+        (edit_outer_step_layer_ortho); in place on all tensors.  O is taken
+        with FULL, unless `ortho` was made with precision="fast"."""
         if not isinstance(ortho, Orthogonalizer):
             raise TypeError("ortho must be an Orthogonalizer")
         ptrs = self._unit_tensors(layer, theta, momentum, replicas)
-        _check(self._call(self._lib.edit_outer_step_layer_ortho, int(layer), ortho._h, theta.data_ptr(),
-                          momentum.data_ptr(), ptrs, _stream_handle(stream, self.device)),
+        _check(self._call(self._lib.edit_outer_step_layer_ortho, int(layer), ortho._outer_handle(stream),
+                          theta.data_ptr(), momentum.data_ptr(), ptrs, _stream_handle(stream, self.device)),
                "edit_outer_step_layer_ortho")
 
     def prepare_round(self, units: Sequence[tuple], layers: Optional[Sequence[int]] = None,
@@ -654,7 +655,9 @@ class OrthoConfig:
     steps: int = 5                              # Newton-Schulz steps
     # (a, b, c) for all steps or one triple per step; None: 3.4445, -4.7750, 2.0315
     coefficients: Optional[Sequence] = None
-    precision: Optional[str] = None             # "fast" or "full"; None: "fast" for bf16, "full" for f32
+    # "fast" or "full".  None: "fast" for bf16 and "full" for f32, and "full" in
+    # the outer step, whose theta is fp32 whatever the dtype here
+    precision: Optional[str] = None
 
     def scales(self) -> List[float]:
         if self.scale == "spectral":
@@ -671,10 +674,16 @@ class OrthoConfig:
 class Orthogonalizer:
     """Orthogonalised updates of the matrices of one sync unit layout
     (edit_ortho_* of the C ABI).  Calls share the handle's workspace: order
-    them on one stream or with events."""
+    them on one stream or with events.
+
+    A bf16 handle that no precision was named for steps a replica with "fast"
+    and theta, which is fp32, with "full".  The first outer step with it makes
+    that workspace, beside the worker's: it allocates, waits for the device
+    and cannot be captured into a HIP graph; the later ones can."""
 
     def __init__(self, cfg: OrthoConfig, device: Optional[torch.device] = None):
         self._h = None
+        self._outer_h = None
         self.cfg = cfg
         device = torch.device("cuda") if device is None else torch.device(device)
         if device.type != "cuda":
@@ -687,11 +696,29 @@ class Orthogonalizer:
         self._torch_dtype = torch.bfloat16 if cfg.dtype == "bf16" else torch.float32
         self._covered = sum(int(r) * int(k) for _, r, k in cfg.matrices) == self._numel
         self._lib = load_library()
+        self._h = self._init(c)
+        del keep  # the arrays that the configuration points to
+        # the outer step's configuration and its arrays, where it takes another precision
+        by_default = cfg.precision is None and c.precision != ORTHO_FULL
+        self._outer_c = self._c_config(replace(cfg, precision="full")) if by_default else None
+
+    def _init(self, c: _OrthoConfig) -> ctypes.c_void_p:
         h = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             _check(self._lib.edit_ortho_init(ctypes.byref(c), ctypes.byref(h)), "edit_ortho_init")
-        del keep  # the arrays that the configuration points to
-        self._h = h
+        return h
+
+    def _outer_handle(self, stream: Optional[torch.cuda.Stream]) -> Optional[ctypes.c_void_p]:
+        """The C handle that steps theta."""
+        if self._outer_c is None or self._h is None:
+            return self._h
+        if self._outer_h is None:
+            with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+                if torch.cuda.is_current_stream_capturing():
+                    raise EditOuterError(EDIT_ESTATE, "the first outer step with a handle of default precision makes a "
+                                                      "workspace: take one before the capture, or name a precision")
+            self._outer_h = self._init(self._outer_c[0])
+        return self._outer_h
 
     @staticmethod
     def _c_config(cfg: OrthoConfig):
@@ -723,10 +750,12 @@ class Orthogonalizer:
         return c, (mats, coef)
 
     def close(self) -> None:
-        if getattr(self, "_h", None) is not None and self._h.value:
-            with torch.cuda.device(self.device):
-                self._lib.edit_ortho_destroy(self._h)
-            self._h = None
+        for name in ("_h", "_outer_h"):
+            h = getattr(self, name, None)
+            if h is not None and h.value:
+                with torch.cuda.device(self.device):
+                    self._lib.edit_ortho_destroy(h)
+                setattr(self, name, None)
 
     def __del__(self):
         try:
