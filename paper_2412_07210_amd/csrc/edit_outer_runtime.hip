@@ -36,6 +36,9 @@ namespace {
 thread_local std::string g_last_error;
 
 edit_status_t fail(edit_status_t s, const std::string& msg) {
+  // The runtime keeps a call's error until somebody asks for it; a later launch
+  // that asks for its own (here or in the caller's program) would take it for that.
+  if (s == EDIT_EHIP || s == EDIT_ENOMEM) (void)hipGetLastError();
   g_last_error = msg;
   return s;
 }

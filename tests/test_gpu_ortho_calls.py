@@ -1,11 +1,11 @@
 """Calls of the orthogonalised updates that the documentation allows, beside
 those of test_gpu_ortho.py (GPU): handles of default precision in the outer
-step."""
+step, and calls after a failed one."""
 import pytest
 import torch
 
 from ortho_reference import layout
-from paper_2412_07210_amd import EditOuter, EditOuterError, OrthoConfig, Orthogonalizer, OuterConfig
+from paper_2412_07210_amd import ONE_PASS, EditOuter, EditOuterError, OrthoConfig, Orthogonalizer, OuterConfig
 
 pytestmark = pytest.mark.gpu
 
@@ -100,3 +100,17 @@ def test_default_handle_in_a_graph():
             graph.replay()
             torch.cuda.synchronize()
             assert all(torch.equal(x, y) for x, y in zip(fixed, eager)), f"replay {replay}"
+
+
+def test_calls_after_a_failed_init():
+    """A workspace that does not fit is refused, and that is all: later calls are as before."""
+    numel, mats = layout(SHAPES[1])
+    x = _randn(numel, 31).to(torch.bfloat16)
+    with _ortho(numel, mats) as o:
+        want = o.orthogonalize(x)
+        for make in (lambda: _ortho(2 ** 42, mats),  # 16 TiB
+                     lambda: EditOuter(OuterConfig(2, [2 ** 38] * 4000, "bf16", flags=ONE_PASS), DEV)):
+            with pytest.raises(EditOuterError, match="out of memory"):
+                make()
+            assert torch.equal(o.orthogonalize(x), want)
+            assert float(torch.ones(8, device=DEV).sum()) == 8.0
