@@ -63,6 +63,36 @@ def test_updates_that_lack_directions(kernels, rank):
         assert off <= bound + half_step(torch.float32), f"{precision} {kernels}: {off:.3g}, bound {bound:.3g}"
 
 
+def _documented(precision, r, whole):
+    """What the header says that O is off by at most, of its norm."""
+    if precision == "full":
+        return 6e-6 if whole else 2.5e-4
+    if r < 64:
+        return 0.25 / r
+    return 1.3e-3 if whole else 5e-3
+
+
+@pytest.mark.parametrize("precision", ["fast", "full"])
+@pytest.mark.parametrize("shape", [(2, 2), (4, 4), (8, 8), (8, 3000), (16, 16), (200, 16), (32, 32), (64, 64), (64, 300),
+                                   (128, 128), (512, 512), (700, 1024), (1024, 1024)], ids=lambda s: "%dx%d" % s)
+def test_documented_errors(shape, precision):
+    r = min(shape)
+    for seed in range(3):
+        for rank in (1, 2, 4, 16, r):
+            if rank > r:
+                continue
+            u = _of_rank(rank, *shape, seed) if rank < r else _randn(*shape, seed)
+            ref, _ = reference_and_bound(u, precision)
+            off = _error(_orthogonalize(shape, u, precision), ref)
+            assert off <= _documented(precision, r, rank == r), f"{precision} {shape} rank {rank} seed {seed}: {off:.3g}"
+    if precision == "fast":
+        one = torch.zeros(shape, device=DEV)
+        one[shape[0] // 2, shape[1] // 3] = -3.0
+        for u in (torch.ones(shape, device=DEV), one):  # elements that round alike
+            ref, _ = reference_and_bound(u, precision)
+            assert _error(_orthogonalize(shape, u, precision), ref) <= 2.5e-2
+
+
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 6, 8])
 @pytest.mark.parametrize("shape", [(128, 128), (200, 170), (900, 3900), (2100, 2120), (500, 29201)], ids=lambda s: "%dx%d" % s)
 def test_fast_at_other_step_counts(shape, steps):
