@@ -395,11 +395,12 @@ void edit_group_destroy(edit_group_t h);
  * are the same bit for bit on every run.
  *
  * The handle owns its workspace (10 bytes per element and 4 more per element
- * of A, with FULL 12 and 8, short sides rounded up to multiples of 64, and up
- * to some 50 MB for unfinished sums), made by edit_ortho_init; the calls allocate
- * nothing, do not synchronise and can be captured into HIP graphs.  Calls on
- * one handle, replays of graphs that hold them included, use the same
- * workspace and must not overlap: order them on one stream or with events. */
+ * of A, with FULL 12 and 8, short sides rounded up to multiples of 64; 4 of the
+ * bytes per element serve the outer step only; and up to 192 MiB for unfinished
+ * sums), made by edit_ortho_init; the calls allocate nothing, do not
+ * synchronise and can be captured into HIP graphs.  Calls on one handle,
+ * replays of graphs that hold them included, use the same workspace and must
+ * not overlap: order them on one stream or with events. */
 #define EDIT_ORTHO_MAX_STEPS 32
 
 typedef enum { EDIT_ORTHO_FAST = 0, EDIT_ORTHO_FULL = 1 } edit_ortho_precision_t;

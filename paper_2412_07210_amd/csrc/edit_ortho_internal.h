@@ -8,6 +8,7 @@
 
 #include "edit_outer.h"
 #include "edit_outer_internal.h"
+#include "ortho_tiles.h"
 
 namespace edit {
 
@@ -66,13 +67,6 @@ struct OrthoMat {
 struct OrthoChunk {
   int64_t begin, end;
   int32_t mat, slot;
-};
-
-// Tile (m, n) of a matrix: of its rows and columns (load), of C's p and q (products); mat = -1: none.
-struct OrthoTile {
-  int32_t mat, m, n;
-  int32_t slot;        // update: of x_part;  gram, square: of `pieces` (-1: a whole sum)
-  int32_t begin, end;  // products: slabs of the sum;  join: pieces
 };
 
 // What the update of a call is made from.

@@ -9,9 +9,7 @@
 // small matrices.
 #include <algorithm>
 #include <cmath>
-#include <functional>
 #include <memory>
-#include <queue>
 #include <string>
 #include <vector>
 
@@ -41,7 +39,6 @@ constexpr double kDefaultCoef[3] = {3.4445, -4.7750, 2.0315};
 constexpr int64_t kMaxSide = int64_t(1) << 24;
 constexpr int64_t kMaxMatrix = int64_t(1) << 29;
 constexpr int kGapChunks = 4096;                  // blocks for a run of elements of no matrix, at most
-constexpr int kXcds = 8;                          // workgroups go to the XCDs in turn
 // Sides of the products' tiles.  A CU runs two 128 x 128 tiles side by side at
 // about the time of one, and 64 x 64 tiles take up to 1.4 times the time per
 // operation but fill the GPU with a quarter of the work.  us at 128 and 64, n
@@ -58,18 +55,7 @@ constexpr int kXcds = 8;                          // workgroups go to the XCDs i
 // and 120.  Whole calls: one 4096 x 11008 matrix (688 tiles) 3830 and 3670, a
 // 1B layer's local step (784, the last round nearly empty) 2533 and 2563.
 // FULL's is bound by its operations, and has no registers for them.
-constexpr int kLargeSide = 128, kSmallSide = 64, kHugeSide = 256;
-// Tiles of the symmetric products that would run on when most CUs are done are
-// cut into pieces of the sum, kPieceSlabs slabs at least, where that is expected
-// to save what a tile or piece by itself costs (kTileSlabs), the join pass
-// (kCutGain) and the pieces' way through memory (cut()).  Whole calls, us
-// without and with: one 4096 x 11008 matrix (528 tiles where 512 run at a time;
-// the last 16 in pieces) 3490 and 3240.  Where it does not save that: one 1024 x
-// 1024 matrix with FULL (136 tiles of 32 slabs where 1024 run at a time) 197
-// whole and 214 in four pieces each; a 1B layer's outer step with FULL, the gram
-// product's last 232 of 952 cut, 6624 and 6728.
-constexpr int64_t kPieceSlabs = 10, kTileSlabs = 4, kCutGain = 20;
-int tiles_per_cu(int side) { return side == kLargeSide ? 2 : 4; }  // that run side by side
+constexpr int kLargeSide = kOrthoLargeSide, kSmallSide = 64, kHugeSide = 256;
 // 64 x 64 tiles take four slabs in LDS instead of two where the blocks that
 // then fit, two a CU, are all there are.  Whole calls, us with two and four: one
 // 1024 x 1024 matrix, FULL (256 tiles) 238 and 208; a layer of hidden size 256
@@ -176,87 +162,6 @@ edit_status_t check_layout(const edit_ortho_config_t* cfg) {
   return EDIT_OK;
 }
 
-// The tiles of all matrices, so that the workgroups of an XCD (every eighth)
-// take neighbouring ones of a matrix, whose operands they share in its L2;
-// matrices with the longest sums first, so that short ones fill the end.
-std::vector<OrthoTile> spread(const std::vector<std::vector<OrthoTile>>& of_matrix, const std::vector<int>& order) {
-  std::vector<OrthoTile> list[kXcds];
-  int turn = 0;  // matrices of few tiles start on different XCDs
-  for (int m : order) {
-    const std::vector<OrthoTile>& t = of_matrix[m];
-    const size_t n = t.size();
-    for (int x = 0; x < kXcds; ++x) {
-      std::vector<OrthoTile>& to = list[(x + turn) % kXcds];
-      to.insert(to.end(), t.begin() + n * x / kXcds, t.begin() + n * (x + 1) / kXcds);
-    }
-    turn = (turn + static_cast<int>(n % kXcds)) % kXcds;
-  }
-  size_t longest = 0;
-  for (const auto& l : list) longest = std::max(longest, l.size());
-  std::vector<OrthoTile> out;
-  for (size_t i = 0; i < longest; ++i)
-    for (const auto& l : list) out.push_back(i < l.size() ? l[i] : OrthoTile{-1, 0, 0, 0, 0, 0});
-  while (!out.empty() && out.back().mat < 0) out.pop_back();
-  return out;
-}
-
-// A symmetric product's tiles (whole sums, in `order` of the matrices) for
-// `slots` that run at a time: `tiles` is what to launch, `join` the tiles that
-// are left in pieces.  Each tile goes to the slot that is free first; one that
-// would end behind an even share of all work is cut into pieces that fill what
-// the share leaves.  Returns the number of pieces.
-int cut(const std::vector<std::vector<OrthoTile>>& of_matrix, const std::vector<int>& order, int side,
-        int num_cu, std::vector<OrthoTile>* tiles, std::vector<OrthoTile>* join) {
-  using Ends = std::priority_queue<int64_t, std::vector<int64_t>, std::greater<int64_t>>;
-  int64_t work = 0;
-  for (const auto& l : of_matrix)
-    for (const OrthoTile& t : l) work += t.end + kTileSlabs;
-  const int slots = tiles_per_cu(side) * num_cu;
-  const int64_t share = oceil_div(work, slots);
-  std::vector<std::vector<OrthoTile>> lists = of_matrix, pieces(of_matrix.size());
-  int64_t last_whole = 0, last_cut = 0;
-  int count = 0;
-  Ends whole(std::greater<int64_t>(), std::vector<int64_t>(slots, 0)), parts = whole;
-  auto run = [](Ends& ends, int64_t slabs, int64_t* last) {
-    const int64_t end = ends.top() + slabs + kTileSlabs;
-    ends.pop();
-    ends.push(end);
-    *last = std::max(*last, end);
-  };
-  for (int m : order) {
-    lists[m].clear();
-    for (const OrthoTile& t : of_matrix[m]) {
-      run(whole, t.end, &last_whole);
-      const int64_t room = std::max(kPieceSlabs, share - parts.top() - kTileSlabs);
-      const int32_t n = t.end <= room + kPieceSlabs ? 1 : static_cast<int32_t>(oceil_div(t.end, room));
-      if (n == 1) {
-        run(parts, t.end, &last_cut);
-        lists[m].push_back(t);
-        continue;
-      }
-      join->push_back({t.mat, t.m, t.n, 0, count, count + n});
-      for (int32_t k = 0; k < n; ++k) {
-        const int32_t begin = static_cast<int32_t>(static_cast<int64_t>(t.end) * k / n);
-        const int32_t end = static_cast<int32_t>(static_cast<int64_t>(t.end) * (k + 1) / n);
-        pieces[m].push_back({t.mat, t.m, t.n, count++, begin, end});
-        run(parts, end - begin, &last_cut);
-      }
-    }
-  }
-  if (last_whole - last_cut < kCutGain + count / (side == kLargeSide ? 16 : 64)) {
-    join->clear();
-    *tiles = spread(of_matrix, order);
-    return 0;
-  }
-  std::vector<int> all = order;
-  for (int m : order) {  // a matrix's pieces behind all whole tiles
-    all.push_back(static_cast<int>(lists.size()));
-    lists.push_back(pieces[m]);
-  }
-  *tiles = spread(lists, all);
-  return count;
-}
-
 // [begin, end) in about `most` chunks at most, cut at whole vectors: one a thread
 // at least (four: 272 us for 264 of a 1024 x 1024 matrix's outer step).
 void add_chunks(std::vector<OrthoChunk>& out, int64_t begin, int64_t end, int mat, int most, int* count) {
@@ -340,10 +245,10 @@ Tables make_tables(const edit_ortho_config_t* cfg, int num_cu) {
   std::vector<int> order(t.mats.size());
   for (size_t i = 0; i < order.size(); ++i) order[i] = static_cast<int>(i);
   std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return t.mats[a].c > t.mats[b].c; });
-  t.pieces = cut(gram, order, t.gram_side, num_cu, &t.gram, &t.gram_join);
+  t.pieces = cut_tiles(gram, order, t.gram_side, num_cu, &t.gram, &t.gram_join);
   std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return t.mats[a].r > t.mats[b].r; });
-  t.pieces = std::max(t.pieces, cut(square, order, t.gram_side, num_cu, &t.square, &t.square_join));
-  t.update = spread(update, order);
+  t.pieces = std::max(t.pieces, cut_tiles(square, order, t.gram_side, num_cu, &t.square, &t.square_join));
+  t.update = spread_tiles(update, order);
   return t;
 }
 
