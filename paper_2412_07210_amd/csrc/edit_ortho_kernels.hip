@@ -315,9 +315,11 @@ __device__ __forceinline__ int chunk_swizzle(int row, int chunk) {
 }
 
 // 16 bytes a lane from global memory to LDS, no register in between: lane l's
-// go to `lds` + 16 l.  The compiler keeps nothing in m0 here (no indirect
-// register access, no messages); with its own builtin it would wait for the
-// load before any other read of LDS.
+// go to `lds` + 16 l.  m0 is a reserved register, which a list of clobbers
+// cannot name; the compiler writes it right before uses of its own, and these
+// kernels have none (no indirect register access, no messages: in the generated
+// code m0 occurs in these lines only).  With its own builtin it would wait for
+// the load before any other read of LDS.
 __device__ __forceinline__ void load_to_lds(uint32_t lds, const void* base, uint32_t offset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
@@ -663,17 +665,15 @@ void ortho_product_kernel(const OrthoMat* __restrict__ mats, const OrthoTile* __
   const int64_t step = PRODUCT == kProductGram ? S::kSlabK * L::pitch(ld) : 64;
   const int slabs = t.end - t.begin;
   p += t.begin * step, q += t.begin * step;
-  // Slab n, or of its loads those with number part mod parts.
-  auto fetch = [&](int n, int part = 0, int parts = 1) {
+  auto fetch = [&](int n) {  // slab n
     const uint32_t at = lds0 + (n & (RING - 1)) * S::kSlab;
     const _Float16* from_p = p + n * step;
     const _Float16* from_q = q + n * step;
 #pragma unroll
-    for (int i = 0; i < S::kLoadsP; ++i)
-      if (i % parts == part) load_to_lds(at + (wave + i * S::kWaves) * 1024, from_p, off_p[i]);
+    for (int i = 0; i < S::kLoadsP; ++i) load_to_lds(at + (wave + i * S::kWaves) * 1024, from_p, off_p[i]);
 #pragma unroll
     for (int i = 0; i < S::kLoadsQ; ++i)
-      if (i % parts == part) load_to_lds(at + S::kBytesP + (wave + i * S::kWaves) * 1024, from_q, off_q[i]);
+      load_to_lds(at + S::kBytesP + (wave + i * S::kWaves) * 1024, from_q, off_q[i]);
   };
   for (int n = 0; n < RING - 1; ++n)
     if (n < slabs) fetch(n);
