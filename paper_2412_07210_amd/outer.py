@@ -730,6 +730,9 @@ class Orthogonalizer:
         precision = cfg.precision or ("fast" if cfg.dtype == "bf16" else "full")
         if precision not in ("fast", "full"):
             raise ValueError("precision must be 'fast' or 'full'")
+        for name, value, bits in (("numel", cfg.numel, 63), ("steps", cfg.steps, 31)):
+            if int(value) != value or abs(int(value)) >= 2 ** bits:
+                raise ValueError(f"{name} must be a whole number below 2^{bits}")
         steps = int(cfg.steps)
         coef = None
         if cfg.coefficients is not None:
@@ -740,9 +743,10 @@ class Orthogonalizer:
                 raise ValueError(f"coefficients must be one triple or {steps} of them")
             coef = (ctypes.c_double * flat.size)(*flat.reshape(-1).tolist())
         for m in cfg.matrices:
-            for x in m:
-                if int(x) != x:
-                    raise ValueError("a matrix is (offset, rows, cols) in whole numbers")
+            if len(m) != 3 or any(int(x) != x for x in m):
+                raise ValueError("a matrix is (offset, rows, cols) in whole numbers")
+            if abs(int(m[0])) >= 2 ** 63:
+                raise ValueError("offset must be below 2^63")
             if not all(abs(int(x)) < 2 ** 31 for x in m[1:]):
                 raise ValueError("rows and cols must be below 2^31")
         mats = (_OrthoMatrix * max(1, len(cfg.matrices)))(
