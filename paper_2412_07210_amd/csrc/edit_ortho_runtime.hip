@@ -418,6 +418,10 @@ edit_status_t edit_ortho_init(const edit_ortho_config_t* cfg, edit_ortho_t* out)
     h->device = dev;
     h->coef = coef;
     Tables t = make_tables(cfg, num_cu);
+    // a launch takes less than 2^32 threads; no kernel has more than 512 a block
+    for (const size_t blocks : {t.mats.size(), t.chunks.size(), t.load.size(), t.gram.size(), t.square.size(), t.update.size(),
+                                4 * t.gram_join.size(), 4 * t.square_join.size()})
+      if (blocks >= (size_t(1) << 32) / 512) return ofail(EDIT_EINVAL, "too many matrices, gaps or tiles for one launch");
     const size_t total = std::max<size_t>(lay_out(h.get(), t, nullptr, num_cu), 256);
     hipError_t e = hipMalloc(reinterpret_cast<void**>(&h->arena), total);
     if (e != hipSuccess) return ofail(EDIT_ENOMEM, std::string("hipMalloc of the workspace: ") + hipGetErrorString(e));

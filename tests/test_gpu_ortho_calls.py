@@ -1,10 +1,11 @@
 """Calls of the orthogonalised updates that the documentation allows, beside
 those of test_gpu_ortho.py (GPU): handles of default precision in the outer
-step, and calls after a failed one."""
+step, calls after a failed one, and layouts beyond a launch."""
 import pytest
 import torch
 
 from ortho_reference import layout
+from paper_2412_07210_amd.outer import EDIT_EINVAL
 from paper_2412_07210_amd import ONE_PASS, EditOuter, EditOuterError, OrthoConfig, Orthogonalizer, OuterConfig
 
 pytestmark = pytest.mark.gpu
@@ -114,3 +115,11 @@ def test_calls_after_a_failed_init():
                 make()
             assert torch.equal(o.orthogonalize(x), want)
             assert float(torch.ones(8, device=DEV).sum()) == 8.0
+
+
+def test_layouts_beyond_a_launch_are_refused():
+    """More tiles than a launch takes are refused at init, not in the middle of a step."""
+    long = 2 ** 24
+    with pytest.raises(EditOuterError, match="too many") as e:
+        _ortho(32 * long, [(k * long, long, 1) for k in range(32)])
+    assert e.value.status == EDIT_EINVAL
