@@ -462,7 +462,8 @@ edit_status_t edit_ortho_local_step(edit_ortho_t h, void *param, const void *gra
 edit_status_t edit_outer_step_layer_ortho(edit_outer_t h, int32_t layer, edit_ortho_t ortho, float *theta,
                                           float *momentum, void *const *replicas, void *stream);
 
-/* Release the workspace (waits for the device's pending work). */
+/* Release the workspace (waits for the pending work of the handle's device,
+ * whichever is current). */
 void edit_ortho_destroy(edit_ortho_t h);
 
 /* ---- measurement helpers (not part of the method) ---------------------- */

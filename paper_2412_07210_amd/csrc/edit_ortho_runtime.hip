@@ -495,10 +495,13 @@ edit_status_t edit_ortho_local_step(edit_ortho_t h, void* param, const void* gra
 
 void edit_ortho_destroy(edit_ortho_t h) {
   if (!h) return;
+  int prev = -1;
+  if (hipGetDevice(&prev) == hipSuccess && prev != h->device) (void)hipSetDevice(h->device);
   if (h->arena) {
     (void)hipDeviceSynchronize();
     (void)hipFree(h->arena);
   }
+  if (prev >= 0 && prev != h->device) (void)hipSetDevice(prev);
   delete h;
 }
 

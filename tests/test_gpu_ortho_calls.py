@@ -123,3 +123,21 @@ def test_layouts_beyond_a_launch_are_refused():
     with pytest.raises(EditOuterError, match="too many") as e:
         _ortho(32 * long, [(k * long, long, 1) for k in range(32)])
     assert e.value.status == EDIT_EINVAL
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two devices")
+def test_destroy_beside_another_current_device():
+    """The workspace is released behind its own device's work, and the current device stays."""
+    numel, mats = layout([(2000, 2000)])
+    x = _randn(numel, 32).to(torch.bfloat16)
+    with _ortho(numel, mats) as o:
+        want = o.orthogonalize(x)
+    out = torch.empty_like(x)
+    o = _ortho(numel, mats)
+    with torch.cuda.device(1):
+        o.orthogonalize(x, out)
+        o._lib.edit_ortho_destroy(o._h)
+        o._h = None
+        assert torch.cuda.current_device() == 1
+    torch.cuda.synchronize(DEV)
+    assert torch.equal(out, want)
