@@ -389,7 +389,7 @@ void edit_group_destroy(edit_group_t h);
  * single one) may put it off by 2.5e-2.  An iteration rounded to bf16 is off by
  * 1e-2 to 9e-2, and by 0.3 to 1.9 where U lacks directions.
  * EDIT_ORTHO_FULL takes three products (high*high, high*low, low*high) at up to
- * 2.3 times the time and is off by 1e-6 to 6e-6, and by up to 2.5e-4 where U
+ * 2.5 times the time and is off by 1e-6 to 6e-6, and by up to 2.5e-4 where U
  * lacks directions: one to four times the error of an fp32 iteration.
  * Norms are summed in fp64, steps are taken in fp64 and rounded once.  Results
  * are the same bit for bit on every run.

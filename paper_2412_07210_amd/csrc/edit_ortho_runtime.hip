@@ -44,7 +44,9 @@ constexpr int kGapChunks = 4096;                  // blocks for a run of element
 // operation but fill the GPU with a quarter of the work.  us at 128 and 64, n
 // matrices of 1024 x 1024 (FAST): symmetric products of 40 tiles (of 128 x
 // 128) 19 and 8, 160: 22 and 18, 240: 23 and 24, 280: 33 and 25, 400: 34 and
-// 33, 480: 35 and 39; update product of 64 tiles 14 and 8, 192: 18 and 15, 256:
+// 33, 480: 35 and 39 (with the XCDs' shares as spread_tiles() deals them, of
+// which some are a quarter larger than others where a matrix's tiles do not
+// divide by eight); update product of 64 tiles 14 and 8, 192: 18 and 15, 256:
 // 19 and 20, 512: 29 and 35.
 //
 // FAST's update product of much work takes 256 x 256 tiles, which load half as

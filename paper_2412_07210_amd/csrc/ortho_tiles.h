@@ -26,6 +26,8 @@ inline int64_t tiles_ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // The tiles of all matrices, so that the workgroups of an XCD (every eighth)
 // take neighbouring ones of a matrix, whose operands they share in its L2;
 // matrices with the longest sums first, so that short ones fill the end.
+// What a matrix has beyond a multiple of eight is not evened out over the
+// matrices: seven of 36 tiles come out as 28 and 35 a list.
 inline std::vector<OrthoTile> spread_tiles(const std::vector<std::vector<OrthoTile>>& of_matrix,
                                            const std::vector<int>& order) {
   std::vector<OrthoTile> list[kXcds];

@@ -656,7 +656,7 @@ class OrthoConfig:
     # (a, b, c) for all steps or one triple per step; None: 3.4445, -4.7750, 2.0315
     coefficients: Optional[Sequence] = None
     # "fast" (O is off by 1e-3 of its norm, small or low-rank matrices by more:
-    # see edit_outer.h) or "full" (as an fp32 iteration, at up to 2.3 times the
+    # see edit_outer.h) or "full" (as an fp32 iteration, at up to 2.5 times the
     # time).  None: "fast" for bf16 and "full" for f32, and "full" in the outer
     # step, whose theta is fp32 whatever the dtype here
     precision: Optional[str] = None
