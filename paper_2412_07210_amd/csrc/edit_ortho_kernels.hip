@@ -24,14 +24,14 @@
 //    near I, and what fp16 rounds off R is small with it; b A + c A^2 would
 //    cancel to a third of its terms.  Only s must be the same in the three
 //    products, so it is computed once per iteration and stored.
-// Error of O against 64 bits, of its norm: 2e-4 to 1.3e-3 with FAST over
+// Error of O against 64 bits, of its norm: 2e-4 to 2e-3 with FAST over
 // Gaussian, low-rank (over noise) and power-law spectra of 64 rows and more (1e-3
-// to 4e-2 if X itself were rounded to fp16, 1e-2 to 9e-2 in bf16); 1e-6 to 6e-6
-// with FULL.  Directions that X lacks gather noise, which grows by a = 3.4 a
+// to 4e-2 if X itself were rounded to fp16, 1e-2 to 9e-2 in bf16); with FULL 0.6
+// to 1.7 times an fp32 iteration's (1024 x 1024 Gaussian 1.7e-6 for its 3.1e-6).  Directions that X lacks gather noise, which grows by a = 3.4 a
 // step: with FAST F (X - X_high) is left out, and F is -(bs + cs^2) I there, s
 // = ||X||^2 / r; so an exact low rank is off by up to 5e-3, and by up to 0.25 / r
 // of fewer than 64 rows (rank 1 of 512 x 512 1.2e-3, of 8 x 8 2e-2; without X's
-// low half 0.15); with FULL by up to 2.5e-4.
+// low half 0.15); with FULL 512 x 512 of rank 1 by 1.2e-4.
 #include <type_traits>
 
 #include "edit_ortho_device.h"

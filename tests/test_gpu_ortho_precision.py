@@ -93,6 +93,24 @@ def test_documented_errors(shape, precision):
             assert _error(_orthogonalize(shape, u, precision), ref) <= 2.5e-2
 
 
+@pytest.mark.parametrize("shape", [(64, 64), (1024, 1024), (2048, 5632), (4096, 4096)], ids=lambda s: "%dx%d" % s)
+def test_documented_errors_of_layers(shape):
+    """Full, nearly low and low rank up to a layer's sizes."""
+    r = min(shape)
+    nearly = _of_rank(16, *shape, 81) + 0.1 * _randn(*shape, 83)
+    full = 2.4e-4 + 1.3e-5 * math.sqrt(r)  # above the derived bound for every rank
+    cases = [(_randn(*shape, 80), 2e-3, 6e-6), (nearly, 2e-3, full)]
+    for rank in (1, 4, 16):
+        u = _of_rank(rank, *shape, 84)
+        assert reference_and_bound(u, "full", deficient=True)[1] <= full
+        cases.append((u, 5e-3, full))
+    for u, *documented in cases:
+        ref, _ = reference_and_bound(u, "full")
+        for precision, most in zip(("fast", "full"), documented):
+            off = _error(_orthogonalize(shape, u, precision), ref)
+            assert off <= most, f"{precision} {shape}: {off:.3g}, documented {most:.3g}"
+
+
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 6, 8])
 @pytest.mark.parametrize("shape", [(128, 128), (200, 170), (900, 3900), (2100, 2120), (500, 29201)], ids=lambda s: "%dx%d" % s)
 def test_fast_at_other_step_counts(shape, steps):
