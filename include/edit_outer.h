@@ -467,6 +467,142 @@ edit_status_t edit_outer_step_layer_ortho(edit_outer_t h, int32_t layer, edit_or
  * whichever is current). */
 void edit_ortho_destroy(edit_ortho_t h);
 
+/* ---- AdamW over many tensors ------------------------------------------- */
+
+/* The workers' local optimizer of the paper (AdamW, Algorithm 1), for all
+ * tensors of a replica in one call: whole sync units, the tensors of a module,
+ * or the gains and biases that edit_ortho_local_step leaves to another
+ * optimizer.  With gradients g and t counting the steps,
+ *
+ *     S = sum of g^2 over all tensors;   c = min(1, max_norm / (sqrt(S) + 1e-6))
+ *     t <- t + 1;  g' = c g;  m <- beta1 m + (1 - beta1) g';
+ *     v <- beta2 v + (1 - beta2) g'^2
+ *     p <- p - (lr lambda d_k p + lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps))
+ *
+ * d_k is the factor of the weight decay lambda for tensor k (0 for a gain, say).
+ *
+ * A handle serves one list of tensors, numel[k] elements each, and holds t;
+ * parameters, gradients and states are the caller's.  Parameters and gradients
+ * begin at any element (views into a flat unit) and are contiguous; states are
+ * 16-byte aligned, scales 4-byte aligned.
+ *
+ * Precision.  S is summed in fp64, g' is rounded to fp32, m and v are taken in
+ * fp64 and rounded once to fp32, and the step of p is taken in fp32 with one
+ * rounding of p behind it: an fp32 p is off by half a place and 1e-6 of its
+ * step, and a bf16 one by half a place of bf16, or, with EDIT_ADAMW_STOCHASTIC,
+ * by less than one: it is rounded to q floor(|p| / q + u), q the spacing of bf16
+ * at p and u random, so that steps of less than half a place count on average.
+ *
+ * States in 8 bits (EDIT_ADAMW_E4M3): OCP e4m3 values, and an fp32 scale, a power
+ * of two, for every EDIT_ADAMW_BLOCK elements of a tensor (the last block may be
+ * shorter).  The new m and v step p in fp32 and are then held: with E =
+ * floor(log2) of the block's largest finite |x|, at least -119, scale = 2^(E - 7),
+ * y = x / scale, q = 2^(max(floor(log2 |y|), -6) - 3),
+ *
+ *     code = sign(y) q floor(|y| / q + u),  u random: 20 bits over 2^20
+ *
+ * which is right on average.  (Rounded to nearest, v would stay where it is: a
+ * step moves it by less than half the distance to its neighbours.)  v's |y| is
+ * 2^-9 at least, the smallest code above zero, so that elements far below their
+ * block's largest (2^-16 of its v and less) take smaller steps instead of
+ * unbounded ones.  A NaN or an infinity in an element makes this element NaN
+ * and leaves the others of its block alone.
+ *
+ * Random numbers are a function of the call's seed, t, the tensor's index and
+ * the element: results are the same bit for bit on every run, and a run that is
+ * resumed with edit_adamw_state_set goes on as it would have.
+ *
+ * Calls allocate nothing, do not synchronise and can be captured into HIP
+ * graphs; a replay takes the next t.  Calls on one handle, replays included,
+ * share its record of the step and must not overlap: order them on one stream
+ * or with events. */
+#define EDIT_ADAMW_BLOCK 256
+#define EDIT_ADAMW_CLIP_EPS 1e-6
+
+/* Round a bf16 p stochastically. */
+#define EDIT_ADAMW_STOCHASTIC 1u
+
+/* How m and v are held. */
+typedef enum { EDIT_ADAMW_F32 = 0, EDIT_ADAMW_E4M3 = 1 } edit_adamw_held_t;
+
+typedef struct edit_adamw *edit_adamw_t; /* opaque, library-owned */
+
+typedef struct {
+  int32_t num_tensors;  /* >= 0                                               */
+  const int64_t *numel; /* [num_tensors], 0..2^34 each; copied at init         */
+  const double *decay;  /* [num_tensors] d_k, finite and >= 0; NULL: 1 for all */
+  int32_t dtype;        /* edit_dtype_t of the parameters                      */
+  int32_t grad_dtype;   /* edit_dtype_t of the gradients                       */
+  int32_t held;         /* edit_adamw_held_t                                   */
+  uint32_t flags;       /* 0 or EDIT_ADAMW_STOCHASTIC                          */
+  double beta1, beta2;  /* in [0, 1)                                           */
+  double eps;           /* 1e-12 at least                                      */
+  double weight_decay;  /* lambda, >= 0                                        */
+} edit_adamw_config_t;
+
+/* Host arrays of num_tensors device pointers.  Entries of empty tensors are
+ * not looked at. */
+typedef struct {
+  void *const *param;            /* [numel] of dtype                                  */
+  const void *const *grad;       /* [numel] of grad_dtype; NULL: tensor k stays as it */
+                                 /* is in this call, states included                  */
+  void *const *exp_avg;          /* m: [numel] fp32, or e4m3 codes                    */
+  void *const *exp_avg_sq;       /* v                                                 */
+  float *const *exp_avg_scale;   /* [ceil(numel / EDIT_ADAMW_BLOCK)], E4M3 only       */
+  float *const *exp_avg_sq_scale;
+} edit_adamw_tensors_t;
+
+typedef struct {
+  double lr;               /* finite and >= 0                                   */
+  const double *lr_device; /* device: lr is read there when the call runs (a    */
+                           /* schedule under a captured graph); NULL: lr        */
+  double max_norm;         /* clips; finite, > 0; 0: no clip                    */
+  const double *sumsq;     /* device: S, e.g. added up over a module's shards;  */
+                           /* NULL: taken from grad where max_norm > 0          */
+  uint64_t seed;           /* of the random numbers                             */
+} edit_adamw_call_t;
+
+/* Of the last call that ran (host memory). */
+typedef struct {
+  int64_t step;     /* t                                                      */
+  int64_t skipped;  /* calls left out: their S was not finite                 */
+  double norm;      /* sqrt(S) of the last call that had one                  */
+  double clip_coef; /* c of the last call; 0 if it was left out               */
+} edit_adamw_state_t;
+
+/* Create a handle on the current device, t = 0.  EDIT_EINVAL for a bad
+ * configuration, EDIT_ENODEV off gfx950, EDIT_ENOMEM. */
+edit_status_t edit_adamw_init(const edit_adamw_config_t *cfg, edit_adamw_t *out);
+
+/* *sumsq = S of the gradients (device memory, fp64, 8-byte aligned; NULL
+ * gradients are left out).  Changes no state. */
+edit_status_t edit_adamw_sumsq(edit_adamw_t h, const void *const *grad, double *sumsq, void *stream);
+
+/* One step of all tensors, enqueued on `stream`, in place on parameters and
+ * states.  If S is there (max_norm > 0 or sumsq) and not finite, the call
+ * changes nothing but `skipped`: t, parameters and states stay.  What is written
+ * must overlap nothing else; gradients may share memory with each other.
+ * EDIT_EINVAL otherwise, before anything is enqueued. */
+edit_status_t edit_adamw_step(edit_adamw_t h, const edit_adamw_tensors_t *tensors, const edit_adamw_call_t *call,
+                              void *stream);
+
+/* fp32 states (16-byte aligned) to E4M3 ones as a step holds them, with t = 0 in
+ * the random numbers, and back (exactly).  Handles of EDIT_ADAMW_E4M3; param and
+ * grad of `tensors` are not looked at.  Overlaps as in edit_adamw_step. */
+edit_status_t edit_adamw_pack(edit_adamw_t h, const float *const *exp_avg, const float *const *exp_avg_sq,
+                              const edit_adamw_tensors_t *tensors, uint64_t seed, void *stream);
+edit_status_t edit_adamw_unpack(edit_adamw_t h, const edit_adamw_tensors_t *tensors, float *const *exp_avg,
+                                float *const *exp_avg_sq, void *stream);
+
+/* The record of the last call, after waiting for the handle's device; t (0 or
+ * more) for a run that is resumed, likewise. */
+edit_status_t edit_adamw_state_get(edit_adamw_t h, edit_adamw_state_t *out);
+edit_status_t edit_adamw_state_set(edit_adamw_t h, int64_t step);
+
+/* Release the handle (waits for the pending work of its device, whichever is
+ * current). */
+void edit_adamw_destroy(edit_adamw_t h);
+
 /* ---- measurement helpers (not part of the method) ---------------------- */
 
 /* every > 0: steps of units whose index is a multiple of `every` record HIP

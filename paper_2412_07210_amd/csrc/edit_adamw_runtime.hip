@@ -1,0 +1,402 @@
+// Host runtime of the AdamW step (include/edit_outer.h, "AdamW over many
+// tensors"): checks, the tables of tensors that launches take as kernel
+// arguments, and the launches.  A call enqueues norm pass (with a clip) ->
+// decision -> update passes on the caller's stream.
+#include <algorithm>
+#include <cmath>
+#include <memory>
+#include <string>
+#include <vector>
+
+#include "edit_adamw_internal.h"
+#include "edit_group_internal.h"
+
+using namespace edit;
+
+namespace {
+
+#define ADAM_TRY(expr)                \
+  do {                                \
+    const edit_status_t st_ = (expr); \
+    if (st_ != EDIT_OK) return st_;   \
+  } while (0)
+
+edit_status_t afail(edit_status_t s, const std::string& msg) { return set_error(s, msg.c_str()); }
+
+edit_status_t afail_hip(hipError_t e, const char* what) {
+  return afail(EDIT_EHIP, std::string(what) + ": " + hipGetErrorString(e));
+}
+
+constexpr int64_t kMaxNumel = int64_t(1) << 34;
+constexpr int64_t kMaxBlocks = kMaxNumel / kAdamChunk;  // of a launch: fewer than 2^32 threads
+
+int64_t chunks_of(int64_t numel, int64_t chunk) { return (numel + chunk - 1) / chunk; }
+
+struct Range {
+  uintptr_t lo, hi;
+};
+
+}  // namespace
+
+struct edit_adamw {
+  std::vector<int64_t> numel;
+  std::vector<float> decay;
+  bool param_bf16 = false, grad_bf16 = false, held = false, stochastic = false;
+  AdamHyper hyper{};
+  double weight_decay = 0.0;
+  int device = 0, num_cu = 0;
+  AdamRecord* rec = nullptr;
+  double* partials = nullptr;  // a norm launch's follow the one's before
+  std::vector<Range> written, read;  // of the call being checked
+};
+
+namespace {
+
+edit_status_t check_adamw_config(const edit_adamw_config_t* cfg) {
+  if (cfg->num_tensors < 0) return afail(EDIT_EINVAL, "num_tensors must be >= 0");
+  if (cfg->num_tensors > 0 && !cfg->numel) return afail(EDIT_EINVAL, "numel must not be NULL");
+  for (const auto& [value, name] : {std::pair<int32_t, const char*>{cfg->dtype, "dtype"}, {cfg->grad_dtype, "grad_dtype"}})
+    if (value != EDIT_F32 && value != EDIT_BF16)
+      return afail(EDIT_EINVAL, std::string(name) + " must be EDIT_F32 or EDIT_BF16");
+  if (cfg->held != EDIT_ADAMW_F32 && cfg->held != EDIT_ADAMW_E4M3)
+    return afail(EDIT_EINVAL, "held must be EDIT_ADAMW_F32 or EDIT_ADAMW_E4M3");
+  if (cfg->flags & ~EDIT_ADAMW_STOCHASTIC) return afail(EDIT_EINVAL, "unknown flag bits");
+  if ((cfg->flags & EDIT_ADAMW_STOCHASTIC) && cfg->dtype != EDIT_BF16)
+    return afail(EDIT_EINVAL, "EDIT_ADAMW_STOCHASTIC needs bf16 parameters");
+  if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0)) return afail(EDIT_EINVAL, "beta1 must be in [0, 1)");
+  if (!(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0)) return afail(EDIT_EINVAL, "beta2 must be in [0, 1)");
+  if (!(cfg->eps >= 1e-12) || !(cfg->eps <= 1e30)) return afail(EDIT_EINVAL, "eps must be in [1e-12, 1e30]");
+  if (!(cfg->weight_decay >= 0.0) || !std::isfinite(cfg->weight_decay))
+    return afail(EDIT_EINVAL, "weight_decay must be finite and >= 0");
+  for (int k = 0; k < cfg->num_tensors; ++k) {
+    const std::string at = "[" + std::to_string(k) + "]";
+    if (cfg->numel[k] < 0) return afail(EDIT_EINVAL, "numel" + at + " is negative");
+    if (cfg->numel[k] > kMaxNumel) return afail(EDIT_EINVAL, "numel" + at + " must be at most 2^34");
+    if (cfg->decay && (!(cfg->decay[k] >= 0.0) || !std::isfinite(cfg->decay[k])))
+      return afail(EDIT_EINVAL, "decay" + at + " must be finite and >= 0");
+  }
+  return EDIT_OK;
+}
+
+edit_status_t check_adamw_device(const edit_adamw* h) {
+  int dev = -1;
+  const hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return afail_hip(e, "hipGetDevice");
+  if (dev != h->device)
+    return afail(EDIT_EINVAL, "call made with device " + std::to_string(dev) +
+                                  " current; the handle belongs to device " + std::to_string(h->device));
+  return EDIT_OK;
+}
+
+// Notes the buffer of tensor k for the check of overlaps.
+edit_status_t note(std::vector<Range>* ranges, const void* p, int64_t bytes, uintptr_t align, const char* name, int k) {
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+  if (!p || (lo & (align - 1))) {
+    const std::string what = std::string(name) + "[" + std::to_string(k) + "]";
+    if (!p) return afail(EDIT_EINVAL, what + " must not be NULL");
+    return afail(EDIT_EINVAL, what + " must be " + std::to_string(align) + "-byte aligned");
+  }
+  ranges->push_back({lo, lo + static_cast<uintptr_t>(bytes)});
+  return EDIT_OK;
+}
+
+// What is written overlaps nothing.
+edit_status_t check_overlaps(edit_adamw* h) {
+  auto less = [](const Range& a, const Range& b) { return a.lo < b.lo; };
+  std::sort(h->written.begin(), h->written.end(), less);
+  std::sort(h->read.begin(), h->read.end(), less);
+  for (size_t i = 1; i < h->written.size(); ++i)
+    if (h->written[i].lo < h->written[i - 1].hi)
+      return afail(EDIT_EINVAL, "parameters and states must not overlap (the same tensor twice?)");
+  // written ranges are disjoint, so ascending at both ends
+  for (const Range& r : h->read) {
+    const auto it = std::upper_bound(h->written.begin(), h->written.end(), r.lo,
+                                     [](uintptr_t lo, const Range& w) { return lo < w.hi; });
+    if (it != h->written.end() && it->lo < r.hi) return afail(EDIT_EINVAL, "what is read must not overlap what is written");
+  }
+  return EDIT_OK;
+}
+
+edit_status_t check_states(edit_adamw* h, const edit_adamw_tensors_t* t, std::vector<Range>* ranges, int k) {
+  const int64_t n = h->numel[k], bytes = h->held ? n : 4 * n, scales = 4 * chunks_of(n, EDIT_ADAMW_BLOCK);
+  ADAM_TRY(note(ranges, t->exp_avg[k], bytes, 16, "exp_avg", k));
+  ADAM_TRY(note(ranges, t->exp_avg_sq[k], bytes, 16, "exp_avg_sq", k));
+  if (h->held) {
+    ADAM_TRY(note(ranges, t->exp_avg_scale[k], scales, 4, "exp_avg_scale", k));
+    ADAM_TRY(note(ranges, t->exp_avg_sq_scale[k], scales, 4, "exp_avg_sq_scale", k));
+  }
+  return EDIT_OK;
+}
+
+edit_status_t check_state_arrays(const edit_adamw* h, const edit_adamw_tensors_t* t) {
+  if (!t->exp_avg || !t->exp_avg_sq) return afail(EDIT_EINVAL, "exp_avg and exp_avg_sq must not be NULL");
+  if (h->held && (!t->exp_avg_scale || !t->exp_avg_sq_scale))
+    return afail(EDIT_EINVAL, "exp_avg_scale and exp_avg_sq_scale must not be NULL");
+  return EDIT_OK;
+}
+
+// Partial sums of the gradients' squares; *count: how many there are.
+edit_status_t enqueue_norm(edit_adamw* h, const void* const* grad, int* count, hipStream_t s) {
+  const int most = kAdamNormBlocksPerCu * h->num_cu, tensors = static_cast<int>(h->numel.size());
+  *count = 0;
+  for (int k = 0; k < tensors;) {
+    AdamNormTable t;
+    int used = 0;
+    int64_t chunks = 0;
+    for (; k < tensors && used < kAdamNormTensors; ++k) {
+      if (!grad[k] || h->numel[k] == 0) continue;
+      const int64_t more = chunks_of(h->numel[k], kAdamNormChunk);
+      if (chunks + more > INT32_MAX / 2) break;
+      t.first[used] = static_cast<int32_t>(chunks);
+      t.numel[used] = h->numel[k];
+      t.grad[used++] = grad[k];
+      chunks += more;
+    }
+    if (used == 0) continue;
+    std::fill(t.first + used, t.first + kAdamNormTensors, INT32_MAX);
+    t.chunks = static_cast<int32_t>(chunks);
+    const int blocks = static_cast<int>(std::min<int64_t>(chunks, most));
+    const hipError_t e = launch_adamw_norm(h->grad_bf16, blocks, t, h->partials + *count, s);
+    if (e != hipSuccess) return afail_hip(e, "norm pass launch");
+    *count += blocks;
+  }
+  return EDIT_OK;
+}
+
+// Calls launch(blocks, table) for every table of tensors; fill(k, &tensor): whether tensor k takes part.
+template <typename Fill, typename Launch>
+edit_status_t for_tables(const edit_adamw* h, const Fill& fill, const Launch& launch) {
+  const int tensors = static_cast<int>(h->numel.size());
+  for (int k = 0; k < tensors;) {
+    AdamTable t;
+    int used = 0, skipped = 0;
+    int64_t blocks = 0;
+    t.base = k;
+    // a tensor that takes no part keeps its place, so that base + place is its index
+    for (; k < tensors && used < kAdamTensors; ++k) {
+      AdamTensor& to = t.tensor[used];
+      const int64_t more = chunks_of(h->numel[k], kAdamChunk);
+      if (blocks + more > kMaxBlocks) break;
+      t.first[used] = static_cast<int32_t>(blocks);
+      t.decay[used] = h->decay[k];
+      to = {};
+      if (more && fill(k, &to)) {
+        to.numel = h->numel[k];
+        blocks += more;
+      } else {
+        ++skipped;
+      }
+      ++used;
+    }
+    if (skipped == used) continue;
+    std::fill(t.first + used, t.first + 64, INT32_MAX);
+    const hipError_t e = launch(static_cast<int>(blocks), t);
+    if (e != hipSuccess) return afail_hip(e, "update pass launch");
+  }
+  return EDIT_OK;
+}
+
+void fill_states(const edit_adamw* h, const edit_adamw_tensors_t* t, int k, AdamTensor* to) {
+  to->m = t->exp_avg[k];
+  to->v = t->exp_avg_sq[k];
+  if (h->held) {
+    to->m_scale = t->exp_avg_scale[k];
+    to->v_scale = t->exp_avg_sq_scale[k];
+  }
+}
+
+edit_status_t convert(edit_adamw* h, bool pack, const edit_adamw_tensors_t* t, const float* const* m, const float* const* v,
+                      uint64_t seed, hipStream_t s) {
+  if (!h) return afail(EDIT_EINVAL, "NULL handle");
+  if (!h->held) return afail(EDIT_EINVAL, "the handle holds its states in fp32");
+  if (!t || (!h->numel.empty() && (!m || !v))) return afail(EDIT_EINVAL, "tensors, exp_avg and exp_avg_sq must not be NULL");
+  ADAM_TRY(check_adamw_device(h));
+  if (h->numel.empty()) return EDIT_OK;
+  ADAM_TRY(check_state_arrays(h, t));
+  h->written.clear();
+  h->read.clear();
+  for (size_t k = 0; k < h->numel.size(); ++k) {
+    const int64_t n = h->numel[k];
+    if (n == 0) continue;
+    const int i = static_cast<int>(k);
+    ADAM_TRY(note(pack ? &h->read : &h->written, m[k], 4 * n, 16, "fp32 exp_avg", i));
+    ADAM_TRY(note(pack ? &h->read : &h->written, v[k], 4 * n, 16, "fp32 exp_avg_sq", i));
+    ADAM_TRY(check_states(h, t, pack ? &h->written : &h->read, i));
+  }
+  ADAM_TRY(check_overlaps(h));
+  return for_tables(
+      h,
+      [&](int k, AdamTensor* to) {
+        fill_states(h, t, k, to);
+        to->param = const_cast<float*>(m[k]);
+        to->grad = v[k];
+        return true;
+      },
+      [&](int blocks, const AdamTable& table) { return launch_adamw_convert(pack, blocks, table, adamw_key(seed, 0), s); });
+}
+
+}  // namespace
+
+extern "C" {
+
+edit_status_t edit_adamw_init(const edit_adamw_config_t* cfg, edit_adamw_t* out) {
+  set_error(EDIT_OK, "");
+  if (!cfg || !out) return afail(EDIT_EINVAL, "cfg and out must not be NULL");
+  *out = nullptr;
+  try {
+    ADAM_TRY(check_adamw_config(cfg));
+    int dev = 0, num_cu = 0;
+    ADAM_TRY(current_gfx950(&dev, &num_cu));
+    auto h = std::make_unique<edit_adamw>();
+    const size_t tensors = static_cast<size_t>(cfg->num_tensors);
+    h->numel.assign(cfg->numel, cfg->numel + tensors);
+    h->decay.assign(tensors, 1.f);
+    for (size_t k = 0; cfg->decay && k < tensors; ++k) h->decay[k] = static_cast<float>(cfg->decay[k]);
+    h->param_bf16 = cfg->dtype == EDIT_BF16;
+    h->grad_bf16 = cfg->grad_dtype == EDIT_BF16;
+    h->held = cfg->held == EDIT_ADAMW_E4M3;
+    h->stochastic = cfg->flags & EDIT_ADAMW_STOCHASTIC;
+    h->hyper = {cfg->beta1, cfg->beta2, cfg->eps};
+    h->weight_decay = cfg->weight_decay;
+    h->device = dev;
+    h->num_cu = num_cu;
+    h->written.reserve(5 * tensors);
+    h->read.reserve(4 * tensors);
+    // launches of the norm pass: full tables, and ones that end at their count of chunks
+    int64_t chunks = 0;
+    for (int64_t n : h->numel) chunks += chunks_of(n, kAdamNormChunk);
+    const size_t launches = tensors / kAdamNormTensors + 2 + static_cast<size_t>(2 * (chunks / (INT32_MAX / 2)));
+    const size_t partials = launches * kAdamNormBlocksPerCu * num_cu * sizeof(double);
+    char* arena = nullptr;
+    hipError_t e = hipMalloc(reinterpret_cast<void**>(&arena), 256 + partials);
+    if (e != hipSuccess) return afail(EDIT_ENOMEM, std::string("hipMalloc of the workspace: ") + hipGetErrorString(e));
+    e = hipMemset(arena, 0, 256);
+    if (e == hipSuccess) e = hipDeviceSynchronize();
+    if (e != hipSuccess) {
+      (void)hipFree(arena);
+      return afail_hip(e, "edit_adamw_init");
+    }
+    h->rec = reinterpret_cast<AdamRecord*>(arena);
+    h->partials = reinterpret_cast<double*>(arena + 256);
+    *out = h.release();
+    return EDIT_OK;
+  } catch (const std::exception&) {  // the lists' host memory
+    return afail(EDIT_ENOMEM, "host allocation failed");
+  }
+}
+
+edit_status_t edit_adamw_sumsq(edit_adamw_t h, const void* const* grad, double* sumsq, void* stream) {
+  if (!h) return afail(EDIT_EINVAL, "NULL handle");
+  if (!h->numel.empty() && !grad) return afail(EDIT_EINVAL, "grad must not be NULL");
+  ADAM_TRY(check_adamw_device(h));
+  h->written.clear();
+  h->read.clear();
+  ADAM_TRY(note(&h->written, sumsq, 8, 8, "sumsq", 0));
+  const int64_t size = h->grad_bf16 ? 2 : 4;
+  for (size_t k = 0; k < h->numel.size(); ++k)
+    if (h->numel[k] && grad[k]) ADAM_TRY(note(&h->read, grad[k], size * h->numel[k], size, "grad", static_cast<int>(k)));
+  ADAM_TRY(check_overlaps(h));
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  int count = 0;
+  ADAM_TRY(enqueue_norm(h, grad, &count, s));
+  const hipError_t e = launch_adamw_sum(h->partials, count, sumsq, s);
+  return e == hipSuccess ? EDIT_OK : afail_hip(e, "sum launch");
+}
+
+edit_status_t edit_adamw_step(edit_adamw_t h, const edit_adamw_tensors_t* t, const edit_adamw_call_t* call, void* stream) {
+  if (!h) return afail(EDIT_EINVAL, "NULL handle");
+  if (!t || !call) return afail(EDIT_EINVAL, "tensors and call must not be NULL");
+  if (!call->lr_device && (!(call->lr >= 0.0) || !std::isfinite(call->lr)))
+    return afail(EDIT_EINVAL, "lr must be finite and >= 0");
+  if (reinterpret_cast<uintptr_t>(call->lr_device) & 7u) return afail(EDIT_EINVAL, "lr_device must be 8-byte aligned");
+  if (reinterpret_cast<uintptr_t>(call->sumsq) & 7u) return afail(EDIT_EINVAL, "sumsq must be 8-byte aligned");
+  if (!(call->max_norm >= 0.0) || !std::isfinite(call->max_norm))
+    return afail(EDIT_EINVAL, "max_norm must be finite and > 0, or 0 for no clip");
+  ADAM_TRY(check_adamw_device(h));
+  const int tensors = static_cast<int>(h->numel.size());
+  h->written.clear();
+  h->read.clear();
+  if (tensors > 0) {
+    if (!t->param || !t->grad) return afail(EDIT_EINVAL, "param and grad must not be NULL");
+    ADAM_TRY(check_state_arrays(h, t));
+  }
+  const int64_t pb = h->param_bf16 ? 2 : 4, gb = h->grad_bf16 ? 2 : 4;
+  for (int k = 0; k < tensors; ++k) {
+    const int64_t n = h->numel[k];
+    if (n == 0 || !t->grad[k]) continue;
+    ADAM_TRY(note(&h->written, t->param[k], pb * n, pb, "param", k));
+    ADAM_TRY(note(&h->read, t->grad[k], gb * n, gb, "grad", k));
+    ADAM_TRY(check_states(h, t, &h->written, k));
+  }
+  ADAM_TRY(check_overlaps(h));
+
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  AdamCall c = {};
+  c.lr = call->lr;
+  c.lr_device = call->lr_device;
+  c.weight_decay = h->weight_decay;
+  c.max_norm = call->max_norm > 0.0 ? call->max_norm : INFINITY;
+  c.seed = call->seed;
+  c.check = call->max_norm > 0.0 || call->sumsq;
+  int count = 0;
+  if (c.check && !call->sumsq) ADAM_TRY(enqueue_norm(h, t->grad, &count, s));
+  const hipError_t e = launch_adamw_decide(h->partials, count, call->sumsq, c, h->hyper, h->rec, s);
+  if (e != hipSuccess) return afail_hip(e, "decision launch");
+  return for_tables(
+      h,
+      [&](int k, AdamTensor* to) {
+        if (!t->grad[k]) return false;
+        to->param = t->param[k];
+        to->grad = t->grad[k];
+        fill_states(h, t, k, to);
+        return true;
+      },
+      [&](int blocks, const AdamTable& table) {
+        return launch_adamw_step(h->param_bf16, h->grad_bf16, h->held, h->stochastic, blocks, table, h->hyper, h->rec, s);
+      });
+}
+
+edit_status_t edit_adamw_pack(edit_adamw_t h, const float* const* exp_avg, const float* const* exp_avg_sq,
+                              const edit_adamw_tensors_t* tensors, uint64_t seed, void* stream) {
+  return convert(h, true, tensors, exp_avg, exp_avg_sq, seed, reinterpret_cast<hipStream_t>(stream));
+}
+
+edit_status_t edit_adamw_unpack(edit_adamw_t h, const edit_adamw_tensors_t* tensors, float* const* exp_avg,
+                                float* const* exp_avg_sq, void* stream) {
+  return convert(h, false, tensors, exp_avg, exp_avg_sq, 0, reinterpret_cast<hipStream_t>(stream));
+}
+
+edit_status_t edit_adamw_state_get(edit_adamw_t h, edit_adamw_state_t* out) {
+  if (!h || !out) return afail(EDIT_EINVAL, "h and out must not be NULL");
+  ADAM_TRY(check_adamw_device(h));
+  hipError_t e = hipDeviceSynchronize();
+  AdamRecord r;
+  if (e == hipSuccess) e = hipMemcpy(&r, h->rec, sizeof r, hipMemcpyDeviceToHost);
+  if (e != hipSuccess) return afail_hip(e, "edit_adamw_state_get");
+  *out = {r.step, r.skipped, r.norm, r.clip};
+  return EDIT_OK;
+}
+
+edit_status_t edit_adamw_state_set(edit_adamw_t h, int64_t step) {
+  if (!h) return afail(EDIT_EINVAL, "NULL handle");
+  if (step < 0) return afail(EDIT_EINVAL, "step must be >= 0");
+  ADAM_TRY(check_adamw_device(h));
+  hipError_t e = hipDeviceSynchronize();
+  if (e == hipSuccess) e = hipMemcpy(&h->rec->step, &step, sizeof step, hipMemcpyHostToDevice);
+  if (e == hipSuccess) e = hipDeviceSynchronize();
+  return e == hipSuccess ? EDIT_OK : afail_hip(e, "edit_adamw_state_set");
+}
+
+void edit_adamw_destroy(edit_adamw_t h) {
+  if (!h) return;
+  int prev = -1;
+  if (hipGetDevice(&prev) == hipSuccess && prev != h->device) (void)hipSetDevice(h->device);
+  if (h->rec) {
+    (void)hipDeviceSynchronize();
+    (void)hipFree(h->rec);
+  }
+  if (prev >= 0 && prev != h->device) (void)hipSetDevice(prev);
+  delete h;
+}
+
+}  // extern "C"

@@ -41,6 +41,11 @@ EXPORTS = (
 )
 ORTHO_EXPORTS = ("edit_ortho_init", "edit_ortho_apply", "edit_ortho_local_step", "edit_ortho_destroy")
 ORTHO_FAST, ORTHO_FULL = 0, 1
+ADAMW_EXPORTS = ("edit_adamw_init", "edit_adamw_sumsq", "edit_adamw_step", "edit_adamw_pack", "edit_adamw_unpack",
+                 "edit_adamw_state_get", "edit_adamw_state_set", "edit_adamw_destroy")
+ADAMW_F32, ADAMW_E4M3 = 0, 1
+ADAMW_STOCHASTIC = 1
+ADAMW_BLOCK = 256  # elements that share a scale
 
 
 class EditOuterError(RuntimeError):
@@ -101,6 +106,46 @@ class _OrthoConfig(ctypes.Structure):
         ("precision", ctypes.c_int32),
         ("steps", ctypes.c_int32),
         ("coefficients", ctypes.POINTER(ctypes.c_double)),
+    ]
+
+
+class _AdamWConfig(ctypes.Structure):
+    _fields_ = [
+        ("num_tensors", ctypes.c_int32),
+        ("numel", ctypes.POINTER(ctypes.c_int64)),
+        ("decay", ctypes.POINTER(ctypes.c_double)),
+        ("dtype", ctypes.c_int32),
+        ("grad_dtype", ctypes.c_int32),
+        ("held", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+        ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double),
+        ("eps", ctypes.c_double),
+        ("weight_decay", ctypes.c_double),
+    ]
+
+
+class _AdamWTensors(ctypes.Structure):
+    _fields_ = [(name, ctypes.POINTER(ctypes.c_void_p)) for name in (
+        "param", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale")]
+
+
+class _AdamWCall(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_double),
+        ("lr_device", ctypes.c_void_p),
+        ("max_norm", ctypes.c_double),
+        ("sumsq", ctypes.c_void_p),
+        ("seed", ctypes.c_uint64),
+    ]
+
+
+class _AdamWState(ctypes.Structure):
+    _fields_ = [
+        ("step", ctypes.c_int64),
+        ("skipped", ctypes.c_int64),
+        ("norm", ctypes.c_double),
+        ("clip_coef", ctypes.c_double),
     ]
 
 
@@ -181,6 +226,23 @@ def load_library() -> ctypes.CDLL:
     lib.edit_ortho_destroy.restype = None
     lib.edit_outer_step_layer_ortho.argtypes = [vp, ctypes.c_int32, vp, vp, vp, ctypes.POINTER(vp), vp]
     lib.edit_outer_step_layer_ortho.restype = st
+    ptrs = ctypes.POINTER(vp)
+    lib.edit_adamw_init.argtypes = [ctypes.POINTER(_AdamWConfig), ctypes.POINTER(vp)]
+    lib.edit_adamw_init.restype = st
+    lib.edit_adamw_sumsq.argtypes = [vp, ptrs, vp, vp]
+    lib.edit_adamw_sumsq.restype = st
+    lib.edit_adamw_step.argtypes = [vp, ctypes.POINTER(_AdamWTensors), ctypes.POINTER(_AdamWCall), vp]
+    lib.edit_adamw_step.restype = st
+    lib.edit_adamw_pack.argtypes = [vp, ptrs, ptrs, ctypes.POINTER(_AdamWTensors), ctypes.c_uint64, vp]
+    lib.edit_adamw_pack.restype = st
+    lib.edit_adamw_unpack.argtypes = [vp, ctypes.POINTER(_AdamWTensors), ptrs, ptrs, vp]
+    lib.edit_adamw_unpack.restype = st
+    lib.edit_adamw_state_get.argtypes = [vp, ctypes.POINTER(_AdamWState)]
+    lib.edit_adamw_state_get.restype = st
+    lib.edit_adamw_state_set.argtypes = [vp, ctypes.c_int64]
+    lib.edit_adamw_state_set.restype = st
+    lib.edit_adamw_destroy.argtypes = [vp]
+    lib.edit_adamw_destroy.restype = None
     _lib = lib
     return lib
 
