@@ -10,8 +10,7 @@
 namespace edit {
 
 constexpr int kAdamThreads = 256;
-constexpr int kAdamVec = 8;                              // consecutive elements of a lane
-constexpr int kAdamChunk = kAdamThreads * kAdamVec;      // elements of a block: whole scale blocks
+constexpr int kAdamChunk = kAdamThreads * 8;              // elements of a block: whole scale blocks
 constexpr int kAdamTensors = 56;                         // of one launch: its table is in the kernel arguments
 constexpr int kAdamNormTensors = 192;                    // of one launch of the norm pass
 constexpr int kAdamNormVecs = 4;                         // vectors of a lane and chunk of the norm pass

@@ -18,11 +18,10 @@ namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef u32x4 u32x4_any __attribute__((aligned(2)));  // parameters and gradients begin at any element
+typedef unsigned int u32x1 __attribute__((ext_vector_type(1)));
+typedef u32x4 u32x4_any __attribute__((aligned(4)));  // parameters and gradients begin at any element
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-
-constexpr int V = kAdamVec;
 
 // The first 64 bits behind the point of sqrt(2) and of sqrt(3).
 constexpr uint64_t kMixA = 0x6A09E667F3BCC909ull, kMixB = 0xBB67AE8584CAA73Bull;
@@ -50,13 +49,29 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));  // RNE
 }
 
+// V elements of 16 bits or of 8, packed.
+template <int V>
+struct Packed;
+template <>
+struct Packed<8> {
+  typedef u32x4 Half;
+  typedef u32x2 Byte;
+};
+template <>
+struct Packed<4> {
+  typedef u32x2 Half;
+  typedef u32x1 Byte;
+};
+
 // Elements [at, at + n) of a buffer, n <= V; zeros behind them.
-template <bool BF16>
+template <bool BF16, int V>
 __device__ __forceinline__ void load_vec(const void* base, int64_t at, int n, float (&x)[V]) {
   if constexpr (BF16) {
+    typedef typename Packed<V>::Half Half;
+    typedef Half Half_any __attribute__((aligned(2)));
     const uint16_t* p = static_cast<const uint16_t*>(base) + at;
     if (n == V) {
-      const u32x4 raw = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
+      const Half raw = __builtin_nontemporal_load(reinterpret_cast<const Half_any*>(p));
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const uint32_t w = raw[e >> 1];
@@ -82,15 +97,17 @@ __device__ __forceinline__ void load_vec(const void* base, int64_t at, int n, fl
   }
 }
 
-template <bool BF16>
+template <bool BF16, int V>
 __device__ __forceinline__ void store_vec(void* base, int64_t at, int n, const float (&x)[V]) {
   if constexpr (BF16) {
+    typedef typename Packed<V>::Half Half;
+    typedef Half Half_any __attribute__((aligned(2)));
     uint16_t* p = static_cast<uint16_t*>(base) + at;
-    u32x4 raw;
+    Half raw;
 #pragma unroll
     for (int e = 0; e < V / 2; ++e) raw[e] = pack2(x[2 * e], x[2 * e + 1]);
     if (n == V) {
-      __builtin_nontemporal_store(raw, reinterpret_cast<u32x4_any*>(p));
+      __builtin_nontemporal_store(raw, reinterpret_cast<Half_any*>(p));
     } else {
 #pragma unroll
       for (int e = 0; e < V; ++e)
@@ -114,29 +131,32 @@ __device__ __forceinline__ void store_vec(void* base, int64_t at, int n, const f
   }
 }
 
-// V codes, packed.
-__device__ __forceinline__ u32x2 load_codes(const void* base, int64_t at, int n) {
+// V codes.
+template <int V, typename Byte = typename Packed<V>::Byte>
+__device__ __forceinline__ Byte load_codes(const void* base, int64_t at, int n) {
   const uint8_t* p = static_cast<const uint8_t*>(base) + at;
-  if (n == V) return __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
-  u32x2 raw = {0, 0};
+  if (n == V) return __builtin_nontemporal_load(reinterpret_cast<const Byte*>(p));
+  Byte raw = {};
 #pragma unroll
   for (int e = 0; e < V; ++e)
     if (e < n) raw[e >> 2] |= static_cast<uint32_t>(p[e]) << (8 * (e & 3));
   return raw;
 }
-__device__ __forceinline__ void store_codes(void* base, int64_t at, int n, u32x2 raw) {
+template <int V, typename Byte = typename Packed<V>::Byte>
+__device__ __forceinline__ void store_codes(void* base, int64_t at, int n, Byte raw) {
   uint8_t* p = static_cast<uint8_t*>(base) + at;
   if (n == V) {
-    __builtin_nontemporal_store(raw, reinterpret_cast<u32x2*>(p));
+    __builtin_nontemporal_store(raw, reinterpret_cast<Byte*>(p));
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e)
       if (e < n) p[e] = static_cast<uint8_t>(raw[e >> 2] >> (8 * (e & 3)));
   }
 }
-__device__ __forceinline__ void decode(u32x2 raw, float scale, float (&x)[V]) {
+template <int V, typename Byte = typename Packed<V>::Byte>
+__device__ __forceinline__ void decode(Byte raw, float scale, float (&x)[V]) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < V / 4; ++h) {
     const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(raw[h], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(raw[h], true);
     x[4 * h] = a[0] * scale, x[4 * h + 1] = a[1] * scale;
     x[4 * h + 2] = b[0] * scale, x[4 * h + 3] = b[1] * scale;
@@ -148,24 +168,31 @@ __device__ __forceinline__ uint32_t dpp_max(uint32_t x) {
   const uint32_t y = __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, true);
   return x > y ? x : y;
 }
-// Largest of the 32 lanes that share a scale: V * 32 = EDIT_ADAMW_BLOCK.
-static_assert(V * 32 == EDIT_ADAMW_BLOCK, "32 lanes share a scale");
+// Largest of the 256 / V lanes that share a scale.
+template <int V>
 __device__ __forceinline__ uint32_t block_max(uint32_t x) {
+  static_assert(EDIT_ADAMW_BLOCK == 32 * V || EDIT_ADAMW_BLOCK == 64 * V, "half a wave or a whole one");
   x = dpp_max<0xB1>(x);   // quad_perm 1 0 3 2
   x = dpp_max<0x4E>(x);   // quad_perm 2 3 0 1
   x = dpp_max<0x141>(x);  // row_half_mirror
   x = dpp_max<0x140>(x);  // row_mirror
   const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  return r[0] > r[1] ? r[0] : r[1];
+  x = max(r[0], r[1]);
+  if constexpr (EDIT_ADAMW_BLOCK == 64 * V) {
+    const auto s = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    x = max(s[0], s[1]);
+  }
+  return x;
 }
 
 // The exponent field of the block's largest finite |x|, at least 8 (so that
 // scale and 1 / scale are normal numbers).
+template <int V>
 __device__ __forceinline__ uint32_t block_exponent(const float (&x)[V]) {
   uint32_t top = 0;
 #pragma unroll
   for (int e = 0; e < V; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-  top = block_max(top);
+  top = block_max<V>(top);
   if (__builtin_expect(top >= 0x7f800000u, 0)) {  // all lanes of the block alike
     top = 0;
 #pragma unroll
@@ -173,7 +200,7 @@ __device__ __forceinline__ uint32_t block_exponent(const float (&x)[V]) {
       const uint32_t a = __float_as_uint(x[e]) & 0x7fffffffu;
       top = max(top, a < 0x7f800000u ? a : 0u);
     }
-    top = block_max(top);
+    top = block_max<V>(top);
   }
   return max(top >> 23, 8u);
 }
@@ -181,12 +208,13 @@ __device__ __forceinline__ float scale_of(uint32_t exponent) { return __uint_as_
 
 // x to 8 bits and their scale.  The conversion adds the top 20 bits of its
 // random operand below the last place kept and cuts: q floor(|y| / q + u).
-template <bool SECOND>
-__device__ __forceinline__ u32x2 encode(const float (&x)[V], uint32_t exponent, const uint32_t (&word)[V]) {
+template <bool SECOND, int V>
+__device__ __forceinline__ typename Packed<V>::Byte encode(const float (&x)[V], uint32_t exponent,
+                                                           const uint32_t (&word)[V]) {
   const float inv = __uint_as_float((261 - exponent) << 23);  // 2^(134 - exponent), exact
-  u32x2 raw = {0, 0};
+  typename Packed<V>::Byte raw = {};
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < V / 4; ++h) {
     uint32_t w = 0;
 #define EDIT_ADAMW_CODE(I)                                                                            \
   {                                                                                                   \
@@ -229,12 +257,13 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_norm_kernel(const AdamNorm
     for (int h = 0; h < kAdamNormTensors / 64; ++h) k += __popcll(__ballot(tab.first[64 * h + lane] <= c));
     const void* g = tab.grad[k];
     const int64_t n = tab.numel[k];
+    constexpr int V = 8;
     const int64_t at = static_cast<int64_t>(c - tab.first[k]) * kAdamNormChunk + threadIdx.x * V;
     float x[kAdamNormVecs][V];
 #pragma unroll
     for (int u = 0; u < kAdamNormVecs; ++u) {
       const int64_t left = n - at - u * kAdamChunk;
-      load_vec<BF16>(g, at + u * kAdamChunk, left >= V ? V : left > 0 ? static_cast<int>(left) : 0, x[u]);
+      load_vec<BF16, V>(g, at + u * kAdamChunk, left >= V ? V : left > 0 ? static_cast<int>(left) : 0, x[u]);
     }
 #pragma unroll
     for (int u = 0; u < kAdamNormVecs; ++u)
@@ -299,19 +328,24 @@ __global__ __launch_bounds__(kAdamDecideThreads) void adamw_decide_kernel(const 
   *rec = r;
 }
 
-// Which tensor, and where in it, a block of the grid works on.
+// Which tensor, and where in it, a wave of the grid works.
 struct Place {
-  int k, n;    // its index in the table; elements of this lane
-  int64_t at;  // the lane's first element
+  int k;       // index of the tensor in the table
+  int64_t at;  // first element of the wave
 };
-__device__ __forceinline__ Place place_of(const AdamTable& tab) {
-  Place p;
+__device__ __forceinline__ Place place_of(const AdamTable& tab, int chunk) {
   const int b = blockIdx.x;
+  Place p;
   p.k = __popcll(__ballot(tab.first[threadIdx.x & 63] <= b)) - 1;
-  p.at = static_cast<int64_t>(b - tab.first[p.k]) * kAdamChunk + threadIdx.x * V;
-  const int64_t left = tab.tensor[p.k].numel - p.at;
-  p.n = left >= V ? V : left > 0 ? static_cast<int>(left) : 0;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  p.at = static_cast<int64_t>(b - tab.first[p.k]) * chunk + wave * (chunk / (kAdamThreads / 64));
   return p;
+}
+// How many of the V elements from `at` on there are.
+template <int V>
+__device__ __forceinline__ int here(int64_t numel, int64_t at) {
+  const int64_t left = numel - at;
+  return left >= V ? V : left > 0 ? static_cast<int>(left) : 0;
 }
 struct Key {
   uint32_t k0, k1;
@@ -321,98 +355,121 @@ __device__ __forceinline__ Key key_of(uint64_t key, int tensor, int64_t at) {
   return {static_cast<uint32_t>(k), static_cast<uint32_t>(k >> 32) ^ (static_cast<uint32_t>(at >> 32) * 0xBB67AE85u)};
 }
 
-// One lane: 8 elements of every buffer.  PB, GB: bf16 parameters, gradients;
-// HELD: states in 8 bits; SR: bf16 parameters rounded stochastically.
-template <bool PB, bool GB, bool HELD, bool SR>
+// One lane: U times V elements of every buffer, each time next to its
+// neighbour's.  PB, GB: bf16 parameters, gradients; HELD: states in 8 bits; SR:
+// bf16 parameters rounded stochastically.
+template <bool PB, bool GB, bool HELD, bool SR, int V, int U>
 __global__ __launch_bounds__(kAdamThreads) void adamw_step_kernel(const AdamTable tab, const AdamHyper hyper,
                                                                   const AdamRecord* __restrict__ rec) {
   if (rec->skip) return;
-  const Place at = place_of(tab);
-  const AdamTensor& t = tab.tensor[at.k];
-  const int64_t block = at.at / EDIT_ADAMW_BLOCK;
-  float p[V], g[V], m[V], v[V];
-  load_vec<PB>(t.param, at.at, at.n, p);
-  load_vec<GB>(t.grad, at.at, at.n, g);
-  if constexpr (HELD) {
-    const u32x2 mc = load_codes(t.m, at.at, at.n), vc = load_codes(t.v, at.at, at.n);
-    const float ms = at.n ? t.m_scale[block] : 0.f, vs = at.n ? t.v_scale[block] : 0.f;
-    decode(mc, ms, m);
-    decode(vc, vs, v);
-  } else {
-    load_vec<false>(t.m, at.at, at.n, m);
-    load_vec<false>(t.v, at.at, at.n, v);
+  const Place place = place_of(tab, kAdamThreads * V * U);
+  const AdamTensor& t = tab.tensor[place.k];
+  int n[U];
+  int64_t at[U];
+  float p[U][V], g[U][V], m[U][V], v[U][V];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    at[u] = place.at + u * 64 * V + (threadIdx.x & 63) * V;
+    n[u] = here<V>(t.numel, at[u]);
+    load_vec<PB>(t.param, at[u], n[u], p[u]);
+    load_vec<GB>(t.grad, at[u], n[u], g[u]);
+    if constexpr (HELD) {
+      const int64_t block = at[u] / EDIT_ADAMW_BLOCK;
+      const auto mc = load_codes<V>(t.m, at[u], n[u]), vc = load_codes<V>(t.v, at[u], n[u]);
+      const float ms = n[u] ? t.m_scale[block] : 0.f, vs = n[u] ? t.v_scale[block] : 0.f;
+      decode<V>(mc, ms, m[u]);
+      decode<V>(vc, vs, v[u]);
+    } else {
+      load_vec<false>(t.m, at[u], n[u], m[u]);
+      load_vec<false>(t.v, at[u], n[u], v[u]);
+    }
   }
   const float clip = rec->clip, rate = rec->rate, root = rec->root, eps = static_cast<float>(hyper.eps);
-  const float decay = static_cast<float>(rec->lr_decay * tab.decay[at.k]);
+  const float decay = static_cast<float>(rec->lr_decay * tab.decay[place.k]);
   const double b1 = hyper.beta1, b2 = hyper.beta2, a1 = 1.0 - b1, a2 = 1.0 - b2;
+  const Key key = key_of(rec->key, tab.base + place.k, place.at);  // 2^32 is a multiple of what a wave takes
 #pragma unroll
-  for (int e = 0; e < V; ++e) {
-    const double gd = clip * g[e];
-    m[e] = static_cast<float>(__builtin_fma(b1, static_cast<double>(m[e]), a1 * gd));
-    v[e] = static_cast<float>(__builtin_fma(b2, static_cast<double>(v[e]), a2 * gd * gd));
-    // The hardware's square root is off by one place and takes values below
-    // 2^-126 as zero; beside an eps of 1e-12 at least neither is seen in p.
-    const float d = __builtin_fmaf(__builtin_amdgcn_sqrtf(v[e]), root, eps);
-    p[e] -= __builtin_fmaf(decay, p[e], rate * m[e] * __builtin_amdgcn_rcpf(d));
-  }
-  if constexpr (HELD || SR) {
-    const Key key = key_of(rec->key, tab.base + at.k, at.at);
-    uint32_t word[V];
+  for (int u = 0; u < U; ++u) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) word[e] = random_word(static_cast<uint32_t>(at.at) + e, key.k0, key.k1);
-    if constexpr (SR) {
+    for (int e = 0; e < V; ++e) {
+      const double gd = clip * g[u][e];
+      m[u][e] = static_cast<float>(__builtin_fma(b1, static_cast<double>(m[u][e]), a1 * gd));
+      v[u][e] = static_cast<float>(__builtin_fma(b2, static_cast<double>(v[u][e]), a2 * gd * gd));
+      // The hardware's square root is off by one place and takes values below
+      // 2^-126 as zero; beside an eps of 1e-12 at least neither is seen in p.
+      const float d = __builtin_fmaf(__builtin_amdgcn_sqrtf(v[u][e]), root, eps);
+      p[u][e] -= __builtin_fmaf(decay, p[u][e], rate * m[u][e] * __builtin_amdgcn_rcpf(d));
+    }
+    if constexpr (HELD || SR) {
+      uint32_t word[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) {  // what cuts the low half afterwards is exact
-        const uint32_t x = __float_as_uint(p[e]);
-        const uint32_t up = (x + (second_word(word[e], key.k0) >> 16)) & 0xffff0000u;
-        p[e] = (x & 0x7fffffffu) < 0x7f800000u ? __uint_as_float(up) : p[e];
+      for (int e = 0; e < V; ++e) word[e] = random_word(static_cast<uint32_t>(at[u]) + e, key.k0, key.k1);
+      if constexpr (SR) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {  // what cuts the low half afterwards is exact
+          const uint32_t x = __float_as_uint(p[u][e]);
+          const uint32_t up = (x + (second_word(word[e], key.k0) >> 16)) & 0xffff0000u;
+          p[u][e] = (x & 0x7fffffffu) < 0x7f800000u ? __uint_as_float(up) : p[u][e];
+        }
+      }
+      if constexpr (HELD) {
+        const uint32_t em = block_exponent(m[u]), ev = block_exponent(v[u]);
+        store_codes<V>(t.m, at[u], n[u], encode<false>(m[u], em, word));
+        store_codes<V>(t.v, at[u], n[u], encode<true>(v[u], ev, word));
+        if (at[u] % EDIT_ADAMW_BLOCK == 0 && n[u]) {
+          t.m_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(em);
+          t.v_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(ev);
+        }
       }
     }
-    if constexpr (HELD) {
-      const uint32_t em = block_exponent(m), ev = block_exponent(v);
-      const u32x2 mc = encode<false>(m, em, word), vc = encode<true>(v, ev, word);
-      store_codes(t.m, at.at, at.n, mc);
-      store_codes(t.v, at.at, at.n, vc);
-      if (at.at % EDIT_ADAMW_BLOCK == 0 && at.n) {
-        t.m_scale[block] = scale_of(em);
-        t.v_scale[block] = scale_of(ev);
-      }
+    if constexpr (!HELD) {
+      store_vec<false>(t.m, at[u], n[u], m[u]);
+      store_vec<false>(t.v, at[u], n[u], v[u]);
     }
+    store_vec<PB>(t.param, at[u], n[u], p[u]);
   }
-  if constexpr (!HELD) {
-    store_vec<false>(t.m, at.at, at.n, m);
-    store_vec<false>(t.v, at.at, at.n, v);
-  }
-  store_vec<PB>(t.param, at.at, at.n, p);
 }
 
-template <bool PACK>
+template <bool PACK, int V, int U>
 __global__ __launch_bounds__(kAdamThreads) void adamw_convert_kernel(const AdamTable tab, uint64_t key64) {
-  const Place at = place_of(tab);
-  const AdamTensor& t = tab.tensor[at.k];
-  const int64_t block = at.at / EDIT_ADAMW_BLOCK;
-  float m[V], v[V];
-  if constexpr (PACK) {
-    load_vec<false>(t.param, at.at, at.n, m);
-    load_vec<false>(t.grad, at.at, at.n, v);
-    const Key key = key_of(key64, tab.base + at.k, at.at);
-    uint32_t word[V];
+  const Place place = place_of(tab, kAdamThreads * V * U);
+  const AdamTensor& t = tab.tensor[place.k];
+  int n[U];
+  int64_t at[U];
+  float m[U][V], v[U][V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) word[e] = random_word(static_cast<uint32_t>(at.at) + e, key.k0, key.k1);
-    const uint32_t em = block_exponent(m), ev = block_exponent(v);
-    store_codes(t.m, at.at, at.n, encode<false>(m, em, word));
-    store_codes(t.v, at.at, at.n, encode<true>(v, ev, word));
-    if (at.at % EDIT_ADAMW_BLOCK == 0 && at.n) {
-      t.m_scale[block] = scale_of(em);
-      t.v_scale[block] = scale_of(ev);
+  for (int u = 0; u < U; ++u) {
+    at[u] = place.at + u * 64 * V + (threadIdx.x & 63) * V;
+    n[u] = here<V>(t.numel, at[u]);
+    if constexpr (PACK) {
+      load_vec<false>(t.param, at[u], n[u], m[u]);
+      load_vec<false>(t.grad, at[u], n[u], v[u]);
+    } else {
+      const int64_t block = at[u] / EDIT_ADAMW_BLOCK;
+      const auto mc = load_codes<V>(t.m, at[u], n[u]), vc = load_codes<V>(t.v, at[u], n[u]);
+      const float ms = n[u] ? t.m_scale[block] : 0.f, vs = n[u] ? t.v_scale[block] : 0.f;
+      decode<V>(mc, ms, m[u]);
+      decode<V>(vc, vs, v[u]);
     }
-  } else {
-    const u32x2 mc = load_codes(t.m, at.at, at.n), vc = load_codes(t.v, at.at, at.n);
-    const float ms = at.n ? t.m_scale[block] : 0.f, vs = at.n ? t.v_scale[block] : 0.f;
-    decode(mc, ms, m);
-    decode(vc, vs, v);
-    store_vec<false>(t.param, at.at, at.n, m);
-    store_vec<false>(const_cast<void*>(t.grad), at.at, at.n, v);
+  }
+  const Key key = key_of(key64, tab.base + place.k, place.at);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if constexpr (PACK) {
+      uint32_t word[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) word[e] = random_word(static_cast<uint32_t>(at[u]) + e, key.k0, key.k1);
+      const uint32_t em = block_exponent(m[u]), ev = block_exponent(v[u]);
+      store_codes<V>(t.m, at[u], n[u], encode<false>(m[u], em, word));
+      store_codes<V>(t.v, at[u], n[u], encode<true>(v[u], ev, word));
+      if (at[u] % EDIT_ADAMW_BLOCK == 0 && n[u]) {
+        t.m_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(em);
+        t.v_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(ev);
+      }
+    } else {
+      store_vec<false>(t.param, at[u], n[u], m[u]);
+      store_vec<false>(const_cast<void*>(t.grad), at[u], n[u], v[u]);
+    }
   }
 }
 
@@ -423,9 +480,11 @@ hipError_t launch(void (*kernel)(A...), int blocks, int threads, hipStream_t str
   return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(blocks), dim3(threads), at, 0, stream);
 }
 
+constexpr int step_vec(bool pb, bool gb, bool held) { return pb && gb && held ? 8 : 4; }
+
 template <bool PB, bool GB, bool HELD, bool SR>
 hipError_t step(int blocks, const AdamTable& table, const AdamHyper& hyper, const AdamRecord* rec, hipStream_t stream) {
-  return launch<AdamTable, AdamHyper, const AdamRecord*>(adamw_step_kernel<PB, GB, HELD, SR>, blocks, kAdamThreads, stream,
+  return launch<AdamTable, AdamHyper, const AdamRecord*>(adamw_step_kernel<PB, GB, HELD, SR, step_vec(PB, GB, HELD), 8 / step_vec(PB, GB, HELD)>, blocks, kAdamThreads, stream,
                                                          table, hyper, rec);
 }
 
@@ -469,7 +528,7 @@ hipError_t launch_adamw_step(bool param_bf16, bool grad_bf16, bool held, bool st
 }
 
 hipError_t launch_adamw_convert(bool pack, int blocks, const AdamTable& table, uint64_t key, hipStream_t stream) {
-  return launch<AdamTable, uint64_t>(pack ? adamw_convert_kernel<true> : adamw_convert_kernel<false>, blocks, kAdamThreads,
+  return launch<AdamTable, uint64_t>(pack ? adamw_convert_kernel<true, 4, 2> : adamw_convert_kernel<false, 4, 2>, blocks, kAdamThreads,
                                      stream, table, key);
 }
 
