@@ -529,7 +529,7 @@ typedef struct edit_adamw *edit_adamw_t; /* opaque, library-owned */
 
 typedef struct {
   int32_t num_tensors;  /* >= 0                                               */
-  const int64_t *numel; /* [num_tensors], 0..2^34 each; copied at init         */
+  const int64_t *numel; /* [num_tensors], 0..2^33 each; copied at init         */
   const double *decay;  /* [num_tensors] d_k, finite and >= 0; NULL: 1 for all */
   int32_t dtype;        /* edit_dtype_t of the parameters                      */
   int32_t grad_dtype;   /* edit_dtype_t of the gradients                       */

@@ -287,6 +287,7 @@ class AdamWPlan(GradPlan):
         self._params = list(params)
         self._tensors = _AdamWTensors(handle._pointers(self._params, handle._dtype, "params"), self._grad,
                                       *handle._state_pointers(state))
+        self._call_args = _AdamWCall()
         # the tensors, whatever becomes of the caller's lists
         self._state = [list(x or []) for x in (state.exp_avg, state.exp_avg_sq, state.exp_avg_scale, state.exp_avg_sq_scale)]
 
@@ -300,13 +301,12 @@ class AdamWPlan(GradPlan):
         h = self._handle
         if max_norm is not None and not (max_norm > 0.0 and math.isfinite(max_norm)):
             raise ValueError("max_norm must be finite and > 0, or None")
-        call = _AdamWCall(0.0, None, 0.0 if max_norm is None else float(max_norm), None, _seed(seed))
-        if isinstance(lr, torch.Tensor):
-            call.lr_device = _scalar(h, lr, "lr")
-        else:
-            call.lr = float(lr)
-        if sumsq is not None:
-            call.sumsq = _scalar(h, sumsq, "sumsq")
+        call = self._call_args
+        device_lr = isinstance(lr, torch.Tensor)
+        call.lr, call.lr_device = (0.0, _scalar(h, lr, "lr")) if device_lr else (float(lr), None)
+        call.max_norm = 0.0 if max_norm is None else float(max_norm)
+        call.sumsq = None if sumsq is None else _scalar(h, sumsq, "sumsq")
+        call.seed = _seed(seed)
         h._call(h._lib.edit_adamw_step, "edit_adamw_step", ctypes.byref(self._tensors), ctypes.byref(call),
                 _stream_handle(stream, h.device))
 

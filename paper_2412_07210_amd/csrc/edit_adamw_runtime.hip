@@ -27,14 +27,29 @@ edit_status_t afail_hip(hipError_t e, const char* what) {
   return afail(EDIT_EHIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
-constexpr int64_t kMaxNumel = int64_t(1) << 34;
-constexpr int64_t kMaxBlocks = kMaxNumel / kAdamChunk;  // of a launch: fewer than 2^32 threads
+constexpr int64_t kMaxNumel = int64_t(1) << 33;
+constexpr int64_t kMaxBlocks = (int64_t(1) << 32) / kAdamThreads - 1;  // of a launch: fewer than 2^32 threads
+static_assert(kMaxNumel / (kAdamThreads * 4) <= kMaxBlocks, "a tensor fits a launch");
 
 int64_t chunks_of(int64_t numel, int64_t chunk) { return (numel + chunk - 1) / chunk; }
 
 struct Range {
   uintptr_t lo, hi;
 };
+
+// Buffers of one kind, as a call lists them.
+struct Kind {
+  std::vector<Range> ranges;
+  uintptr_t lo = UINTPTR_MAX, hi = 0;  // around all of them
+  bool ascending = true;               // and disjoint
+  void clear() { ranges.clear(), lo = UINTPTR_MAX, hi = 0, ascending = true; }
+  void add(Range r) {
+    ascending = ascending && r.lo >= hi;
+    lo = std::min(lo, r.lo), hi = std::max(hi, r.hi);
+    ranges.push_back(r);
+  }
+};
+constexpr int kKinds = 6;  // parameters, gradients, m, v and their scales; of a conversion the fp32 m and v first
 
 }  // namespace
 
@@ -47,7 +62,8 @@ struct edit_adamw {
   int device = 0, num_cu = 0;
   AdamRecord* rec = nullptr;
   double* partials = nullptr;  // a norm launch's follow the one's before
-  std::vector<Range> written, read;  // of the call being checked
+  Kind kind[kKinds];  // of the call being checked
+  std::vector<Range> written, read;
 };
 
 namespace {
@@ -71,7 +87,7 @@ edit_status_t check_adamw_config(const edit_adamw_config_t* cfg) {
   for (int k = 0; k < cfg->num_tensors; ++k) {
     const std::string at = "[" + std::to_string(k) + "]";
     if (cfg->numel[k] < 0) return afail(EDIT_EINVAL, "numel" + at + " is negative");
-    if (cfg->numel[k] > kMaxNumel) return afail(EDIT_EINVAL, "numel" + at + " must be at most 2^34");
+    if (cfg->numel[k] > kMaxNumel) return afail(EDIT_EINVAL, "numel" + at + " must be at most 2^33");
     if (cfg->decay && (!(cfg->decay[k] >= 0.0) || !std::isfinite(cfg->decay[k])))
       return afail(EDIT_EINVAL, "decay" + at + " must be finite and >= 0");
   }
@@ -89,25 +105,38 @@ edit_status_t check_adamw_device(const edit_adamw* h) {
 }
 
 // Notes the buffer of tensor k for the check of overlaps.
-edit_status_t note(std::vector<Range>* ranges, const void* p, int64_t bytes, uintptr_t align, const char* name, int k) {
+edit_status_t note(Kind* kind, const void* p, int64_t bytes, uintptr_t align, const char* name, int k) {
   const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
   if (!p || (lo & (align - 1))) {
     const std::string what = std::string(name) + "[" + std::to_string(k) + "]";
     if (!p) return afail(EDIT_EINVAL, what + " must not be NULL");
     return afail(EDIT_EINVAL, what + " must be " + std::to_string(align) + "-byte aligned");
   }
-  ranges->push_back({lo, lo + static_cast<uintptr_t>(bytes)});
+  kind->add({lo, lo + static_cast<uintptr_t>(bytes)});
   return EDIT_OK;
 }
 
-// What is written overlaps nothing.
-edit_status_t check_overlaps(edit_adamw* h) {
-  auto less = [](const Range& a, const Range& b) { return a.lo < b.lo; };
-  std::sort(h->written.begin(), h->written.end(), less);
-  std::sort(h->read.begin(), h->read.end(), less);
+// What is written overlaps nothing; `writes`: a bit for each kind that is.
+edit_status_t check_overlaps(edit_adamw* h, unsigned writes) {
+  // Mostly every kind lies in a stretch of its own, in order: nothing to sort.
+  bool clear = true;
+  for (int i = 0; i < kKinds; ++i) {
+    const Kind& a = h->kind[i];
+    clear = clear && (a.ascending || !(writes >> i & 1));
+    for (int j = 0; j < i; ++j)
+      if ((writes >> i | writes >> j) & 1) clear = clear && (a.hi <= h->kind[j].lo || h->kind[j].hi <= a.lo);
+  }
+  if (clear) return EDIT_OK;
+  h->written.clear();
+  h->read.clear();
+  for (int i = 0; i < kKinds; ++i) {
+    std::vector<Range>& to = writes >> i & 1 ? h->written : h->read;
+    to.insert(to.end(), h->kind[i].ranges.begin(), h->kind[i].ranges.end());
+  }
+  std::sort(h->written.begin(), h->written.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
   for (size_t i = 1; i < h->written.size(); ++i)
     if (h->written[i].lo < h->written[i - 1].hi)
-      return afail(EDIT_EINVAL, "parameters and states must not overlap (the same tensor twice?)");
+      return afail(EDIT_EINVAL, "what is written must not overlap: parameters and states, or one of them twice");
   // written ranges are disjoint, so ascending at both ends
   for (const Range& r : h->read) {
     const auto it = std::upper_bound(h->written.begin(), h->written.end(), r.lo,
@@ -117,13 +146,13 @@ edit_status_t check_overlaps(edit_adamw* h) {
   return EDIT_OK;
 }
 
-edit_status_t check_states(edit_adamw* h, const edit_adamw_tensors_t* t, std::vector<Range>* ranges, int k) {
+edit_status_t check_states(edit_adamw* h, const edit_adamw_tensors_t* t, int k) {
   const int64_t n = h->numel[k], bytes = h->held ? n : 4 * n, scales = 4 * chunks_of(n, EDIT_ADAMW_BLOCK);
-  ADAM_TRY(note(ranges, t->exp_avg[k], bytes, 16, "exp_avg", k));
-  ADAM_TRY(note(ranges, t->exp_avg_sq[k], bytes, 16, "exp_avg_sq", k));
+  ADAM_TRY(note(&h->kind[2], t->exp_avg[k], bytes, 16, "exp_avg", k));
+  ADAM_TRY(note(&h->kind[3], t->exp_avg_sq[k], bytes, 16, "exp_avg_sq", k));
   if (h->held) {
-    ADAM_TRY(note(ranges, t->exp_avg_scale[k], scales, 4, "exp_avg_scale", k));
-    ADAM_TRY(note(ranges, t->exp_avg_sq_scale[k], scales, 4, "exp_avg_sq_scale", k));
+    ADAM_TRY(note(&h->kind[4], t->exp_avg_scale[k], scales, 4, "exp_avg_scale", k));
+    ADAM_TRY(note(&h->kind[5], t->exp_avg_sq_scale[k], scales, 4, "exp_avg_sq_scale", k));
   }
   return EDIT_OK;
 }
@@ -145,7 +174,7 @@ edit_status_t enqueue_norm(edit_adamw* h, const void* const* grad, int* count, h
     int64_t chunks = 0;
     for (; k < tensors && used < kAdamNormTensors; ++k) {
       if (!grad[k] || h->numel[k] == 0) continue;
-      const int64_t more = chunks_of(h->numel[k], kAdamNormChunk);
+      const int64_t more = chunks_of(h->numel[k], adamw_norm_chunk(h->grad_bf16));
       if (chunks + more > INT32_MAX / 2) break;
       t.first[used] = static_cast<int32_t>(chunks);
       t.numel[used] = h->numel[k];
@@ -163,33 +192,33 @@ edit_status_t enqueue_norm(edit_adamw* h, const void* const* grad, int* count, h
   return EDIT_OK;
 }
 
-// Calls launch(blocks, table) for every table of tensors; fill(k, &tensor): whether tensor k takes part.
+// Calls launch(blocks, table) for every table of tensors, the last ones first;
+// fill(k, &tensor): whether tensor k takes part; chunk: elements of a block.
 template <typename Fill, typename Launch>
-edit_status_t for_tables(const edit_adamw* h, const Fill& fill, const Launch& launch) {
-  const int tensors = static_cast<int>(h->numel.size());
-  for (int k = 0; k < tensors;) {
-    AdamTable t;
-    int used = 0, skipped = 0;
+edit_status_t for_tables(const edit_adamw* h, int chunk, const Fill& fill, const Launch& launch) {
+  for (int end = static_cast<int>(h->numel.size()), begin = end; end > 0; end = begin) {
     int64_t blocks = 0;
-    t.base = k;
-    // a tensor that takes no part keeps its place, so that base + place is its index
-    for (; k < tensors && used < kAdamTensors; ++k) {
-      AdamTensor& to = t.tensor[used];
-      const int64_t more = chunks_of(h->numel[k], kAdamChunk);
+    for (; begin > 0 && end - begin < kAdamTensors; --begin) {
+      const int64_t more = chunks_of(h->numel[begin - 1], chunk);
       if (blocks + more > kMaxBlocks) break;
-      t.first[used] = static_cast<int32_t>(blocks);
-      t.decay[used] = h->decay[k];
-      to = {};
-      if (more && fill(k, &to)) {
-        to.numel = h->numel[k];
-        blocks += more;
-      } else {
-        ++skipped;
-      }
-      ++used;
+      blocks += more;
     }
-    if (skipped == used) continue;
-    std::fill(t.first + used, t.first + 64, INT32_MAX);
+    AdamTable t;
+    t.base = begin;
+    blocks = 0;
+    // a tensor that takes no part keeps its place, so that base + place is its index
+    for (int k = begin; k < end; ++k) {
+      AdamTensor& to = t.tensor[k - begin];
+      t.first[k - begin] = static_cast<int32_t>(blocks);
+      t.decay[k - begin] = h->decay[k];
+      to = {};
+      if (h->numel[k] && fill(k, &to)) {
+        to.numel = h->numel[k];
+        blocks += chunks_of(h->numel[k], chunk);
+      }
+    }
+    if (blocks == 0) continue;
+    std::fill(t.first + (end - begin), t.first + 64, INT32_MAX);
     const hipError_t e = launch(static_cast<int>(blocks), t);
     if (e != hipSuccess) return afail_hip(e, "update pass launch");
   }
@@ -213,19 +242,17 @@ edit_status_t convert(edit_adamw* h, bool pack, const edit_adamw_tensors_t* t, c
   ADAM_TRY(check_adamw_device(h));
   if (h->numel.empty()) return EDIT_OK;
   ADAM_TRY(check_state_arrays(h, t));
-  h->written.clear();
-  h->read.clear();
-  for (size_t k = 0; k < h->numel.size(); ++k) {
+  for (Kind& kind : h->kind) kind.clear();
+  for (int k = 0; k < static_cast<int>(h->numel.size()); ++k) {
     const int64_t n = h->numel[k];
     if (n == 0) continue;
-    const int i = static_cast<int>(k);
-    ADAM_TRY(note(pack ? &h->read : &h->written, m[k], 4 * n, 16, "fp32 exp_avg", i));
-    ADAM_TRY(note(pack ? &h->read : &h->written, v[k], 4 * n, 16, "fp32 exp_avg_sq", i));
-    ADAM_TRY(check_states(h, t, pack ? &h->written : &h->read, i));
+    ADAM_TRY(note(&h->kind[0], m[k], 4 * n, 16, "fp32 exp_avg", k));
+    ADAM_TRY(note(&h->kind[1], v[k], 4 * n, 16, "fp32 exp_avg_sq", k));
+    ADAM_TRY(check_states(h, t, k));
   }
-  ADAM_TRY(check_overlaps(h));
+  ADAM_TRY(check_overlaps(h, pack ? 0x3cu : 0x03u));
   return for_tables(
-      h,
+      h, kAdamConvertChunk,
       [&](int k, AdamTensor* to) {
         fill_states(h, t, k, to);
         to->param = const_cast<float*>(m[k]);
@@ -260,11 +287,12 @@ edit_status_t edit_adamw_init(const edit_adamw_config_t* cfg, edit_adamw_t* out)
     h->weight_decay = cfg->weight_decay;
     h->device = dev;
     h->num_cu = num_cu;
-    h->written.reserve(5 * tensors);
-    h->read.reserve(4 * tensors);
+    for (Kind& kind : h->kind) kind.ranges.reserve(tensors + 1);
+    h->written.reserve(5 * tensors + 1);
+    h->read.reserve(4 * tensors + 1);
     // launches of the norm pass: full tables, and ones that end at their count of chunks
     int64_t chunks = 0;
-    for (int64_t n : h->numel) chunks += chunks_of(n, kAdamNormChunk);
+    for (int64_t n : h->numel) chunks += chunks_of(n, adamw_norm_chunk(false));
     const size_t launches = tensors / kAdamNormTensors + 2 + static_cast<size_t>(2 * (chunks / (INT32_MAX / 2)));
     const size_t partials = launches * kAdamNormBlocksPerCu * num_cu * sizeof(double);
     char* arena = nullptr;
@@ -289,13 +317,12 @@ edit_status_t edit_adamw_sumsq(edit_adamw_t h, const void* const* grad, double* 
   if (!h) return afail(EDIT_EINVAL, "NULL handle");
   if (!h->numel.empty() && !grad) return afail(EDIT_EINVAL, "grad must not be NULL");
   ADAM_TRY(check_adamw_device(h));
-  h->written.clear();
-  h->read.clear();
-  ADAM_TRY(note(&h->written, sumsq, 8, 8, "sumsq", 0));
+  for (Kind& kind : h->kind) kind.clear();
+  ADAM_TRY(note(&h->kind[0], sumsq, 8, 8, "sumsq", 0));
   const int64_t size = h->grad_bf16 ? 2 : 4;
   for (size_t k = 0; k < h->numel.size(); ++k)
-    if (h->numel[k] && grad[k]) ADAM_TRY(note(&h->read, grad[k], size * h->numel[k], size, "grad", static_cast<int>(k)));
-  ADAM_TRY(check_overlaps(h));
+    if (h->numel[k] && grad[k]) ADAM_TRY(note(&h->kind[1], grad[k], size * h->numel[k], size, "grad", static_cast<int>(k)));
+  ADAM_TRY(check_overlaps(h, 1u));
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   int count = 0;
   ADAM_TRY(enqueue_norm(h, grad, &count, s));
@@ -314,8 +341,7 @@ edit_status_t edit_adamw_step(edit_adamw_t h, const edit_adamw_tensors_t* t, con
     return afail(EDIT_EINVAL, "max_norm must be finite and > 0, or 0 for no clip");
   ADAM_TRY(check_adamw_device(h));
   const int tensors = static_cast<int>(h->numel.size());
-  h->written.clear();
-  h->read.clear();
+  for (Kind& kind : h->kind) kind.clear();
   if (tensors > 0) {
     if (!t->param || !t->grad) return afail(EDIT_EINVAL, "param and grad must not be NULL");
     ADAM_TRY(check_state_arrays(h, t));
@@ -324,11 +350,11 @@ edit_status_t edit_adamw_step(edit_adamw_t h, const edit_adamw_tensors_t* t, con
   for (int k = 0; k < tensors; ++k) {
     const int64_t n = h->numel[k];
     if (n == 0 || !t->grad[k]) continue;
-    ADAM_TRY(note(&h->written, t->param[k], pb * n, pb, "param", k));
-    ADAM_TRY(note(&h->read, t->grad[k], gb * n, gb, "grad", k));
-    ADAM_TRY(check_states(h, t, &h->written, k));
+    ADAM_TRY(note(&h->kind[0], t->param[k], pb * n, pb, "param", k));
+    ADAM_TRY(note(&h->kind[1], t->grad[k], gb * n, gb, "grad", k));
+    ADAM_TRY(check_states(h, t, k));
   }
-  ADAM_TRY(check_overlaps(h));
+  ADAM_TRY(check_overlaps(h, 0x3du));
 
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   AdamCall c = {};
@@ -343,7 +369,7 @@ edit_status_t edit_adamw_step(edit_adamw_t h, const edit_adamw_tensors_t* t, con
   const hipError_t e = launch_adamw_decide(h->partials, count, call->sumsq, c, h->hyper, h->rec, s);
   if (e != hipSuccess) return afail_hip(e, "decision launch");
   return for_tables(
-      h,
+      h, adamw_chunk(h->param_bf16, h->grad_bf16, h->held),
       [&](int k, AdamTensor* to) {
         if (!t->grad[k]) return false;
         to->param = t->param[k];

@@ -71,7 +71,7 @@ def _init(numel=(64, 8), decay=None, null_numel=False, **over):
     (dict(num_tensors=-1), "num_tensors"),
     (dict(null_numel=True), "numel must not be NULL"),
     (dict(numel=(3, -1)), "numel[1] is negative"),
-    (dict(numel=(2 ** 34 + 1,)), "2^34"),
+    (dict(numel=(2 ** 33 + 1,)), "2^33"),
     (dict(dtype=2), "dtype"),
     (dict(grad_dtype=-1), "grad_dtype"),
     (dict(held=2), "held"),
@@ -100,7 +100,7 @@ def test_init_refuses(over, needle):
 
 @pytest.mark.skipif(torch.cuda.is_available(), reason="the CPU's answer to a good configuration")
 @pytest.mark.parametrize("over", [
-    dict(), dict(numel=()), dict(numel=(), null_numel=True), dict(numel=(0, 0, 5)), dict(numel=(2 ** 34,)),
+    dict(), dict(numel=()), dict(numel=(), null_numel=True), dict(numel=(0, 0, 5)), dict(numel=(2 ** 33,)),
     dict(dtype=0, grad_dtype=1, held=1), dict(flags=1), dict(beta1=0.0, beta2=0.0), dict(eps=1e-12),
     dict(decay=(0.0, 2.5)),
 ])
