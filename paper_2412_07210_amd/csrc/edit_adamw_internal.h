@@ -18,30 +18,33 @@ constexpr int kAdamDecideThreads = 512;
 // A lane of the update pass takes V consecutive elements of every buffer, U
 // times, the next V beside its neighbour's: a block V * U * 64.  Eight bf16 and
 // eight codes are 16 and 8 bytes; with fp32 buffers four, as 16-byte accesses
-// 32 bytes apart run at half the rate.  Then twice for 8-bit states, whose loads
-// are short, once for fp32 ones.  us for 308M elements, V U = 8 1, 4 2 and 4 1:
-// bf16 parameters and gradients with e4m3 states 506, 583 and 683; fp32 and
-// bf16 800, 732 and 729 (770, 696 and 729 with the best cap); fp32 states, 4 2
-// and 4 1: bf16 1148 and 1039, fp32 1506 and 1368.  Blocks of 256 threads take
-// 0 to 2% more.
+// 32 bytes apart run at half the rate.  Twice for 8-bit states, whose loads are
+// short, once for fp32 ones.  us for 308M elements at the best cap below: e4m3
+// states with bf16 parameters and gradients, V U = 8 1 and 8 2, 530 and 508 (4 2
+// 10% more); fp32 and bf16, 8 1, 4 1 and 4 2, 770, 689 and 693; fp32 states, 4 1
+// and 4 2: bf16 1039 and 1105, fp32 1305 and 1515.  Blocks of 256 threads take 0
+// to 2% more.
 constexpr int adamw_vec(bool param_bf16, bool grad_bf16, bool held) { return param_bf16 && grad_bf16 && held ? 8 : 4; }
-constexpr int adamw_times(bool param_bf16, bool grad_bf16, bool held) {
-  return held && adamw_vec(param_bf16, grad_bf16, held) == 4 ? 2 : 1;
-}
+constexpr int adamw_times(bool held) { return held ? 2 : 1; }
 constexpr int adamw_chunk(bool param_bf16, bool grad_bf16, bool held) {
-  return kAdamThreads * adamw_vec(param_bf16, grad_bf16, held) * adamw_times(param_bf16, grad_bf16, held);
+  return kAdamThreads * adamw_vec(param_bf16, grad_bf16, held) * adamw_times(held);
 }
 // Blocks of it that run on a CU, of the 32 that fit: the mix of reads and writes
-// runs faster with fewer of its loads in flight.  us uncapped, at 24, 20 and 16:
-// e4m3 states: bf16 506, 559, 610, 724; bf16 and fp32 gradients 588, 620, 675,
-// 796; fp32 and bf16 732, 696, 702, 810; fp32 809, 798, 778, 759.  fp32 states:
-// bf16 1039, 1059, 1145, 1346; bf16 and fp32 1147, 1117, 1171, 1369; fp32 and
-// bf16 1253, 1225, 1245, 1396; fp32 1368, 1322, 1311, 1431.
+// runs faster with fewer of its loads in flight.  us uncapped, capped and (two
+// blocks a CU more and fewer): e4m3 states: bf16 511, 508 (510, 513); bf16 and
+// fp32 gradients 604, none (613 at 22); fp32 and bf16 715, 693 (696, 697); fp32
+// 820, 787 (795, 790).  fp32 states: bf16 1096, 1039 (1045, 1051); bf16 and fp32
+// 1199, 1129 (1143, 1152); fp32 and bf16 1309, 1221 (1231, 1224); fp32 1365, 1307
+// (1308, 1320).
 constexpr int adamw_resident(bool param_bf16, bool grad_bf16, bool held) {
-  if (held) return param_bf16 ? 32 : grad_bf16 ? 24 : 16;
-  return param_bf16 && grad_bf16 ? 32 : param_bf16 || grad_bf16 ? 24 : 20;
+  if (held) return param_bf16 ? (grad_bf16 ? 22 : 32) : grad_bf16 ? 20 : 18;
+  return param_bf16 && grad_bf16 ? 16 : param_bf16 || grad_bf16 ? 14 : 12;
 }
-constexpr int kAdamConvertChunk = kAdamThreads * 8;
+// Conversions: a lane takes four elements once to pack (308M elements in 461 us;
+// twice 475), twice to unpack, capped (493; 611 uncapped, once 511).
+constexpr int adamw_convert_times(bool pack) { return pack ? 1 : 2; }
+constexpr int adamw_convert_chunk(bool pack) { return kAdamThreads * 4 * adamw_convert_times(pack); }
+constexpr int kAdamUnpackResident = 18;
 
 // The norm pass: persistent blocks that stride over chunks, a lane kAdamNormVecs
 // 16-byte vectors of one, the next chunk's in flight.
@@ -59,8 +62,7 @@ struct alignas(16) AdamRecord {
   double lr_decay;   // lr * weight_decay of this call
   uint64_t key;      // of this call's random numbers
   float clip;        // c
-  float rate;        // lr / (1 - beta1^t)
-  float root;        // 1 / sqrt(1 - beta2^t)
+  float root, eps;   // 1 / sqrt(1 - beta2^t) and eps, over lr / (1 - beta1^t)
   int32_t skip;      // this call changes nothing
 };
 

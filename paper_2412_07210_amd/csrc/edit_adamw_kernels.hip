@@ -11,6 +11,8 @@
 // All of them are bound by memory.  m and v are taken in fp64 and rounded once
 // to fp32, so that what is rounded to 8 bits afterwards does not depend on the
 // order of operations; fp64 multiply-adds run at the rate of fp32 ones here.
+#include <type_traits>
+
 #include "edit_adamw_internal.h"
 
 namespace edit {
@@ -18,8 +20,6 @@ namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned int u32x1 __attribute__((ext_vector_type(1)));
-typedef u32x4 u32x4_any __attribute__((aligned(4)));  // parameters and gradients begin at any element
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
@@ -32,11 +32,11 @@ __host__ __device__ __forceinline__ uint64_t mix(uint64_t z) {
   return z ^ (z >> 32);
 }
 
-// 32 random bits of the element whose low word is `element`; key: of its
-// tensor, its high word mixed with the element's.
-__device__ __forceinline__ uint32_t random_word(uint32_t element, uint32_t k0, uint32_t k1) {
-  uint32_t x = (element ^ k0) * 0xBB67AE85u;
-  x = (x ^ (x >> 17) ^ k1) * 0x6A09E667u;
+// 32 random bits of an element: `mixed`, its low word ^ the key's; k1: the high
+// words of both.
+__device__ __forceinline__ uint32_t random_word(uint32_t mixed, uint32_t k1) {
+  uint32_t x = mixed * 0xBB67AE85u;
+  x = __builtin_amdgcn_bitop3_b32(x, x >> 17, k1, 0x96) * 0x6A09E667u;  // x ^ (x >> 17) ^ k1
   return x ^ (x >> 15);
 }
 __device__ __forceinline__ uint32_t second_word(uint32_t w, uint32_t k0) {
@@ -44,122 +44,101 @@ __device__ __forceinline__ uint32_t second_word(uint32_t w, uint32_t k0) {
   return y ^ (y >> 15);
 }
 
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  const f32x2 f = {a, b};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));  // RNE
-}
-
-// V elements of 16 bits or of 8, packed.
-template <int V>
-struct Packed;
-template <>
-struct Packed<8> {
-  typedef u32x4 Half;
-  typedef u32x2 Byte;
+// V elements of a buffer as they lie in memory.
+template <bool BF16, int V>
+struct RawOf {
+  typedef u32x4 T;  // 8 bf16 or 4 fp32
+  static_assert(V == (BF16 ? 8 : 4), "16 bytes, or 4 bf16");
 };
 template <>
-struct Packed<4> {
-  typedef u32x2 Half;
-  typedef u32x1 Byte;
+struct RawOf<true, 4> {
+  typedef u32x2 T;
 };
-
-// Elements [at, at + n) of a buffer, n <= V; zeros behind them.
 template <bool BF16, int V>
-__device__ __forceinline__ void load_vec(const void* base, int64_t at, int n, float (&x)[V]) {
-  if constexpr (BF16) {
-    typedef typename Packed<V>::Half Half;
-    typedef Half Half_any __attribute__((aligned(2)));
-    const uint16_t* p = static_cast<const uint16_t*>(base) + at;
-    if (n == V) {
-      const Half raw = __builtin_nontemporal_load(reinterpret_cast<const Half_any*>(p));
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const uint32_t w = raw[e >> 1];
-        x[e] = __uint_as_float((e & 1) ? (w & 0xffff0000u) : (w << 16));
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < V; ++e) x[e] = e < n ? __uint_as_float(static_cast<uint32_t>(p[e]) << 16) : 0.f;
-    }
-  } else {
-    const float* p = static_cast<const float*>(base) + at;
-    if (n == V) {
-#pragma unroll
-      for (int h = 0; h < V / 4; ++h) {
-        const u32x4 raw = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p) + h);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * h + e] = __uint_as_float(raw[e]);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < V; ++e) x[e] = e < n ? p[e] : 0.f;
-    }
-  }
-}
+using Raw = typename RawOf<BF16, V>::T;
 
-template <bool BF16, int V>
-__device__ __forceinline__ void store_vec(void* base, int64_t at, int n, const float (&x)[V]) {
-  if constexpr (BF16) {
-    typedef typename Packed<V>::Half Half;
-    typedef Half Half_any __attribute__((aligned(2)));
-    uint16_t* p = static_cast<uint16_t*>(base) + at;
-    Half raw;
+// Elements [at, at + V) of a buffer of `numel` > 0, zeros behind its end; FULL:
+// all of them are there.  Parameters and gradients begin at any element.  Next to
+// the end the elements are loaded one by one, the last one in place of those
+// behind it, so that no load waits for a branch.
+template <bool FULL, bool BF16, int V>
+__device__ __forceinline__ Raw<BF16, V> load_raw(const void* base, int64_t at, int64_t numel) {
+  typedef Raw<BF16, V> T;
+  typedef T T_any __attribute__((aligned(BF16 ? 2 : 4)));
+  typedef typename std::conditional<BF16, uint16_t, uint32_t>::type E;
+  const E* p = static_cast<const E*>(base);
+  if constexpr (FULL) return __builtin_nontemporal_load(reinterpret_cast<const T_any*>(p + at));
+  T raw = {};
 #pragma unroll
-    for (int e = 0; e < V / 2; ++e) raw[e] = pack2(x[2 * e], x[2 * e + 1]);
-    if (n == V) {
-      __builtin_nontemporal_store(raw, reinterpret_cast<Half_any*>(p));
-    } else {
-#pragma unroll
-      for (int e = 0; e < V; ++e)
-        if (e < n) p[e] = static_cast<uint16_t>(raw[e >> 1] >> (16 * (e & 1)));
-    }
-  } else {
-    float* p = static_cast<float*>(base) + at;
-    if (n == V) {
-#pragma unroll
-      for (int h = 0; h < V / 4; ++h) {
-        u32x4 raw;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) raw[e] = __float_as_uint(x[4 * h + e]);
-        __builtin_nontemporal_store(raw, reinterpret_cast<u32x4_any*>(p) + h);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < V; ++e)
-        if (e < n) p[e] = x[e];
-    }
+  for (int e = 0; e < V; ++e) {
+    const bool in = at + e < numel;
+    const uint32_t x = p[in ? at + e : numel - 1];
+    raw[BF16 ? e >> 1 : e] |= (in ? x : 0u) << (BF16 ? 16 * (e & 1) : 0);
   }
-}
-
-// V codes.
-template <int V, typename Byte = typename Packed<V>::Byte>
-__device__ __forceinline__ Byte load_codes(const void* base, int64_t at, int n) {
-  const uint8_t* p = static_cast<const uint8_t*>(base) + at;
-  if (n == V) return __builtin_nontemporal_load(reinterpret_cast<const Byte*>(p));
-  Byte raw = {};
-#pragma unroll
-  for (int e = 0; e < V; ++e)
-    if (e < n) raw[e >> 2] |= static_cast<uint32_t>(p[e]) << (8 * (e & 3));
   return raw;
 }
-template <int V, typename Byte = typename Packed<V>::Byte>
-__device__ __forceinline__ void store_codes(void* base, int64_t at, int n, Byte raw) {
-  uint8_t* p = static_cast<uint8_t*>(base) + at;
-  if (n == V) {
-    __builtin_nontemporal_store(raw, reinterpret_cast<Byte*>(p));
+template <bool FULL, bool BF16, int V>
+__device__ __forceinline__ void store_raw(void* base, int64_t at, int64_t numel, Raw<BF16, V> raw) {
+  typedef Raw<BF16, V> T_any __attribute__((aligned(BF16 ? 2 : 4)));
+  typedef typename std::conditional<BF16, uint16_t, uint32_t>::type E;
+  E* p = static_cast<E*>(base) + at;
+  if constexpr (FULL) {
+    __builtin_nontemporal_store(raw, reinterpret_cast<T_any*>(p));
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e)
-      if (e < n) p[e] = static_cast<uint8_t>(raw[e >> 2] >> (8 * (e & 3)));
+      if (at + e < numel) p[e] = static_cast<E>(BF16 ? raw[e >> 1] >> (16 * (e & 1)) : raw[e]);
   }
 }
-template <int V, typename Byte = typename Packed<V>::Byte>
-__device__ __forceinline__ void decode(Byte raw, float scale, float (&x)[V]) {
+template <bool BF16, int V>
+__device__ __forceinline__ float element(const Raw<BF16, V>& raw, int e) {
+  if constexpr (BF16) return __uint_as_float((e & 1) ? (raw[e >> 1] & 0xffff0000u) : (raw[e >> 1] << 16));
+  return __uint_as_float(raw[e]);
+}
+
+// V codes.
+template <int V>
+struct CodesOf {
+  typedef unsigned int T __attribute__((ext_vector_type(V / 4)));
+};
+template <int V>
+using Codes = typename CodesOf<V>::T;
+
+template <bool FULL, int V>
+__device__ __forceinline__ Codes<V> load_codes(const void* base, int64_t at, int64_t numel) {
+  const uint8_t* p = static_cast<const uint8_t*>(base);
+  if constexpr (FULL) return __builtin_nontemporal_load(reinterpret_cast<const Codes<V>*>(p + at));
+  Codes<V> raw = {};
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const bool in = at + e < numel;
+    const uint32_t x = p[in ? at + e : numel - 1];
+    raw[e >> 2] |= (in ? x : 0u) << (8 * (e & 3));
+  }
+  return raw;
+}
+template <bool FULL, int V>
+__device__ __forceinline__ void store_codes(void* base, int64_t at, int64_t numel, Codes<V> raw) {
+  uint8_t* p = static_cast<uint8_t*>(base) + at;
+  if constexpr (FULL) {
+    __builtin_nontemporal_store(raw, reinterpret_cast<Codes<V>*>(p));
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (at + e < numel) p[e] = static_cast<uint8_t>(raw[e >> 2] >> (8 * (e & 3)));
+  }
+}
+// Index of the scale of element `at`, the last one's behind the end.
+template <bool FULL>
+__device__ __forceinline__ int64_t scale_index(int64_t at, int64_t numel) {
+  return (FULL || at < numel ? at : numel - 1) / EDIT_ADAMW_BLOCK;
+}
+template <int V>
+__device__ __forceinline__ void decode(const Codes<V>& raw, float (&x)[V]) {
 #pragma unroll
   for (int h = 0; h < V / 4; ++h) {
     const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(raw[h], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(raw[h], true);
-    x[4 * h] = a[0] * scale, x[4 * h + 1] = a[1] * scale;
-    x[4 * h + 2] = b[0] * scale, x[4 * h + 3] = b[1] * scale;
+    x[4 * h] = a[0], x[4 * h + 1] = a[1], x[4 * h + 2] = b[0], x[4 * h + 3] = b[1];
   }
 }
 
@@ -186,12 +165,19 @@ __device__ __forceinline__ uint32_t block_max(uint32_t x) {
 }
 
 // The exponent field of the block's largest finite |x|, at least 8 (so that
-// scale and 1 / scale are normal numbers).
-template <int V>
+// scale and 1 / scale are normal numbers).  SIGNED: x has a sign; v has none.
+template <bool SIGNED, int V>
 __device__ __forceinline__ uint32_t block_exponent(const float (&x)[V]) {
   uint32_t top = 0;
+  if constexpr (SIGNED) {
+    float t = 0.f;
 #pragma unroll
-  for (int e = 0; e < V; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+    for (int e = 0; e < V; ++e) t = fmaxf(t, fabsf(x[e]));  // leaves a NaN out
+    top = __float_as_uint(t);
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) top = max(top, __float_as_uint(x[e]));
+  }
   top = block_max<V>(top);
   if (__builtin_expect(top >= 0x7f800000u, 0)) {  // all lanes of the block alike
     top = 0;
@@ -206,29 +192,55 @@ __device__ __forceinline__ uint32_t block_exponent(const float (&x)[V]) {
 }
 __device__ __forceinline__ float scale_of(uint32_t exponent) { return __uint_as_float((exponent - 7) << 23); }
 
-// x to 8 bits and their scale.  The conversion adds the top 20 bits of its
-// random operand below the last place kept and cuts: q floor(|y| / q + u).
-template <bool SECOND, int V>
-__device__ __forceinline__ typename Packed<V>::Byte encode(const float (&x)[V], uint32_t exponent,
-                                                           const uint32_t (&word)[V]) {
-  const float inv = __uint_as_float((261 - exponent) << 23);  // 2^(134 - exponent), exact
-  typename Packed<V>::Byte raw = {};
+// x to 8 bits.  The conversion divides by the scale, adds the top 20 bits of its
+// random operand below the last place kept and cuts: q floor(|y| / q + u).  LEAST:
+// |y| is 2^-9 at least, for an x without a sign.
+template <bool LEAST, int V>
+__device__ __forceinline__ Codes<V> encode(const float (&x)[V], uint32_t exponent, const uint32_t (&word)[V]) {
+  const float scale = scale_of(exponent);
+  const uint32_t least = __float_as_uint(scale * 0x1p-9f);  // subnormal down to 2^-135; products keep those
+  Codes<V> raw = {};
 #pragma unroll
   for (int h = 0; h < V / 4; ++h) {
-    uint32_t w = 0;
-#define EDIT_ADAMW_CODE(I)                                                                            \
-  {                                                                                                   \
-    float y = x[4 * h + I] * inv;                                                                     \
-    uint32_t r = word[4 * h + I];                                                                     \
-    if constexpr (SECOND) {                                                                           \
-      y = __uint_as_float(max(__float_as_uint(y), 0x3b000000u)); /* v: 2^-9 at least; keeps a NaN */  \
-      r = __builtin_amdgcn_alignbit(r, r, 16);                                                        \
-    }                                                                                                 \
-    w = __builtin_amdgcn_cvt_sr_fp8_f32(y, r, w, I);                                                  \
+    int w = 0;
+#define EDIT_ADAMW_CODE(I)                                                             \
+  {                                                                                    \
+    float y = x[4 * h + I];                                                            \
+    uint32_t r = word[4 * h + I];                                                      \
+    if constexpr (LEAST) {                                                             \
+      y = __uint_as_float(max(__float_as_uint(y), least)); /* as bits: keeps a NaN */  \
+      r = __builtin_amdgcn_alignbit(r, r, 16);                                         \
+    }                                                                                  \
+    w = __builtin_amdgcn_cvt_scalef32_sr_fp8_f32(w, y, r, scale, I);                   \
   }
     EDIT_ADAMW_CODE(0) EDIT_ADAMW_CODE(1) EDIT_ADAMW_CODE(2) EDIT_ADAMW_CODE(3)
 #undef EDIT_ADAMW_CODE
     raw[h] = w;
+  }
+  return raw;
+}
+
+// fp32 values as elements of a buffer: bf16 rounded to nearest, or to
+// q floor(|x| / q + u), u the top 16 bits of `word`.
+template <bool BF16, bool SR, int V>
+__device__ __forceinline__ Raw<BF16, V> rounded(const float (&x)[V], const uint32_t (&word)[V]) {
+  Raw<BF16, V> raw;
+  if constexpr (BF16) {
+#pragma unroll
+    for (int e = 0; e < V; e += 2) {
+      bf16x2_t h = {};
+      if constexpr (SR) {
+        h = __builtin_amdgcn_cvt_sr_bf16_f32(h, x[e], word[e], false);
+        h = __builtin_amdgcn_cvt_sr_bf16_f32(h, x[e + 1], word[e + 1], true);
+      } else {
+        const f32x2 f = {x[e], x[e + 1]};
+        h = __builtin_convertvector(f, bf16x2_t);  // RNE
+      }
+      raw[e >> 1] = __builtin_bit_cast(uint32_t, h);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) raw[e] = __float_as_uint(x[e]);
   }
   return raw;
 }
@@ -247,30 +259,6 @@ __device__ __forceinline__ double block_sum(double x) {
   return x;
 }
 
-// 16 bytes from element `at` of n on; zeros behind them.
-template <bool BF16>
-__device__ __forceinline__ u32x4 load_raw(const void* base, int64_t at, int64_t n) {
-  constexpr int V = BF16 ? 8 : 4;
-  if constexpr (BF16) {
-    typedef u32x4 u32x4_half __attribute__((aligned(2)));
-    const uint16_t* p = static_cast<const uint16_t*>(base) + at;
-    if (n - at >= V) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_half*>(p));
-    u32x4 raw = {0, 0, 0, 0};
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (at + e < n) raw[e >> 1] |= static_cast<uint32_t>(p[e]) << (16 * (e & 1));
-    return raw;
-  } else {
-    const uint32_t* p = static_cast<const uint32_t*>(base) + at;
-    if (n - at >= V) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
-    u32x4 raw = {0, 0, 0, 0};
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (at + e < n) raw[e] = p[e];
-    return raw;
-  }
-}
-
 // Reads 2 or 4 bytes an element: 1.23G bf16 ones in 352 us (7.0 TB/s; where a
 // chunk's tensor was looked up and its loads waited for before the next one's,
 // 439).  Squares are exact in fp64.
@@ -284,10 +272,19 @@ __global__ __launch_bounds__(kAdamNormThreads) void adamw_norm_kernel(const Adam
     int k = -1;
 #pragma unroll
     for (int h = 0; h < kAdamNormTensors / 64; ++h) k += __popcll(__ballot(first[h] <= c));
-    const int64_t at = static_cast<int64_t>(c - tab.first[k]) * adamw_norm_chunk(BF16) + threadIdx.x * (BF16 ? 8 : 4);
+    constexpr int V = BF16 ? 8 : 4, chunk = adamw_norm_chunk(BF16);
+    static_assert(kAdamNormTensors == 192, "three words of first[] a lane");
+    const int begin = __builtin_amdgcn_readlane(k < 64 ? first[0] : k < 128 ? first[1] : first[2], k & 63);
+    const int64_t at = static_cast<int64_t>(c - begin) * chunk, n = tab.numel[k];
+    if (at + chunk <= n) {
 #pragma unroll
-    for (int u = 0; u < kAdamNormVecs; ++u)
-      raw[u] = load_raw<BF16>(tab.grad[k], at + u * (adamw_norm_chunk(BF16) / kAdamNormVecs), tab.numel[k]);
+      for (int u = 0; u < kAdamNormVecs; ++u)
+        raw[u] = load_raw<true, BF16, V>(tab.grad[k], at + (u * kAdamNormThreads + threadIdx.x) * V, n);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kAdamNormVecs; ++u)
+        raw[u] = load_raw<false, BF16, V>(tab.grad[k], at + (u * kAdamNormThreads + threadIdx.x) * V, n);
+    }
   };
   double sum[2] = {0.0, 0.0};
   u32x4 raw[kAdamNormVecs];
@@ -359,8 +356,10 @@ __global__ __launch_bounds__(kAdamDecideThreads) void adamw_decide_kernel(const 
     r.step += 1;
     r.clip = clip;
     r.lr_decay = lr * call.weight_decay;
-    r.rate = static_cast<float>(lr / (1.0 - power(hyper.beta1, r.step)));
-    r.root = static_cast<float>(1.0 / sqrt(1.0 - power(hyper.beta2, r.step)));
+    // lr = 0 takes the largest numbers: a quotient of zero
+    const double most = 3.4028234663852886e38, over = fmax((1.0 - power(hyper.beta1, r.step)) / lr, 0.0);
+    r.root = static_cast<float>(fmin(over / sqrt(1.0 - power(hyper.beta2, r.step)), most));
+    r.eps = static_cast<float>(fmin(over * hyper.eps, most));
     r.key = mix(mix(call.seed) + static_cast<uint64_t>(r.step));
   }
   *rec = r;
@@ -374,17 +373,11 @@ struct Place {
   int64_t at;  // first element of the block
 };
 __device__ __forceinline__ Place place_of(const AdamTable& tab, int chunk) {
-  const int b = gridDim.x - 1 - blockIdx.x;
+  const int b = gridDim.x - 1 - blockIdx.x, first = tab.first[threadIdx.x];
   Place p;
-  p.k = __popcll(__ballot(tab.first[threadIdx.x] <= b)) - 1;
-  p.at = static_cast<int64_t>(b - tab.first[p.k]) * chunk;
+  p.k = __popcll(__ballot(first <= b)) - 1;
+  p.at = static_cast<int64_t>(b - __builtin_amdgcn_readlane(first, p.k)) * chunk;
   return p;
-}
-// How many of the V elements from `at` on there are.
-template <int V>
-__device__ __forceinline__ int here(int64_t numel, int64_t at) {
-  const int64_t left = numel - at;
-  return left >= V ? V : left > 0 ? static_cast<int>(left) : 0;
 }
 struct Key {
   uint32_t k0, k1;
@@ -394,121 +387,171 @@ __device__ __forceinline__ Key key_of(uint64_t key, int tensor, int64_t at) {
   return {static_cast<uint32_t>(k), static_cast<uint32_t>(k >> 32) ^ (static_cast<uint32_t>(at >> 32) * 0xBB67AE85u)};
 }
 
-// One lane: U times V elements of every buffer, each time next to its
-// neighbour's.  PB, GB: bf16 parameters, gradients; HELD: states in 8 bits; SR:
-// bf16 parameters rounded stochastically.
-template <bool PB, bool GB, bool HELD, bool SR, int V, int U>
-__global__ __launch_bounds__(kAdamThreads) void adamw_step_kernel(const AdamTable tab, const AdamHyper hyper,
-                                                                  const AdamRecord* __restrict__ rec) {
-  if (rec->skip) return;
-  const Place place = place_of(tab, kAdamThreads * V * U);
-  const AdamTensor& t = tab.tensor[place.k];
-  int n[U];
+// The work of one block: U times V elements a lane of every buffer, each time
+// next to its neighbour's; FULL: all of them are there.
+template <bool FULL, bool PB, bool GB, bool HELD, bool SR, int V, int U>
+__device__ __forceinline__ void step_block(const AdamTensor& t, float decay_factor, int tensor, const AdamHyper& hyper,
+                                           const AdamRecord& rec, int64_t begin) {
+  if (rec.skip) return;  // here, so that the record is loaded beside the tensor's entry
+  const int64_t n = t.numel;
   int64_t at[U];
-  float p[U][V], g[U][V], m[U][V], v[U][V];
+  Raw<PB, V> p_raw[U];
+  Raw<GB, V> g_raw[U];
+  Raw<false, 4> m_raw[U], v_raw[U];
+  Codes<V> m_codes[U], v_codes[U];
+  float m_scale[U], v_scale[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    at[u] = place.at + u * 64 * V + threadIdx.x * V;
-    n[u] = here<V>(t.numel, at[u]);
-    load_vec<PB>(t.param, at[u], n[u], p[u]);
-    load_vec<GB>(t.grad, at[u], n[u], g[u]);
+    at[u] = begin + u * kAdamThreads * V + threadIdx.x * V;
+    p_raw[u] = load_raw<FULL, PB, V>(t.param, at[u], n);
+    g_raw[u] = load_raw<FULL, GB, V>(t.grad, at[u], n);
     if constexpr (HELD) {
-      const int64_t block = at[u] / EDIT_ADAMW_BLOCK;
-      const auto mc = load_codes<V>(t.m, at[u], n[u]), vc = load_codes<V>(t.v, at[u], n[u]);
-      const float ms = n[u] ? t.m_scale[block] : 0.f, vs = n[u] ? t.v_scale[block] : 0.f;
-      decode<V>(mc, ms, m[u]);
-      decode<V>(vc, vs, v[u]);
+      m_scale[u] = t.m_scale[scale_index<FULL>(at[u], n)];
+      v_scale[u] = t.v_scale[scale_index<FULL>(at[u], n)];
+      m_codes[u] = load_codes<FULL, V>(t.m, at[u], n);
+      v_codes[u] = load_codes<FULL, V>(t.v, at[u], n);
     } else {
-      load_vec<false>(t.m, at[u], n[u], m[u]);
-      load_vec<false>(t.v, at[u], n[u], v[u]);
+      m_raw[u] = load_raw<FULL, false, V>(t.m, at[u], n);
+      v_raw[u] = load_raw<FULL, false, V>(t.v, at[u], n);
     }
   }
-  const float clip = rec->clip, rate = rec->rate, root = rec->root, eps = static_cast<float>(hyper.eps);
-  const float decay = static_cast<float>(rec->lr_decay * tab.decay[place.k]);
+  const float clip = rec.clip, root = rec.root, eps = rec.eps;
+  const float decay = static_cast<float>(rec.lr_decay * decay_factor);
   const double b1 = hyper.beta1, b2 = hyper.beta2, a1 = 1.0 - b1, a2 = 1.0 - b2;
-  const Key key = key_of(rec->key, tab.base + place.k, place.at);  // 2^32 is a multiple of what a block takes
+  const Key key = key_of(rec.key, tensor, begin);  // 2^32 is a multiple of what a block takes
 #pragma unroll
   for (int u = 0; u < U; ++u) {
+    float m[V], v[V], p[V];
+    double keep1 = b1, keep2 = b2;
+    if constexpr (HELD) {  // the scale, a power of two, goes with the factor
+      decode<V>(m_codes[u], m);
+      decode<V>(v_codes[u], v);
+      keep1 *= m_scale[u];
+      keep2 *= v_scale[u];
+    }
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      const double gd = clip * g[u][e];
-      m[u][e] = static_cast<float>(__builtin_fma(b1, static_cast<double>(m[u][e]), a1 * gd));
-      v[u][e] = static_cast<float>(__builtin_fma(b2, static_cast<double>(v[u][e]), a2 * gd * gd));
+      if constexpr (!HELD) {
+        m[e] = element<false, V>(m_raw[u], e);
+        v[e] = element<false, V>(v_raw[u], e);
+      }
+      p[e] = element<PB, V>(p_raw[u], e);
+      const double g = clip * element<GB, V>(g_raw[u], e);
+      m[e] = static_cast<float>(__builtin_fma(keep1, static_cast<double>(m[e]), a1 * g));
+      v[e] = static_cast<float>(__builtin_fma(keep2, static_cast<double>(v[e]), a2 * g * g));
       // The hardware's square root is off by one place and takes values below
       // 2^-126 as zero; beside an eps of 1e-12 at least neither is seen in p.
-      const float d = __builtin_fmaf(__builtin_amdgcn_sqrtf(v[u][e]), root, eps);
-      p[u][e] -= __builtin_fmaf(decay, p[u][e], rate * m[u][e] * __builtin_amdgcn_rcpf(d));
+      const float d = __builtin_fmaf(__builtin_amdgcn_sqrtf(v[e]), root, eps);
+      p[e] -= __builtin_fmaf(decay, p[e], m[e] * __builtin_amdgcn_rcpf(d));
     }
+    uint32_t word[V], second[V];
     if constexpr (HELD || SR) {
-      uint32_t word[V];
+      const uint32_t base = static_cast<uint32_t>(at[u]) ^ key.k0;  // at is a multiple of V: + e is ^ e
 #pragma unroll
-      for (int e = 0; e < V; ++e) word[e] = random_word(static_cast<uint32_t>(at[u]) + e, key.k0, key.k1);
-      if constexpr (SR) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) {  // what cuts the low half afterwards is exact
-          const uint32_t x = __float_as_uint(p[u][e]);
-          const uint32_t up = (x + (second_word(word[e], key.k0) >> 16)) & 0xffff0000u;
-          p[u][e] = (x & 0x7fffffffu) < 0x7f800000u ? __uint_as_float(up) : p[u][e];
-        }
-      }
-      if constexpr (HELD) {
-        const uint32_t em = block_exponent(m[u]), ev = block_exponent(v[u]);
-        store_codes<V>(t.m, at[u], n[u], encode<false>(m[u], em, word));
-        store_codes<V>(t.v, at[u], n[u], encode<true>(v[u], ev, word));
-        if (at[u] % EDIT_ADAMW_BLOCK == 0 && n[u]) {
-          t.m_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(em);
-          t.v_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(ev);
-        }
+      for (int e = 0; e < V; ++e) {
+        word[e] = random_word(base ^ e, key.k1);
+        if constexpr (SR) second[e] = second_word(word[e], key.k0);
       }
     }
-    if constexpr (!HELD) {
-      store_vec<false>(t.m, at[u], n[u], m[u]);
-      store_vec<false>(t.v, at[u], n[u], v[u]);
-    }
-    store_vec<PB>(t.param, at[u], n[u], p[u]);
-  }
-}
-
-template <bool PACK, int V, int U>
-__global__ __launch_bounds__(kAdamThreads) void adamw_convert_kernel(const AdamTable tab, uint64_t key64) {
-  const Place place = place_of(tab, kAdamThreads * V * U);
-  const AdamTensor& t = tab.tensor[place.k];
-  int n[U];
-  int64_t at[U];
-  float m[U][V], v[U][V];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    at[u] = place.at + u * 64 * V + threadIdx.x * V;
-    n[u] = here<V>(t.numel, at[u]);
-    if constexpr (PACK) {
-      load_vec<false>(t.param, at[u], n[u], m[u]);
-      load_vec<false>(t.grad, at[u], n[u], v[u]);
-    } else {
-      const int64_t block = at[u] / EDIT_ADAMW_BLOCK;
-      const auto mc = load_codes<V>(t.m, at[u], n[u]), vc = load_codes<V>(t.v, at[u], n[u]);
-      const float ms = n[u] ? t.m_scale[block] : 0.f, vs = n[u] ? t.v_scale[block] : 0.f;
-      decode<V>(mc, ms, m[u]);
-      decode<V>(vc, vs, v[u]);
-    }
-  }
-  const Key key = key_of(key64, tab.base + place.k, place.at);
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if constexpr (PACK) {
-      uint32_t word[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) word[e] = random_word(static_cast<uint32_t>(at[u]) + e, key.k0, key.k1);
-      const uint32_t em = block_exponent(m[u]), ev = block_exponent(v[u]);
-      store_codes<V>(t.m, at[u], n[u], encode<false>(m[u], em, word));
-      store_codes<V>(t.v, at[u], n[u], encode<true>(v[u], ev, word));
-      if (at[u] % EDIT_ADAMW_BLOCK == 0 && n[u]) {
+    store_raw<FULL, PB, V>(t.param, at[u], n, rounded<PB, SR, V>(p, second));
+    if constexpr (HELD) {
+      const uint32_t em = block_exponent<true>(m), ev = block_exponent<false>(v);
+      store_codes<FULL, V>(t.m, at[u], n, encode<false>(m, em, word));
+      store_codes<FULL, V>(t.v, at[u], n, encode<true>(v, ev, word));
+      if (at[u] % EDIT_ADAMW_BLOCK == 0 && (FULL || at[u] < n)) {
         t.m_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(em);
         t.v_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(ev);
       }
     } else {
-      store_vec<false>(t.param, at[u], n[u], m[u]);
-      store_vec<false>(const_cast<void*>(t.grad), at[u], n[u], v[u]);
+      store_raw<FULL, false, V>(t.m, at[u], n, rounded<false, false, V>(m, word));
+      store_raw<FULL, false, V>(t.v, at[u], n, rounded<false, false, V>(v, word));
     }
+  }
+}
+
+// PB, GB: bf16 parameters, gradients; HELD: states in 8 bits; SR: bf16 parameters
+// rounded stochastically.
+template <bool PB, bool GB, bool HELD, bool SR, int V, int U>
+__global__ __launch_bounds__(kAdamThreads, 4) void adamw_step_kernel(const AdamTable tab, const AdamHyper hyper,
+                                                                  const AdamRecord* __restrict__ rec) {
+  constexpr int chunk = kAdamThreads * V * U;
+  const AdamRecord r = *rec;
+  const Place place = place_of(tab, chunk);
+  const AdamTensor t = tab.tensor[place.k];
+  const float decay = tab.decay[place.k];
+  if (place.at + chunk <= t.numel) {
+    step_block<true, PB, GB, HELD, SR, V, U>(t, decay, tab.base + place.k, hyper, r, place.at);
+  } else {
+#pragma unroll 1
+    for (int64_t at = place.at; at < t.numel; at += kAdamThreads * V)
+      step_block<false, PB, GB, HELD, SR, V, 1>(t, decay, tab.base + place.k, hyper, r, at);
+  }
+}
+
+template <bool FULL, bool PACK, int V, int U>
+__device__ __forceinline__ void convert_block(const AdamTensor& t, int tensor, uint64_t key64, int64_t begin) {
+  const int64_t n = t.numel;
+  int64_t at[U];
+  Raw<false, V> m_raw[U], v_raw[U];
+  Codes<V> m_codes[U], v_codes[U];
+  float m_scale[U], v_scale[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    at[u] = begin + u * kAdamThreads * V + threadIdx.x * V;
+    if constexpr (PACK) {
+      m_raw[u] = load_raw<FULL, false, V>(t.param, at[u], n);
+      v_raw[u] = load_raw<FULL, false, V>(t.grad, at[u], n);
+    } else {
+      m_scale[u] = t.m_scale[scale_index<FULL>(at[u], n)];
+      v_scale[u] = t.v_scale[scale_index<FULL>(at[u], n)];
+      m_codes[u] = load_codes<FULL, V>(t.m, at[u], n);
+      v_codes[u] = load_codes<FULL, V>(t.v, at[u], n);
+    }
+  }
+  const Key key = key_of(key64, tensor, begin);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float m[V], v[V];
+    uint32_t word[V];
+    if constexpr (PACK) {
+      const uint32_t base = static_cast<uint32_t>(at[u]) ^ key.k0;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        m[e] = element<false, V>(m_raw[u], e);
+        v[e] = element<false, V>(v_raw[u], e);
+        word[e] = random_word(base ^ e, key.k1);
+      }
+      // a negative v, which no step makes, is taken by its size
+      const uint32_t em = block_exponent<true>(m), ev = block_exponent<true>(v);
+      store_codes<FULL, V>(t.m, at[u], n, encode<false>(m, em, word));
+      store_codes<FULL, V>(t.v, at[u], n, encode<true>(v, ev, word));
+      if (at[u] % EDIT_ADAMW_BLOCK == 0 && (FULL || at[u] < n)) {
+        t.m_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(em);
+        t.v_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(ev);
+      }
+    } else {
+      decode<V>(m_codes[u], m);
+      decode<V>(v_codes[u], v);
+#pragma unroll
+      for (int e = 0; e < V; ++e) m[e] *= m_scale[u], v[e] *= v_scale[u];
+      store_raw<FULL, false, V>(t.param, at[u], n, rounded<false, false, V>(m, word));
+      store_raw<FULL, false, V>(const_cast<void*>(t.grad), at[u], n, rounded<false, false, V>(v, word));
+    }
+  }
+}
+
+template <bool PACK, int V, int U>
+__global__ __launch_bounds__(kAdamThreads) void adamw_convert_kernel(const AdamTable tab, uint64_t key) {
+  constexpr int chunk = kAdamThreads * V * U;
+  static_assert(chunk == adamw_convert_chunk(PACK), "as the tables count blocks");
+  const Place place = place_of(tab, chunk);
+  const AdamTensor t = tab.tensor[place.k];
+  if (place.at + chunk <= t.numel) {
+    convert_block<true, PACK, V, U>(t, tab.base + place.k, key, place.at);
+  } else {
+#pragma unroll 1
+    for (int64_t at = place.at; at < t.numel; at += kAdamThreads * V)
+      convert_block<false, PACK, V, 1>(t, tab.base + place.k, key, at);
   }
 }
 
@@ -521,7 +564,7 @@ hipError_t launch(void (*kernel)(A...), int blocks, int threads, int lds, hipStr
 
 template <bool PB, bool GB, bool HELD, bool SR>
 hipError_t step(int blocks, const AdamTable& table, const AdamHyper& hyper, const AdamRecord* rec, hipStream_t stream) {
-  constexpr int V = adamw_vec(PB, GB, HELD), U = adamw_times(PB, GB, HELD), resident = adamw_resident(PB, GB, HELD);
+  constexpr int V = adamw_vec(PB, GB, HELD), U = adamw_times(HELD), resident = adamw_resident(PB, GB, HELD);
   constexpr int lds = resident == 32 ? 0 : lds_for_blocks(resident, 0, kLdsPerCu);
   return launch<AdamTable, AdamHyper, const AdamRecord*>(adamw_step_kernel<PB, GB, HELD, SR, V, U>, blocks, kAdamThreads, lds,
                                                          stream, table, hyper, rec);
@@ -567,8 +610,8 @@ hipError_t launch_adamw_step(bool param_bf16, bool grad_bf16, bool held, bool st
 }
 
 hipError_t launch_adamw_convert(bool pack, int blocks, const AdamTable& table, uint64_t key, hipStream_t stream) {
-  return launch<AdamTable, uint64_t>(pack ? adamw_convert_kernel<true, 4, 2> : adamw_convert_kernel<false, 4, 2>, blocks, kAdamThreads,
-                                     0, stream, table, key);
+  return launch<AdamTable, uint64_t>(pack ? adamw_convert_kernel<true, 4, adamw_convert_times(true)> : adamw_convert_kernel<false, 4, adamw_convert_times(false)>, blocks, kAdamThreads,
+                                     pack ? 0 : lds_for_blocks(kAdamUnpackResident, 0, kLdsPerCu), stream, table, key);
 }
 
 }  // namespace edit

@@ -252,7 +252,7 @@ edit_status_t convert(edit_adamw* h, bool pack, const edit_adamw_tensors_t* t, c
   }
   ADAM_TRY(check_overlaps(h, pack ? 0x3cu : 0x03u));
   return for_tables(
-      h, kAdamConvertChunk,
+      h, adamw_convert_chunk(pack),
       [&](int k, AdamTensor* to) {
         fill_states(h, t, k, to);
         to->param = const_cast<float*>(m[k]);
