@@ -61,12 +61,13 @@ using Raw = typename RawOf<BF16, V>::T;
 // all of them are there.  Parameters and gradients begin at any element.  Next to
 // the end the elements are loaded one by one, the last one in place of those
 // behind it, so that no load waits for a branch.
-template <bool FULL, bool BF16, int V>
+template <bool FULL, bool BF16, int V, bool CACHED = false>
 __device__ __forceinline__ Raw<BF16, V> load_raw(const void* base, int64_t at, int64_t numel) {
   typedef Raw<BF16, V> T;
   typedef T T_any __attribute__((aligned(BF16 ? 2 : 4)));
   typedef typename std::conditional<BF16, uint16_t, uint32_t>::type E;
   const E* p = static_cast<const E*>(base);
+  if constexpr (FULL && CACHED) return *reinterpret_cast<const T_any*>(p + at);
   if constexpr (FULL) return __builtin_nontemporal_load(reinterpret_cast<const T_any*>(p + at));
   T raw = {};
 #pragma unroll
@@ -259,39 +260,35 @@ __device__ __forceinline__ double block_sum(double x) {
   return x;
 }
 
-// Reads 2 or 4 bytes an element: 1.23G bf16 ones in 352 us (7.0 TB/s; where a
-// chunk's tensor was looked up and its loads waited for before the next one's,
-// 439).  Squares are exact in fp64.
-template <bool BF16>
-__global__ __launch_bounds__(kAdamNormThreads) void adamw_norm_kernel(const AdamNormTable tab, double* partials) {
-  const int lane = threadIdx.x & 63;
-  int first[kAdamNormTensors / 64];
-#pragma unroll
-  for (int h = 0; h < kAdamNormTensors / 64; ++h) first[h] = tab.first[64 * h + lane];
-  auto load = [&](int c, u32x4 (&raw)[kAdamNormVecs]) {
+// The chunks of a block from c on, below `end`; first: the table's, a lane three
+// of them; CACHED: the update pass reads them again soon.
+template <bool BF16, bool CACHED>
+__device__ __forceinline__ void norm_chunks(const AdamNormTable& tab, const int (&first)[kAdamNormTensors / 64], int end, int& c,
+                                            double (&sum)[2]) {
+  constexpr int V = BF16 ? 8 : 4, chunk = adamw_norm_chunk(BF16);
+  static_assert(kAdamNormTensors == 192, "three words of first[] a lane");
+  auto load = [&](int i, u32x4 (&raw)[kAdamNormVecs]) {
     int k = -1;
 #pragma unroll
-    for (int h = 0; h < kAdamNormTensors / 64; ++h) k += __popcll(__ballot(first[h] <= c));
-    constexpr int V = BF16 ? 8 : 4, chunk = adamw_norm_chunk(BF16);
-    static_assert(kAdamNormTensors == 192, "three words of first[] a lane");
+    for (int h = 0; h < kAdamNormTensors / 64; ++h) k += __popcll(__ballot(first[h] <= i));
     const int begin = __builtin_amdgcn_readlane(k < 64 ? first[0] : k < 128 ? first[1] : first[2], k & 63);
-    const int64_t at = static_cast<int64_t>(c - begin) * chunk, n = tab.numel[k];
+    const int64_t at = static_cast<int64_t>(i - begin) * chunk, n = tab.numel[k];
     if (at + chunk <= n) {
 #pragma unroll
       for (int u = 0; u < kAdamNormVecs; ++u)
-        raw[u] = load_raw<true, BF16, V>(tab.grad[k], at + (u * kAdamNormThreads + threadIdx.x) * V, n);
+        raw[u] = load_raw<true, BF16, V, CACHED>(tab.grad[k], at + (u * kAdamNormThreads + threadIdx.x) * V, n);
     } else {
 #pragma unroll
       for (int u = 0; u < kAdamNormVecs; ++u)
         raw[u] = load_raw<false, BF16, V>(tab.grad[k], at + (u * kAdamNormThreads + threadIdx.x) * V, n);
     }
   };
-  double sum[2] = {0.0, 0.0};
+  if (c >= end) return;
   u32x4 raw[kAdamNormVecs];
-  load(blockIdx.x, raw);  // the grid has at most a block a chunk
-  for (int c = blockIdx.x; c < tab.chunks; c += gridDim.x) {
+  load(c, raw);
+  for (; c < end; c += gridDim.x) {
     u32x4 next[kAdamNormVecs] = {};
-    if (c + static_cast<int>(gridDim.x) < tab.chunks) load(c + gridDim.x, next);
+    if (c + static_cast<int>(gridDim.x) < end) load(c + gridDim.x, next);
 #pragma unroll
     for (int u = 0; u < kAdamNormVecs; ++u) {
 #pragma unroll
@@ -308,6 +305,21 @@ __global__ __launch_bounds__(kAdamNormThreads) void adamw_norm_kernel(const Adam
       raw[u] = next[u];
     }
   }
+}
+
+// Reads 2 or 4 bytes an element: 1.23G bf16 ones in 341 us (7.2 TB/s; where a
+// chunk's tensor was looked up and its loads waited for before the next one's,
+// 439).  Squares are exact in fp64.
+template <bool BF16>
+__global__ __launch_bounds__(kAdamNormThreads) void adamw_norm_kernel(const AdamNormTable tab, double* partials) {
+  const int lane = threadIdx.x & 63;
+  int first[kAdamNormTensors / 64];
+#pragma unroll
+  for (int h = 0; h < kAdamNormTensors / 64; ++h) first[h] = tab.first[64 * h + lane];
+  double sum[2] = {0.0, 0.0};
+  int c = blockIdx.x;
+  norm_chunks<BF16, false>(tab, first, min(tab.keep, tab.chunks), c, sum);
+  norm_chunks<BF16, true>(tab, first, tab.chunks, c, sum);
   const double s = block_sum<kAdamNormThreads>(sum[0] + sum[1]);
   if (threadIdx.x == 0) partials[blockIdx.x] = s;
 }

@@ -164,9 +164,15 @@ edit_status_t check_state_arrays(const edit_adamw* h, const edit_adamw_tensors_t
   return EDIT_OK;
 }
 
-// Partial sums of the gradients' squares; *count: how many there are.
-edit_status_t enqueue_norm(edit_adamw* h, const void* const* grad, int* count, hipStream_t s) {
+// Partial sums of the gradients' squares; *count: how many there are.  `again`:
+// the update pass reads them next.
+edit_status_t enqueue_norm(edit_adamw* h, const void* const* grad, bool again, int* count, hipStream_t s) {
   const int most = kAdamNormBlocksPerCu * h->num_cu, tensors = static_cast<int>(h->numel.size());
+  const int chunk = adamw_norm_chunk(h->grad_bf16);
+  int64_t left = 0;  // chunks of this launch and those behind it
+  for (int k = 0; k < tensors; ++k)
+    if (grad[k]) left += chunks_of(h->numel[k], chunk);
+  const int64_t keep = again ? kAdamNormKeep / (chunk * (h->grad_bf16 ? 2 : 4)) : 0;
   *count = 0;
   for (int k = 0; k < tensors;) {
     AdamNormTable t;
@@ -174,7 +180,7 @@ edit_status_t enqueue_norm(edit_adamw* h, const void* const* grad, int* count, h
     int64_t chunks = 0;
     for (; k < tensors && used < kAdamNormTensors; ++k) {
       if (!grad[k] || h->numel[k] == 0) continue;
-      const int64_t more = chunks_of(h->numel[k], adamw_norm_chunk(h->grad_bf16));
+      const int64_t more = chunks_of(h->numel[k], chunk);
       if (chunks + more > INT32_MAX / 2) break;
       t.first[used] = static_cast<int32_t>(chunks);
       t.numel[used] = h->numel[k];
@@ -184,6 +190,8 @@ edit_status_t enqueue_norm(edit_adamw* h, const void* const* grad, int* count, h
     if (used == 0) continue;
     std::fill(t.first + used, t.first + kAdamNormTensors, INT32_MAX);
     t.chunks = static_cast<int32_t>(chunks);
+    t.keep = static_cast<int32_t>(std::min(std::max<int64_t>(left - keep, 0), chunks));
+    left -= chunks;
     const int blocks = static_cast<int>(std::min<int64_t>(chunks, most));
     const hipError_t e = launch_adamw_norm(h->grad_bf16, blocks, t, h->partials + *count, s);
     if (e != hipSuccess) return afail_hip(e, "norm pass launch");
@@ -325,7 +333,7 @@ edit_status_t edit_adamw_sumsq(edit_adamw_t h, const void* const* grad, double* 
   ADAM_TRY(check_overlaps(h, 1u));
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   int count = 0;
-  ADAM_TRY(enqueue_norm(h, grad, &count, s));
+  ADAM_TRY(enqueue_norm(h, grad, false, &count, s));
   const hipError_t e = launch_adamw_sum(h->partials, count, sumsq, s);
   return e == hipSuccess ? EDIT_OK : afail_hip(e, "sum launch");
 }
@@ -365,7 +373,7 @@ edit_status_t edit_adamw_step(edit_adamw_t h, const edit_adamw_tensors_t* t, con
   c.seed = call->seed;
   c.check = call->max_norm > 0.0 || call->sumsq;
   int count = 0;
-  if (c.check && !call->sumsq) ADAM_TRY(enqueue_norm(h, t->grad, &count, s));
+  if (c.check && !call->sumsq) ADAM_TRY(enqueue_norm(h, t->grad, true, &count, s));
   const hipError_t e = launch_adamw_decide(h->partials, count, call->sumsq, c, h->hyper, h->rec, s);
   if (e != hipSuccess) return afail_hip(e, "decision launch");
   return for_tables(

@@ -128,9 +128,9 @@ def test_steps(dtype, grad, state, stochastic, clip):
 ], ids=str)
 def test_hyper_parameters(state, over, sizes, seed):
     run = Run(sizes, "f32", None, state, seed=seed, **over)
-    for t in range(3):
+    for t, lr in enumerate((1.0, 0.0, 1e-3, 1e-30)):
         run.draw(t)
-        run.step(lr=0.1 ** t)
+        run.step(lr=lr)
     run.close()
 
 

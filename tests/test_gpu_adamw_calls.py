@@ -1,0 +1,161 @@
+"""The AdamW step beside the framework's other steps, and at the largest sizes (GPU)."""
+import numpy as np
+import pytest
+import torch
+
+import adamw_reference as ref
+from paper_2412_07210_amd import AdamW, AdamWConfig, EditOuter, OrthoConfig, Orthogonalizer, OuterConfig
+
+pytestmark = pytest.mark.gpu
+
+DEV = torch.device("cuda:0")
+
+
+def randn(n, seed, std=1.0, dtype=torch.float32):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    return torch.empty(n, dtype=dtype, device=DEV).normal_(0.0, std, generator=gen)
+
+
+def gaps(numel, matrices):
+    """(offset, length) of the runs of elements of no matrix."""
+    out, at = [], 0
+    for o, r, c in sorted(matrices) + [(numel, 0, 0)]:
+        if o > at:
+            out.append((at, o - at))
+        at = o + r * c
+    return out
+
+
+@pytest.mark.parametrize("state", ["f32", "e4m3"])
+def test_rounds_of_workers_with_both_local_steps(state):
+    """Two rounds of three workers, four local steps each: the matrices of every replica
+    by orthogonalised updates, all other elements by AdamW, clipped by the norm of the
+    whole unit's gradient, then the outer step.  The elements of no matrix against the
+    same run in 64 bits (their own states in 8 bits are read back for it)."""
+    mats = [(5, 96, 80), (7685 + 300, 40, 130), (7985 + 5200, 64, 64)]
+    numel = 7985 + 5200 + 4096 + 77
+    runs = gaps(numel, mats)
+    assert [n for _, n in runs] == [5, 300, 77]
+    K, rounds, steps, lr, decay, max_norm = 3, 2, 4, 1e-3, 0.1, 0.05
+    theta, b = randn(numel, 1, 0.02), torch.zeros(numel, device=DEV)
+    replicas = [theta.clone() for _ in range(K)]
+    momenta = [torch.zeros(numel, device=DEV) for _ in range(K)]
+    cfg = OuterConfig(K, [numel], "f32", outer_lr=0.7, momentum=0.9, ema_warmup_rounds=10)
+    index = np.concatenate([np.arange(a, a + n) for a, n in runs])
+    t64, b64 = theta.double().cpu().numpy()[index], np.zeros(len(index))
+    opts = [AdamW(AdamWConfig([n for _, n in runs], "f32", state=state, betas=(0.9, 0.95), weight_decay=decay), DEV)
+            for _ in range(K)]
+    whole = AdamW(AdamWConfig([numel], "f32"), DEV)  # its gradient norm only
+    states = [o.new_state() for o in opts]
+    m64, v64 = [np.zeros(len(index)) for _ in range(K)], [np.zeros(len(index)) for _ in range(K)]
+    with EditOuter(cfg, DEV) as outer, Orthogonalizer(OrthoConfig(numel, mats, "f32", scale="rms"), DEV) as ortho:
+        for r in range(rounds):
+            p64 = [t64.copy() for _ in range(K)]
+            for j in range(K):
+                params = [replicas[j][a:a + n] for a, n in runs]
+                for t in range(steps):
+                    g = randn(numel, 100 + 50 * r + 10 * j + t, 1e-3 * (1 + j))
+                    s = whole.sum_squares([g])
+                    opts[j].step(params, [g[a:a + n] for a, n in runs], states[j], lr, max_norm=max_norm, sumsq=s, seed=j)
+                    ortho.local_step(replicas[j], g, momenta[j], lr=lr)
+                    clip = min(1.0, max_norm / (float(g.double().square().sum()) ** 0.5 + 1e-6))
+                    assert clip < 1.0
+                    p64[j], m64[j], v64[j], _, _ = ref.step64(
+                        p64[j], g.cpu().numpy()[index], m64[j], v64[j], r * steps + t + 1, lr, (0.9, 0.95), 1e-8, decay, clip)
+                    if state == "e4m3":
+                        x = opts[j].unpack(states[j])
+                        m64[j], v64[j] = (torch.cat(y).double().cpu().numpy() for y in x)
+            outer.step_layer(0, theta, b, replicas)
+            st = outer.state_get(0)
+            d = -st.clip_coef * sum(w * (p - t64) for w, p in zip(st.weight, p64))
+            b64 = cfg.momentum * b64 + d
+            t64 = t64 - cfg.outer_lr * (d + cfg.momentum * b64)
+            got = theta.double().cpu().numpy()[index]
+            # the bar of the outer step; a local step's own error is 2^-24 of p and 1e-6 of its step
+            assert np.abs(got - t64).max() <= 1e-5 * np.sqrt((t64 ** 2).mean()), r
+            assert all(torch.equal(x, theta) for x in replicas)
+            t64 = got  # the replicas begin the next round there
+    assert [o.state_get().step for o in opts] == [rounds * steps] * K
+    for o in (*opts, whole):
+        o.close()
+
+
+def test_states_change_over_in_mid_run():
+    """fp32 states packed for a handle with 8-bit ones, which goes on from the same t; and back."""
+    sizes = [5000, 257]
+    cfg = dict(numel=sizes, dtype="f32", betas=(0.9, 0.95))
+    p, g = [randn(n, n, 0.02) for n in sizes], [randn(n, 7 * n, 1e-3) for n in sizes]
+    with AdamW(AdamWConfig(**cfg), DEV) as full, AdamW(AdamWConfig(**cfg, state="e4m3"), DEV) as small:
+        a = full.new_state()
+        for _ in range(3):
+            full.step(p, g, a, 1e-3)
+        q = [x.clone() for x in p]
+        small.state_set(full.state_get().step)
+        b = small.pack(a.exp_avg, a.exp_avg_sq, seed=3)
+        m, v = small.unpack(b)
+        for x, y in zip(a.exp_avg, m):  # within the spacing of e4m3, or of its smallest codes
+            top = float(x.abs().max())
+            assert (x - y).abs().le(2.0 ** -3 * x.abs() + top * 2.0 ** -15).all()
+        small.step(q, g, b, 1e-3, seed=3)
+        full.step(p, g, a, 1e-3)
+        assert full.state_get().step == small.state_get().step == 4
+        m2, v2 = small.unpack(b)
+        for k, n in enumerate(sizes):
+            old = (m[k].double().cpu().numpy(), v[k].double().cpu().numpy())
+            want = 0.9 * old[0] + 0.1 * g[k].double().cpu().numpy()
+            w, _ = ref.words(3, 4, k, np.arange(n))
+            ref.assert_held(b.exp_avg[k], b.exp_avg_scale[k], want.astype(np.float32), w, False, "m")
+            assert torch.isfinite(q[k]).all()
+
+
+# (elements, state): offsets past 2^32 in elements and past 2^33 in bytes
+@pytest.mark.parametrize("n,state", [(2 ** 32 + 300, "e4m3"), (2 ** 31 + 5001, "f32")])
+def test_largest_sizes(n, state):
+    spans = [(0, 4096), (2 ** 31 - 2048, 4096), (n // 512 * 256, 4096), (n // 256 * 256 - 2560, n - (n // 256 * 256 - 2560))]
+    if n > 2 ** 32:
+        spans.append((2 ** 32 - 2048, 2048 + 300))
+    p, g = randn(n, 1, 0.02, torch.bfloat16), randn(n, 2, 1e-3, torch.bfloat16)
+    with AdamW(AdamWConfig([n], "bf16", state=state, betas=(0.9, 0.95), stochastic=True), DEV) as o:
+        s = o.new_state()
+        before = [p[a:a + k].double().cpu().numpy() for a, k in spans]
+        total = sum(float(g[a:a + 2 ** 28].double().square().sum()) for a in range(0, n, 2 ** 28))
+        assert abs(float(o.sum_squares([g])) - total) <= 2 * n * 2.0 ** -53 * total
+        for t in (1, 2):
+            olds = []
+            for a, k in spans:
+                if state == "f32":
+                    olds.append([x[0][a:a + k].double().cpu().numpy() for x in (s.exp_avg, s.exp_avg_sq)])
+                else:
+                    b = slice(a // 256, -(-(a + k) // 256))
+                    olds.append([ref.values(x[0][a:a + k], y[0][b]) for x, y in ((s.exp_avg, s.exp_avg_scale),
+                                                                                (s.exp_avg_sq, s.exp_avg_sq_scale))])
+            o.step([p], [g], s, 1e-3, max_norm=1.0, seed=9)
+            clip = o.state_get().clip_coef
+            for i, (a, k) in enumerate(spans):
+                what = f"{state} at {a}, t = {t}"
+                want, m, v, step, terms = ref.step64(before[i], g[a:a + k].float().cpu().numpy(), *olds[i], t, 1e-3, (0.9, 0.95),
+                                                     1e-8, 0.01, clip)
+                first, second = ref.words(9, t, 0, np.arange(a, a + k))
+                ref.assert_params(p[a:a + k], want, step, what, second)
+                if state == "f32":
+                    ref.assert_states(s.exp_avg[0][a:a + k], m, what, terms)
+                    ref.assert_states(s.exp_avg_sq[0][a:a + k], v, what)
+                else:
+                    b = slice(a // 256, -(-(a + k) // 256))
+                    ref.assert_held(s.exp_avg[0][a:a + k], s.exp_avg_scale[0][b], m.astype(np.float32), first, False, what)
+                    ref.assert_held(s.exp_avg_sq[0][a:a + k], s.exp_avg_sq_scale[0][b], v.astype(np.float32), first, True, what)
+                before[i] = p[a:a + k].double().cpu().numpy()
+
+
+def test_calls_after_a_failed_one():
+    """A stale error of the program's own does not fail a call, nor does a refused call the next."""
+    p, g = [randn(100, 1)], [randn(100, 2)]
+    with AdamW(AdamWConfig([100], "f32"), DEV) as o:
+        s = o.new_state()
+        with pytest.raises(Exception):
+            torch.empty(2 ** 50, device=DEV)
+        o.step(p, g, s, 1e-3)
+        with pytest.raises(Exception):
+            o.step(p, p, s, 1e-3)
+        o.step(p, g, s, 1e-3)
+        assert o.state_get().step == 2
