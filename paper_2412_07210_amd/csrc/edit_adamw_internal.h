@@ -57,7 +57,14 @@ constexpr int kAdamNormTensors = 192;                    // of one launch
 // whole steps with 0, 96, 160, 224 and 256 MiB: 350M model fp32 1488, 1484, 1477,
 // 1470, 1467; its fp32 parameters, bf16 gradients, e4m3 states 795, 787, 784, 780, 783.
 constexpr int64_t kAdamNormKeep = int64_t(224) << 20;
-constexpr int adamw_norm_chunk(bool bf16) { return kAdamNormThreads * kAdamNormVecs * (bf16 ? 8 : 4); }
+constexpr int adamw_norm_chunk(bool bf16, int threads = kAdamNormThreads) { return threads * kAdamNormVecs * (bf16 ? 8 : 4); }
+// Few gradients: one block takes them all, a wave a chunk, and decides: a launch
+// less.  us of a sum and of a clipped step, so and with one launch more, of 2048
+// bf16 elements in each of 8 tensors: in a graph 2.6 and 5.5, 6.0 and 8.8; 32: 4.3
+// and 5.7, 7.8 and 9.1; 64: 6.2 and 5.7, 11.5 and 10.9, but eager 7.2 and 8.5, 14.2
+// and 15.9.
+constexpr int kAdamSmallThreads = 1024;
+constexpr int kAdamSmallChunks = 64;
 
 // Device-resident state of a handle and what its next update pass goes by.
 struct alignas(16) AdamRecord {
@@ -81,6 +88,20 @@ struct AdamTensor {
   int64_t numel;
 };
 
+struct AdamHyper {
+  double beta1, beta2, eps;
+};
+
+// What a call does beside the tensors.
+struct AdamCall {
+  double lr;
+  const double* lr_device;  // in place of lr
+  double weight_decay;
+  double max_norm;          // infinity: no clip
+  uint64_t seed;
+  bool check;               // S is there
+};
+
 // Block b works on the tensor whose first[] is the last one that is <= b.
 struct AdamTable {
   int32_t first[64];  // beyond the tensors: more than any block
@@ -97,23 +118,13 @@ struct AdamNormTable {
   int64_t numel[kAdamNormTensors];
   const void* grad[kAdamNormTensors];
 };
-static_assert(sizeof(AdamNormTable) + 128 <= 4096, "kernel arguments");
-
-struct AdamHyper {
-  double beta1, beta2, eps;
-};
-
-// What a call does beside the tensors.
-struct AdamCall {
-  double lr;
-  const double* lr_device;  // in place of lr
-  double weight_decay;
-  double max_norm;          // infinity: no clip
-  uint64_t seed;
-  bool check;               // S is there
-};
+static_assert(sizeof(AdamNormTable) + sizeof(AdamCall) + 64 <= 4096, "kernel arguments");
 
 hipError_t launch_adamw_norm(bool bf16, int blocks, const AdamNormTable& table, double* partials, hipStream_t stream);
+// The same of few gradients, chunks of a wave, and what follows: *out = S, or
+// with no `out` the record.
+hipError_t launch_adamw_small(bool bf16, const AdamNormTable& table, double* out, const AdamCall& call,
+                              const AdamHyper& hyper, AdamRecord* rec, hipStream_t stream);
 // out = the sum of `count` partials, in their order.
 hipError_t launch_adamw_sum(const double* partials, int count, double* out, hipStream_t stream);
 // S from `count` partials, or from *sumsq where that is given, and the record.

@@ -260,12 +260,13 @@ __device__ __forceinline__ double block_sum(double x) {
   return x;
 }
 
-// The chunks of a block from c on, below `end`; first: the table's, a lane three
-// of them; CACHED: the update pass reads them again soon.
-template <bool BF16, bool CACHED>
-__device__ __forceinline__ void norm_chunks(const AdamNormTable& tab, const int (&first)[kAdamNormTensors / 64], int end, int& c,
-                                            double (&sum)[2]) {
-  constexpr int V = BF16 ? 8 : 4, chunk = adamw_norm_chunk(BF16);
+// Every stride-th chunk from c on, below `end`, by THREADS threads; first: the
+// table's, a lane three of them; CACHED: the update pass reads them again soon.
+template <bool BF16, bool CACHED, int THREADS>
+__device__ __forceinline__ void norm_chunks(const AdamNormTable& tab, const int (&first)[kAdamNormTensors / 64], int stride, int end,
+                                            int& c, double (&sum)[2]) {
+  constexpr int V = BF16 ? 8 : 4, chunk = adamw_norm_chunk(BF16, THREADS);
+  const int thread = threadIdx.x % THREADS;
   static_assert(kAdamNormTensors == 192, "three words of first[] a lane");
   auto load = [&](int i, u32x4 (&raw)[kAdamNormVecs]) {
     int k = -1;
@@ -276,19 +277,19 @@ __device__ __forceinline__ void norm_chunks(const AdamNormTable& tab, const int 
     if (at + chunk <= n) {
 #pragma unroll
       for (int u = 0; u < kAdamNormVecs; ++u)
-        raw[u] = load_raw<true, BF16, V, CACHED>(tab.grad[k], at + (u * kAdamNormThreads + threadIdx.x) * V, n);
+        raw[u] = load_raw<true, BF16, V, CACHED>(tab.grad[k], at + (u * THREADS + thread) * V, n);
     } else {
 #pragma unroll
       for (int u = 0; u < kAdamNormVecs; ++u)
-        raw[u] = load_raw<false, BF16, V>(tab.grad[k], at + (u * kAdamNormThreads + threadIdx.x) * V, n);
+        raw[u] = load_raw<false, BF16, V>(tab.grad[k], at + (u * THREADS + thread) * V, n);
     }
   };
   if (c >= end) return;
   u32x4 raw[kAdamNormVecs];
   load(c, raw);
-  for (; c < end; c += gridDim.x) {
+  for (; c < end; c += stride) {
     u32x4 next[kAdamNormVecs] = {};
-    if (c + static_cast<int>(gridDim.x) < end) load(c + gridDim.x, next);
+    if (c + stride < end) load(c + stride, next);
 #pragma unroll
     for (int u = 0; u < kAdamNormVecs; ++u) {
 #pragma unroll
@@ -312,14 +313,13 @@ __device__ __forceinline__ void norm_chunks(const AdamNormTable& tab, const int 
 // 439).  Squares are exact in fp64.
 template <bool BF16>
 __global__ __launch_bounds__(kAdamNormThreads) void adamw_norm_kernel(const AdamNormTable tab, double* partials) {
-  const int lane = threadIdx.x & 63;
   int first[kAdamNormTensors / 64];
 #pragma unroll
-  for (int h = 0; h < kAdamNormTensors / 64; ++h) first[h] = tab.first[64 * h + lane];
+  for (int h = 0; h < kAdamNormTensors / 64; ++h) first[h] = tab.first[64 * h + (threadIdx.x & 63)];
   double sum[2] = {0.0, 0.0};
   int c = blockIdx.x;
-  norm_chunks<BF16, false>(tab, first, min(tab.keep, tab.chunks), c, sum);
-  norm_chunks<BF16, true>(tab, first, tab.chunks, c, sum);
+  norm_chunks<BF16, false, kAdamNormThreads>(tab, first, gridDim.x, min(tab.keep, tab.chunks), c, sum);
+  norm_chunks<BF16, true, kAdamNormThreads>(tab, first, gridDim.x, tab.chunks, c, sum);
   const double s = block_sum<kAdamNormThreads>(sum[0] + sum[1]);
   if (threadIdx.x == 0) partials[blockIdx.x] = s;
 }
@@ -343,15 +343,8 @@ __device__ __forceinline__ double power(double x, int64_t t) {
   return r;
 }
 
-__global__ __launch_bounds__(kAdamDecideThreads) void adamw_decide_kernel(const double* partials, int count,
-                                                                          const double* sumsq, const AdamCall call,
-                                                                          const AdamHyper hyper, AdamRecord* rec) {
-  double s = 0.0;
-  if (sumsq)
-    s = *sumsq;
-  else if (count > 0)
-    s = sum_partials(partials, count);
-  if (threadIdx.x != 0) return;
+// The record of a call whose S is `s`, by one thread.
+__device__ __forceinline__ void decide(double s, const AdamCall& call, const AdamHyper& hyper, AdamRecord* rec) {
   AdamRecord r = *rec;
   float clip = 1.f;
   r.skip = 0;
@@ -375,6 +368,34 @@ __global__ __launch_bounds__(kAdamDecideThreads) void adamw_decide_kernel(const 
     r.key = mix(mix(call.seed) + static_cast<uint64_t>(r.step));
   }
   *rec = r;
+}
+
+__global__ __launch_bounds__(kAdamDecideThreads) void adamw_decide_kernel(const double* partials, int count,
+                                                                          const double* sumsq, const AdamCall call,
+                                                                          const AdamHyper hyper, AdamRecord* rec) {
+  double s = 0.0;
+  if (sumsq)
+    s = *sumsq;
+  else if (count > 0)
+    s = sum_partials(partials, count);
+  if (threadIdx.x == 0) decide(s, call, hyper, rec);
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kAdamSmallThreads) void adamw_small_kernel(const AdamNormTable tab, double* out, const AdamCall call,
+                                                                        const AdamHyper hyper, AdamRecord* rec) {
+  int first[kAdamNormTensors / 64];
+#pragma unroll
+  for (int h = 0; h < kAdamNormTensors / 64; ++h) first[h] = tab.first[64 * h + (threadIdx.x & 63)];
+  double sum[2] = {0.0, 0.0};
+  int c = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  norm_chunks<BF16, true, 64>(tab, first, kAdamSmallThreads / 64, tab.chunks, c, sum);
+  const double s = block_sum<kAdamSmallThreads>(sum[0] + sum[1]);
+  if (threadIdx.x != 0) return;
+  if (out)
+    *out = s;
+  else
+    decide(s, call, hyper, rec);
 }
 
 // Which tensor, and where in it, a block works.  Blocks are taken from the
@@ -589,6 +610,12 @@ uint64_t adamw_key(uint64_t seed, uint64_t t) { return mix(mix(seed) + t); }
 hipError_t launch_adamw_norm(bool bf16, int blocks, const AdamNormTable& table, double* partials, hipStream_t stream) {
   return launch<AdamNormTable, double*>(bf16 ? adamw_norm_kernel<true> : adamw_norm_kernel<false>, blocks,
                                         kAdamNormThreads, 0, stream, table, partials);
+}
+
+hipError_t launch_adamw_small(bool bf16, const AdamNormTable& table, double* out, const AdamCall& call,
+                              const AdamHyper& hyper, AdamRecord* rec, hipStream_t stream) {
+  return launch<AdamNormTable, double*, AdamCall, AdamHyper, AdamRecord*>(
+      bf16 ? adamw_small_kernel<true> : adamw_small_kernel<false>, 1, kAdamSmallThreads, 0, stream, table, out, call, hyper, rec);
 }
 
 hipError_t launch_adamw_sum(const double* partials, int count, double* out, hipStream_t stream) {

@@ -164,40 +164,61 @@ edit_status_t check_state_arrays(const edit_adamw* h, const edit_adamw_tensors_t
   return EDIT_OK;
 }
 
-// Partial sums of the gradients' squares; *count: how many there are.  `again`:
-// the update pass reads them next.
-edit_status_t enqueue_norm(edit_adamw* h, const void* const* grad, bool again, int* count, hipStream_t s) {
-  const int most = kAdamNormBlocksPerCu * h->num_cu, tensors = static_cast<int>(h->numel.size());
-  const int chunk = adamw_norm_chunk(h->grad_bf16);
-  int64_t left = 0;  // chunks of this launch and those behind it
-  for (int k = 0; k < tensors; ++k)
-    if (grad[k]) left += chunks_of(h->numel[k], chunk);
-  const int64_t keep = again ? kAdamNormKeep / (chunk * (h->grad_bf16 ? 2 : 4)) : 0;
-  *count = 0;
-  for (int k = 0; k < tensors;) {
-    AdamNormTable t;
-    int used = 0;
-    int64_t chunks = 0;
-    for (; k < tensors && used < kAdamNormTensors; ++k) {
-      if (!grad[k] || h->numel[k] == 0) continue;
-      const int64_t more = chunks_of(h->numel[k], chunk);
-      if (chunks + more > INT32_MAX / 2) break;
-      t.first[used] = static_cast<int32_t>(chunks);
-      t.numel[used] = h->numel[k];
-      t.grad[used++] = grad[k];
-      chunks += more;
-    }
-    if (used == 0) continue;
-    std::fill(t.first + used, t.first + kAdamNormTensors, INT32_MAX);
-    t.chunks = static_cast<int32_t>(chunks);
-    t.keep = static_cast<int32_t>(std::min(std::max<int64_t>(left - keep, 0), chunks));
-    left -= chunks;
-    const int blocks = static_cast<int>(std::min<int64_t>(chunks, most));
-    const hipError_t e = launch_adamw_norm(h->grad_bf16, blocks, t, h->partials + *count, s);
-    if (e != hipSuccess) return afail_hip(e, "norm pass launch");
-    *count += blocks;
+// The gradients from tensor *k on that a table has room for.
+void fill_norm_table(const edit_adamw* h, const void* const* grad, int chunk, int* k, AdamNormTable* t) {
+  int used = 0;
+  int64_t chunks = 0;
+  for (; *k < static_cast<int>(h->numel.size()) && used < kAdamNormTensors; ++*k) {
+    if (!grad[*k] || h->numel[*k] == 0) continue;
+    const int64_t more = chunks_of(h->numel[*k], chunk);
+    if (chunks + more > INT32_MAX / 2) break;
+    t->first[used] = static_cast<int32_t>(chunks);
+    t->numel[used] = h->numel[*k];
+    t->grad[used++] = grad[*k];
+    chunks += more;
   }
-  return EDIT_OK;
+  std::fill(t->first + used, t->first + kAdamNormTensors, INT32_MAX);
+  t->chunks = static_cast<int32_t>(chunks);
+  t->keep = t->chunks;
+}
+
+// S of the gradients, to *out, or with no `out` into the record that the update
+// pass goes by.
+edit_status_t enqueue_sum(edit_adamw* h, const void* const* grad, double* out, const AdamCall& call, hipStream_t s) {
+  const int tensors = static_cast<int>(h->numel.size()), chunk = adamw_norm_chunk(h->grad_bf16);
+  int64_t left = 0, waves = 0;  // chunks of this launch and those behind it; ones of a wave
+  int present = 0;
+  for (int k = 0; k < tensors; ++k)
+    if (grad[k] && h->numel[k]) {
+      left += chunks_of(h->numel[k], chunk);
+      waves += chunks_of(h->numel[k], adamw_norm_chunk(h->grad_bf16, 64));
+      ++present;
+    }
+  hipError_t e = hipSuccess;
+  int k = 0;
+  if (present <= kAdamNormTensors && waves <= kAdamSmallChunks) {
+    AdamNormTable t;
+    fill_norm_table(h, grad, adamw_norm_chunk(h->grad_bf16, 64), &k, &t);
+    e = launch_adamw_small(h->grad_bf16, t, out, call, h->hyper, h->rec, s);
+    return e == hipSuccess ? EDIT_OK : afail_hip(e, "norm pass launch");
+  }
+  // the update pass reads the gradients next, the last ones first
+  const int64_t keep = out ? 0 : kAdamNormKeep / (chunk * (h->grad_bf16 ? 2 : 4));
+  int count = 0;
+  while (k < tensors) {
+    AdamNormTable t;
+    fill_norm_table(h, grad, chunk, &k, &t);
+    if (t.chunks == 0) continue;
+    t.keep = static_cast<int32_t>(std::min<int64_t>(std::max<int64_t>(left - keep, 0), t.chunks));
+    left -= t.chunks;
+    const int blocks = std::min(t.chunks, kAdamNormBlocksPerCu * h->num_cu);
+    if ((e = launch_adamw_norm(h->grad_bf16, blocks, t, h->partials + count, s)) != hipSuccess)
+      return afail_hip(e, "norm pass launch");
+    count += blocks;
+  }
+  e = out ? launch_adamw_sum(h->partials, count, out, s)
+          : launch_adamw_decide(h->partials, count, nullptr, call, h->hyper, h->rec, s);
+  return e == hipSuccess ? EDIT_OK : afail_hip(e, "decision launch");
 }
 
 // Calls launch(blocks, table) for every table of tensors, the last ones first;
@@ -332,10 +353,7 @@ edit_status_t edit_adamw_sumsq(edit_adamw_t h, const void* const* grad, double* 
     if (h->numel[k] && grad[k]) ADAM_TRY(note(&h->kind[1], grad[k], size * h->numel[k], size, "grad", static_cast<int>(k)));
   ADAM_TRY(check_overlaps(h, 1u));
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  int count = 0;
-  ADAM_TRY(enqueue_norm(h, grad, false, &count, s));
-  const hipError_t e = launch_adamw_sum(h->partials, count, sumsq, s);
-  return e == hipSuccess ? EDIT_OK : afail_hip(e, "sum launch");
+  return enqueue_sum(h, grad, sumsq, AdamCall{}, s);
 }
 
 edit_status_t edit_adamw_step(edit_adamw_t h, const edit_adamw_tensors_t* t, const edit_adamw_call_t* call, void* stream) {
@@ -372,10 +390,12 @@ edit_status_t edit_adamw_step(edit_adamw_t h, const edit_adamw_tensors_t* t, con
   c.max_norm = call->max_norm > 0.0 ? call->max_norm : INFINITY;
   c.seed = call->seed;
   c.check = call->max_norm > 0.0 || call->sumsq;
-  int count = 0;
-  if (c.check && !call->sumsq) ADAM_TRY(enqueue_norm(h, t->grad, true, &count, s));
-  const hipError_t e = launch_adamw_decide(h->partials, count, call->sumsq, c, h->hyper, h->rec, s);
-  if (e != hipSuccess) return afail_hip(e, "decision launch");
+  if (c.check && !call->sumsq) {
+    ADAM_TRY(enqueue_sum(h, t->grad, nullptr, c, s));
+  } else {
+    const hipError_t e = launch_adamw_decide(h->partials, 0, call->sumsq, c, h->hyper, h->rec, s);
+    if (e != hipSuccess) return afail_hip(e, "decision launch");
+  }
   return for_tables(
       h, adamw_chunk(h->param_bf16, h->grad_bf16, h->held),
       [&](int k, AdamTensor* to) {
