@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+from array import array
 from dataclasses import dataclass
 from typing import List, Optional, Sequence, Union
 
@@ -139,17 +140,20 @@ class AdamW:
         """Host array of the tensors' pointers; `per`: elements for each of theirs."""
         if len(tensors) != len(self._numel):
             raise ValueError(f"expected {len(self._numel)} tensors in {what}, got {len(tensors)}")
-        out = (ctypes.c_void_p * max(1, len(self._numel)))()
-        for k, (t, n) in enumerate(zip(tensors, self._numel)):
+        place = self.device.index if self.device.type == "cuda" else -1
+        out = array("Q")
+        for t, n in zip(tensors, self._numel):
             if t is None and optional:
+                out.append(0)
                 continue
+            if per != 1:
+                n = -(-n // per)
             if not isinstance(t, torch.Tensor):
-                raise TypeError(f"{what}[{k}] must be a torch.Tensor")
-            n = -(-n // per)
-            if t.device != self.device or t.dtype != dtype or not t.is_contiguous() or t.numel() != n:
-                raise ValueError(f"{what}[{k}] must be a contiguous {dtype} tensor of {n} elements on {self.device}")
-            out[k] = t.data_ptr()
-        return out
+                raise TypeError(f"{what}[{len(out)}] must be a torch.Tensor")
+            if t.dtype is not dtype or t.get_device() != place or t.numel() != n or not t.is_contiguous():
+                raise ValueError(f"{what}[{len(out)}] must be a contiguous {dtype} tensor of {n} elements on {self.device}")
+            out.append(t.data_ptr())
+        return (ctypes.c_void_p * max(1, len(out))).from_buffer(out if out else array("Q", [0]))
 
     def _state_pointers(self, state: AdamWState) -> list:
         if not isinstance(state, AdamWState):

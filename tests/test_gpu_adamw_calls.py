@@ -99,12 +99,11 @@ def test_states_change_over_in_mid_run():
         small.step(q, g, b, 1e-3, seed=3)
         full.step(p, g, a, 1e-3)
         assert full.state_get().step == small.state_get().step == 4
-        m2, v2 = small.unpack(b)
         for k, n in enumerate(sizes):
-            old = (m[k].double().cpu().numpy(), v[k].double().cpu().numpy())
-            want = 0.9 * old[0] + 0.1 * g[k].double().cpu().numpy()
+            x, y, z = (s[k].double().cpu().numpy() for s in (m, v, g))
             w, _ = ref.words(3, 4, k, np.arange(n))
-            ref.assert_held(b.exp_avg[k], b.exp_avg_scale[k], want.astype(np.float32), w, False, "m")
+            ref.assert_held(b.exp_avg[k], b.exp_avg_scale[k], (0.9 * x + 0.1 * z).astype(np.float32), w, False, "m")
+            ref.assert_held(b.exp_avg_sq[k], b.exp_avg_sq_scale[k], (0.95 * y + 0.05 * z * z).astype(np.float32), w, True, "v")
             assert torch.isfinite(q[k]).all()
 
 
