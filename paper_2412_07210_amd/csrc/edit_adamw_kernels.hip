@@ -57,12 +57,13 @@ struct RawOf<true, 4> {
 template <bool BF16, int V>
 using Raw = typename RawOf<BF16, V>::T;
 
-// Elements [at, at + V) of a buffer of `numel` > 0, zeros behind its end; FULL:
-// all of them are there.  Parameters and gradients begin at any element.  Next to
-// the end the elements are loaded one by one, the last one in place of those
-// behind it, so that no load waits for a branch.
+// Elements [at, at + V) behind `base`, zeros from `left` > 0 on; FULL: all of them
+// are there.  Parameters and gradients begin at any element.  `base` is the same in
+// all lanes and `at` short, so that an address is one register.  Next to the end
+// the elements are loaded one by one, the last one in place of those behind it, so
+// that no load waits for a branch.
 template <bool FULL, bool BF16, int V, bool CACHED = false>
-__device__ __forceinline__ Raw<BF16, V> load_raw(const void* base, int64_t at, int64_t numel) {
+__device__ __forceinline__ Raw<BF16, V> load_raw(const void* base, uint32_t at, uint32_t left) {
   typedef Raw<BF16, V> T;
   typedef T T_any __attribute__((aligned(BF16 ? 2 : 4)));
   typedef typename std::conditional<BF16, uint16_t, uint32_t>::type E;
@@ -72,24 +73,33 @@ __device__ __forceinline__ Raw<BF16, V> load_raw(const void* base, int64_t at, i
   T raw = {};
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    const bool in = at + e < numel;
-    const uint32_t x = p[in ? at + e : numel - 1];
+    const bool in = at + e < left;
+    const uint32_t x = p[in ? at + e : left - 1];
     raw[BF16 ? e >> 1 : e] |= (in ? x : 0u) << (BF16 ? 16 * (e & 1) : 0);
   }
   return raw;
 }
 template <bool FULL, bool BF16, int V>
-__device__ __forceinline__ void store_raw(void* base, int64_t at, int64_t numel, Raw<BF16, V> raw) {
+__device__ __forceinline__ void store_raw(void* base, uint32_t at, uint32_t left, Raw<BF16, V> raw) {
   typedef Raw<BF16, V> T_any __attribute__((aligned(BF16 ? 2 : 4)));
   typedef typename std::conditional<BF16, uint16_t, uint32_t>::type E;
-  E* p = static_cast<E*>(base) + at;
+  E* p = static_cast<E*>(base);
   if constexpr (FULL) {
-    __builtin_nontemporal_store(raw, reinterpret_cast<T_any*>(p));
+    __builtin_nontemporal_store(raw, reinterpret_cast<T_any*>(p + at));
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e)
-      if (at + e < numel) p[e] = static_cast<E>(BF16 ? raw[e >> 1] >> (16 * (e & 1)) : raw[e]);
+      if (at + e < left) p[at + e] = static_cast<E>(BF16 ? raw[e >> 1] >> (16 * (e & 1)) : raw[e]);
   }
+}
+// Element `at` of a buffer, for all lanes.
+template <bool BF16>
+__device__ __forceinline__ const void* element_at(const void* base, int64_t at) {
+  return static_cast<const char*>(base) + at * (BF16 ? 2 : 4);
+}
+template <bool BF16>
+__device__ __forceinline__ void* element_at(void* base, int64_t at) {
+  return static_cast<char*>(base) + at * (BF16 ? 2 : 4);
 }
 template <bool BF16, int V>
 __device__ __forceinline__ float element(const Raw<BF16, V>& raw, int e) {
@@ -106,33 +116,33 @@ template <int V>
 using Codes = typename CodesOf<V>::T;
 
 template <bool FULL, int V>
-__device__ __forceinline__ Codes<V> load_codes(const void* base, int64_t at, int64_t numel) {
+__device__ __forceinline__ Codes<V> load_codes(const void* base, uint32_t at, uint32_t left) {
   const uint8_t* p = static_cast<const uint8_t*>(base);
   if constexpr (FULL) return __builtin_nontemporal_load(reinterpret_cast<const Codes<V>*>(p + at));
   Codes<V> raw = {};
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    const bool in = at + e < numel;
-    const uint32_t x = p[in ? at + e : numel - 1];
+    const bool in = at + e < left;
+    const uint32_t x = p[in ? at + e : left - 1];
     raw[e >> 2] |= (in ? x : 0u) << (8 * (e & 3));
   }
   return raw;
 }
 template <bool FULL, int V>
-__device__ __forceinline__ void store_codes(void* base, int64_t at, int64_t numel, Codes<V> raw) {
-  uint8_t* p = static_cast<uint8_t*>(base) + at;
+__device__ __forceinline__ void store_codes(void* base, uint32_t at, uint32_t left, Codes<V> raw) {
+  uint8_t* p = static_cast<uint8_t*>(base);
   if constexpr (FULL) {
-    __builtin_nontemporal_store(raw, reinterpret_cast<Codes<V>*>(p));
+    __builtin_nontemporal_store(raw, reinterpret_cast<Codes<V>*>(p + at));
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e)
-      if (at + e < numel) p[e] = static_cast<uint8_t>(raw[e >> 2] >> (8 * (e & 3)));
+      if (at + e < left) p[at + e] = static_cast<uint8_t>(raw[e >> 2] >> (8 * (e & 3)));
   }
 }
-// Index of the scale of element `at`, the last one's behind the end.
+// Index of the scale of element `at`, the last one's from `left` on.
 template <bool FULL>
-__device__ __forceinline__ int64_t scale_index(int64_t at, int64_t numel) {
-  return (FULL || at < numel ? at : numel - 1) / EDIT_ADAMW_BLOCK;
+__device__ __forceinline__ uint32_t scale_index(uint32_t at, uint32_t left) {
+  return (FULL || at < left ? at : left - 1) / EDIT_ADAMW_BLOCK;
 }
 template <int V>
 __device__ __forceinline__ void decode(const Codes<V>& raw, float (&x)[V]) {
@@ -203,7 +213,7 @@ __device__ __forceinline__ Codes<V> encode(const float (&x)[V], uint32_t exponen
   Codes<V> raw = {};
 #pragma unroll
   for (int h = 0; h < V / 4; ++h) {
-    int w = 0;
+    int w;
 #define EDIT_ADAMW_CODE(I)                                                             \
   {                                                                                    \
     float y = x[4 * h + I];                                                            \
@@ -212,6 +222,7 @@ __device__ __forceinline__ Codes<V> encode(const float (&x)[V], uint32_t exponen
       y = __uint_as_float(max(__float_as_uint(y), least)); /* as bits: keeps a NaN */  \
       r = __builtin_amdgcn_alignbit(r, r, 16);                                         \
     }                                                                                  \
+    if constexpr (I == 0) w = r; /* any register that is free: four bytes follow */    \
     w = __builtin_amdgcn_cvt_scalef32_sr_fp8_f32(w, y, r, scale, I);                   \
   }
     EDIT_ADAMW_CODE(0) EDIT_ADAMW_CODE(1) EDIT_ADAMW_CODE(2) EDIT_ADAMW_CODE(3)
@@ -229,8 +240,9 @@ __device__ __forceinline__ Raw<BF16, V> rounded(const float (&x)[V], const uint3
   if constexpr (BF16) {
 #pragma unroll
     for (int e = 0; e < V; e += 2) {
-      bf16x2_t h = {};
+      bf16x2_t h;
       if constexpr (SR) {
+        h = __builtin_bit_cast(bf16x2_t, word[e]);  // any register that is free: both halves follow
         h = __builtin_amdgcn_cvt_sr_bf16_f32(h, x[e], word[e], false);
         h = __builtin_amdgcn_cvt_sr_bf16_f32(h, x[e + 1], word[e + 1], true);
       } else {
@@ -273,15 +285,15 @@ __device__ __forceinline__ void norm_chunks(const AdamNormTable& tab, const int 
 #pragma unroll
     for (int h = 0; h < kAdamNormTensors / 64; ++h) k += __popcll(__ballot(first[h] <= i));
     const int begin = __builtin_amdgcn_readlane(k < 64 ? first[0] : k < 128 ? first[1] : first[2], k & 63);
-    const int64_t at = static_cast<int64_t>(i - begin) * chunk, n = tab.numel[k];
-    if (at + chunk <= n) {
+    const int64_t at = static_cast<int64_t>(i - begin) * chunk;
+    const uint32_t left = static_cast<uint32_t>(min(tab.numel[k] - at, static_cast<int64_t>(chunk)));
+    const void* g = element_at<BF16>(tab.grad[k], at);
+    if (left == chunk) {
 #pragma unroll
-      for (int u = 0; u < kAdamNormVecs; ++u)
-        raw[u] = load_raw<true, BF16, V, CACHED>(tab.grad[k], at + (u * THREADS + thread) * V, n);
+      for (int u = 0; u < kAdamNormVecs; ++u) raw[u] = load_raw<true, BF16, V, CACHED>(g, (u * THREADS + thread) * V, left);
     } else {
 #pragma unroll
-      for (int u = 0; u < kAdamNormVecs; ++u)
-        raw[u] = load_raw<false, BF16, V>(tab.grad[k], at + (u * THREADS + thread) * V, n);
+      for (int u = 0; u < kAdamNormVecs; ++u) raw[u] = load_raw<false, BF16, V>(g, (u * THREADS + thread) * V, left);
     }
   };
   if (c >= end) return;
@@ -426,8 +438,14 @@ template <bool FULL, bool PB, bool GB, bool HELD, bool SR, int V, int U>
 __device__ __forceinline__ void step_block(const AdamTensor& t, float decay_factor, int tensor, const AdamHyper& hyper,
                                            const AdamRecord& rec, int64_t begin) {
   if (rec.skip) return;  // here, so that the record is loaded beside the tensor's entry
-  const int64_t n = t.numel;
-  int64_t at[U];
+  void* const pp = element_at<PB>(t.param, begin);
+  const void* const gp = element_at<GB>(t.grad, begin);
+  void* const mp = static_cast<char*>(t.m) + begin * (HELD ? 1 : 4);
+  void* const vp = static_cast<char*>(t.v) + begin * (HELD ? 1 : 4);
+  float* const ms = HELD ? t.m_scale + begin / EDIT_ADAMW_BLOCK : nullptr;
+  float* const vs = HELD ? t.v_scale + begin / EDIT_ADAMW_BLOCK : nullptr;
+  const uint32_t left = static_cast<uint32_t>(min(t.numel - begin, static_cast<int64_t>(kAdamThreads * V * U)));
+  uint32_t at[U];
   Raw<PB, V> p_raw[U];
   Raw<GB, V> g_raw[U];
   Raw<false, 4> m_raw[U], v_raw[U];
@@ -435,17 +453,17 @@ __device__ __forceinline__ void step_block(const AdamTensor& t, float decay_fact
   float m_scale[U], v_scale[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    at[u] = begin + u * kAdamThreads * V + threadIdx.x * V;
-    p_raw[u] = load_raw<FULL, PB, V>(t.param, at[u], n);
-    g_raw[u] = load_raw<FULL, GB, V>(t.grad, at[u], n);
+    at[u] = u * kAdamThreads * V + threadIdx.x * V;
+    p_raw[u] = load_raw<FULL, PB, V>(pp, at[u], left);
+    g_raw[u] = load_raw<FULL, GB, V>(gp, at[u], left);
     if constexpr (HELD) {
-      m_scale[u] = t.m_scale[scale_index<FULL>(at[u], n)];
-      v_scale[u] = t.v_scale[scale_index<FULL>(at[u], n)];
-      m_codes[u] = load_codes<FULL, V>(t.m, at[u], n);
-      v_codes[u] = load_codes<FULL, V>(t.v, at[u], n);
+      m_scale[u] = ms[scale_index<FULL>(at[u], left)];
+      v_scale[u] = vs[scale_index<FULL>(at[u], left)];
+      m_codes[u] = load_codes<FULL, V>(mp, at[u], left);
+      v_codes[u] = load_codes<FULL, V>(vp, at[u], left);
     } else {
-      m_raw[u] = load_raw<FULL, false, V>(t.m, at[u], n);
-      v_raw[u] = load_raw<FULL, false, V>(t.v, at[u], n);
+      m_raw[u] = load_raw<FULL, false, V>(mp, at[u], left);
+      v_raw[u] = load_raw<FULL, false, V>(vp, at[u], left);
     }
   }
   const float clip = rec.clip, root = rec.root, eps = rec.eps;
@@ -479,25 +497,25 @@ __device__ __forceinline__ void step_block(const AdamTensor& t, float decay_fact
     }
     uint32_t word[V], second[V];
     if constexpr (HELD || SR) {
-      const uint32_t base = static_cast<uint32_t>(at[u]) ^ key.k0;  // at is a multiple of V: + e is ^ e
+      const uint32_t base = (static_cast<uint32_t>(begin) + at[u]) ^ key.k0;  // both are multiples of V: + e is ^ e
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         word[e] = random_word(base ^ e, key.k1);
         if constexpr (SR) second[e] = second_word(word[e], key.k0);
       }
     }
-    store_raw<FULL, PB, V>(t.param, at[u], n, rounded<PB, SR, V>(p, second));
+    store_raw<FULL, PB, V>(pp, at[u], left, rounded<PB, SR, V>(p, second));
     if constexpr (HELD) {
       const uint32_t em = block_exponent<true>(m), ev = block_exponent<false>(v);
-      store_codes<FULL, V>(t.m, at[u], n, encode<false>(m, em, word));
-      store_codes<FULL, V>(t.v, at[u], n, encode<true>(v, ev, word));
-      if (at[u] % EDIT_ADAMW_BLOCK == 0 && (FULL || at[u] < n)) {
-        t.m_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(em);
-        t.v_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(ev);
+      store_codes<FULL, V>(vp, at[u], left, encode<true>(v, ev, word));
+      store_codes<FULL, V>(mp, at[u], left, encode<false>(m, em, word));
+      if (at[u] % EDIT_ADAMW_BLOCK == 0 && (FULL || at[u] < left)) {
+        ms[at[u] / EDIT_ADAMW_BLOCK] = scale_of(em);
+        vs[at[u] / EDIT_ADAMW_BLOCK] = scale_of(ev);
       }
     } else {
-      store_raw<FULL, false, V>(t.m, at[u], n, rounded<false, false, V>(m, word));
-      store_raw<FULL, false, V>(t.v, at[u], n, rounded<false, false, V>(v, word));
+      store_raw<FULL, false, V>(mp, at[u], left, rounded<false, false, V>(m, word));
+      store_raw<FULL, false, V>(vp, at[u], left, rounded<false, false, V>(v, word));
     }
   }
 }
@@ -523,22 +541,28 @@ __global__ __launch_bounds__(kAdamThreads, 4) void adamw_step_kernel(const AdamT
 
 template <bool FULL, bool PACK, int V, int U>
 __device__ __forceinline__ void convert_block(const AdamTensor& t, int tensor, uint64_t key64, int64_t begin) {
-  const int64_t n = t.numel;
-  int64_t at[U];
+  void* const m32 = element_at<false>(t.param, begin);
+  void* const v32 = element_at<false>(const_cast<void*>(t.grad), begin);
+  void* const mp = static_cast<char*>(t.m) + begin;
+  void* const vp = static_cast<char*>(t.v) + begin;
+  float* const ms = t.m_scale + begin / EDIT_ADAMW_BLOCK;
+  float* const vs = t.v_scale + begin / EDIT_ADAMW_BLOCK;
+  const uint32_t left = static_cast<uint32_t>(min(t.numel - begin, static_cast<int64_t>(kAdamThreads * V * U)));
+  uint32_t at[U];
   Raw<false, V> m_raw[U], v_raw[U];
   Codes<V> m_codes[U], v_codes[U];
   float m_scale[U], v_scale[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    at[u] = begin + u * kAdamThreads * V + threadIdx.x * V;
+    at[u] = u * kAdamThreads * V + threadIdx.x * V;
     if constexpr (PACK) {
-      m_raw[u] = load_raw<FULL, false, V>(t.param, at[u], n);
-      v_raw[u] = load_raw<FULL, false, V>(t.grad, at[u], n);
+      m_raw[u] = load_raw<FULL, false, V>(m32, at[u], left);
+      v_raw[u] = load_raw<FULL, false, V>(v32, at[u], left);
     } else {
-      m_scale[u] = t.m_scale[scale_index<FULL>(at[u], n)];
-      v_scale[u] = t.v_scale[scale_index<FULL>(at[u], n)];
-      m_codes[u] = load_codes<FULL, V>(t.m, at[u], n);
-      v_codes[u] = load_codes<FULL, V>(t.v, at[u], n);
+      m_scale[u] = ms[scale_index<FULL>(at[u], left)];
+      v_scale[u] = vs[scale_index<FULL>(at[u], left)];
+      m_codes[u] = load_codes<FULL, V>(mp, at[u], left);
+      v_codes[u] = load_codes<FULL, V>(vp, at[u], left);
     }
   }
   const Key key = key_of(key64, tensor, begin);
@@ -547,7 +571,7 @@ __device__ __forceinline__ void convert_block(const AdamTensor& t, int tensor, u
     float m[V], v[V];
     uint32_t word[V];
     if constexpr (PACK) {
-      const uint32_t base = static_cast<uint32_t>(at[u]) ^ key.k0;
+      const uint32_t base = (static_cast<uint32_t>(begin) + at[u]) ^ key.k0;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         m[e] = element<false, V>(m_raw[u], e);
@@ -556,19 +580,19 @@ __device__ __forceinline__ void convert_block(const AdamTensor& t, int tensor, u
       }
       // a negative v, which no step makes, is taken by its size
       const uint32_t em = block_exponent<true>(m), ev = block_exponent<true>(v);
-      store_codes<FULL, V>(t.m, at[u], n, encode<false>(m, em, word));
-      store_codes<FULL, V>(t.v, at[u], n, encode<true>(v, ev, word));
-      if (at[u] % EDIT_ADAMW_BLOCK == 0 && (FULL || at[u] < n)) {
-        t.m_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(em);
-        t.v_scale[at[u] / EDIT_ADAMW_BLOCK] = scale_of(ev);
+      store_codes<FULL, V>(vp, at[u], left, encode<true>(v, ev, word));
+      store_codes<FULL, V>(mp, at[u], left, encode<false>(m, em, word));
+      if (at[u] % EDIT_ADAMW_BLOCK == 0 && (FULL || at[u] < left)) {
+        ms[at[u] / EDIT_ADAMW_BLOCK] = scale_of(em);
+        vs[at[u] / EDIT_ADAMW_BLOCK] = scale_of(ev);
       }
     } else {
       decode<V>(m_codes[u], m);
       decode<V>(v_codes[u], v);
 #pragma unroll
       for (int e = 0; e < V; ++e) m[e] *= m_scale[u], v[e] *= v_scale[u];
-      store_raw<FULL, false, V>(t.param, at[u], n, rounded<false, false, V>(m, word));
-      store_raw<FULL, false, V>(const_cast<void*>(t.grad), at[u], n, rounded<false, false, V>(v, word));
+      store_raw<FULL, false, V>(m32, at[u], left, rounded<false, false, V>(m, word));
+      store_raw<FULL, false, V>(v32, at[u], left, rounded<false, false, V>(v, word));
     }
   }
 }
