@@ -20,9 +20,9 @@ constexpr int kAdamDecideThreads = 512;
 // eight codes are 16 and 8 bytes; with fp32 buffers four, as 16-byte accesses
 // 32 bytes apart run at half the rate.  Twice for 8-bit states, whose loads are
 // short, once for fp32 ones.  us for 308M elements at the best cap below: e4m3
-// states with bf16 parameters and gradients, V U = 8 1 and 8 2, 530 and 508 (4 2
-// 10% more); fp32 and bf16, 8 1, 4 1 and 4 2, 770, 689 and 693; fp32 states, 4 1
-// and 4 2: bf16 1039 and 1105, fp32 1305 and 1515.  Blocks of 256 threads take 0
+// states with bf16 parameters and gradients, V U = 8 1 and 8 2, 520 and 514 (4 2
+// 10% more); fp32 and bf16, 8 1, 4 1 and 4 2, 770, 686 and 690; fp32 states, 4 1
+// and 4 2: bf16 1028 and 1053, fp32 1294 and 1374.  Blocks of 256 threads take 0
 // to 2% more.
 constexpr int adamw_vec(bool param_bf16, bool grad_bf16, bool held) { return param_bf16 && grad_bf16 && held ? 8 : 4; }
 constexpr int adamw_times(bool held) { return held ? 2 : 1; }
@@ -31,17 +31,18 @@ constexpr int adamw_chunk(bool param_bf16, bool grad_bf16, bool held) {
 }
 // Blocks of it that run on a CU, of the 32 that fit: the mix of reads and writes
 // runs faster with fewer of its loads in flight.  us uncapped, capped and (two
-// blocks a CU more and fewer): e4m3 states: bf16 511, 508 (510, 513); bf16 and
-// fp32 gradients 604, none (613 at 22); fp32 and bf16 715, 693 (696, 697); fp32
-// 820, 787 (795, 790).  fp32 states: bf16 1096, 1039 (1045, 1051); bf16 and fp32
-// 1199, 1129 (1143, 1152); fp32 and bf16 1309, 1221 (1231, 1224); fp32 1365, 1307
-// (1308, 1320).
+// blocks a CU more and fewer): e4m3 states: bf16 521, 514 (520, 516); bf16 and
+// fp32 gradients 599, none (616 at 22); fp32 and bf16 709, 690 (691, 696); fp32
+// 813, 792 (793, 798).  fp32 states: bf16 1105, 1028 (1040, 1028); bf16 and fp32
+// 1199, 1129 (1143, 1152); fp32 and bf16 1309, 1221 (1231, 1224); fp32 1404, 1294
+// (1305, 1307).
 constexpr int adamw_resident(bool param_bf16, bool grad_bf16, bool held) {
   if (held) return param_bf16 ? (grad_bf16 ? 22 : 32) : grad_bf16 ? 20 : 18;
   return param_bf16 && grad_bf16 ? 16 : param_bf16 || grad_bf16 ? 14 : 12;
 }
-// Conversions: a lane takes four elements once to pack (308M elements in 461 us;
-// twice 475), twice to unpack, capped (493; 611 uncapped, once 511).
+// Conversions: a lane takes four elements once to pack (308M elements in 458 us,
+// 6.75 TB/s; twice 471), twice to unpack, capped (498, 6.2 TB/s; uncapped 571, once
+// 507).
 constexpr int adamw_convert_times(bool pack) { return pack ? 1 : 2; }
 constexpr int adamw_convert_chunk(bool pack) { return kAdamThreads * 4 * adamw_convert_times(pack); }
 constexpr int kAdamUnpackResident = 18;

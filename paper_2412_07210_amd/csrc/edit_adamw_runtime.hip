@@ -27,6 +27,16 @@ edit_status_t afail_hip(hipError_t e, const char* what) {
   return afail(EDIT_EHIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
+// No exception leaves the library: what the lists and messages of a call throw.
+template <typename F>
+edit_status_t guarded(const F& f) {
+  try {
+    return f();
+  } catch (const std::exception&) {
+    return afail(EDIT_ENOMEM, "host allocation failed");
+  }
+}
+
 constexpr int64_t kMaxNumel = int64_t(1) << 33;
 constexpr int64_t kMaxBlocks = (int64_t(1) << 32) / kAdamThreads - 1;  // of a launch: fewer than 2^32 threads
 static_assert(kMaxNumel / (kAdamThreads * 4) <= kMaxBlocks, "a tensor fits a launch");
@@ -291,6 +301,72 @@ edit_status_t convert(edit_adamw* h, bool pack, const edit_adamw_tensors_t* t, c
       [&](int blocks, const AdamTable& table) { return launch_adamw_convert(pack, blocks, table, adamw_key(seed, 0), s); });
 }
 
+edit_status_t sum_squares(edit_adamw* h, const void* const* grad, double* sumsq, hipStream_t s) {
+  if (!h) return afail(EDIT_EINVAL, "NULL handle");
+  if (!h->numel.empty() && !grad) return afail(EDIT_EINVAL, "grad must not be NULL");
+  ADAM_TRY(check_adamw_device(h));
+  for (Kind& kind : h->kind) kind.clear();
+  ADAM_TRY(note(&h->kind[0], sumsq, 8, 8, "sumsq", 0));
+  const int64_t size = h->grad_bf16 ? 2 : 4;
+  for (size_t k = 0; k < h->numel.size(); ++k)
+    if (h->numel[k] && grad[k]) ADAM_TRY(note(&h->kind[1], grad[k], size * h->numel[k], size, "grad", static_cast<int>(k)));
+  ADAM_TRY(check_overlaps(h, 1u));
+  return enqueue_sum(h, grad, sumsq, AdamCall{}, s);
+}
+
+edit_status_t step(edit_adamw* h, const edit_adamw_tensors_t* t, const edit_adamw_call_t* call, hipStream_t s) {
+  if (!h) return afail(EDIT_EINVAL, "NULL handle");
+  if (!t || !call) return afail(EDIT_EINVAL, "tensors and call must not be NULL");
+  if (!call->lr_device && (!(call->lr >= 0.0) || !std::isfinite(call->lr)))
+    return afail(EDIT_EINVAL, "lr must be finite and >= 0");
+  if (reinterpret_cast<uintptr_t>(call->lr_device) & 7u) return afail(EDIT_EINVAL, "lr_device must be 8-byte aligned");
+  if (reinterpret_cast<uintptr_t>(call->sumsq) & 7u) return afail(EDIT_EINVAL, "sumsq must be 8-byte aligned");
+  if (!(call->max_norm >= 0.0) || !std::isfinite(call->max_norm))
+    return afail(EDIT_EINVAL, "max_norm must be finite and > 0, or 0 for no clip");
+  ADAM_TRY(check_adamw_device(h));
+  const int tensors = static_cast<int>(h->numel.size());
+  for (Kind& kind : h->kind) kind.clear();
+  if (tensors > 0) {
+    if (!t->param || !t->grad) return afail(EDIT_EINVAL, "param and grad must not be NULL");
+    ADAM_TRY(check_state_arrays(h, t));
+  }
+  const int64_t pb = h->param_bf16 ? 2 : 4, gb = h->grad_bf16 ? 2 : 4;
+  for (int k = 0; k < tensors; ++k) {
+    const int64_t n = h->numel[k];
+    if (n == 0 || !t->grad[k]) continue;
+    ADAM_TRY(note(&h->kind[0], t->param[k], pb * n, pb, "param", k));
+    ADAM_TRY(note(&h->kind[1], t->grad[k], gb * n, gb, "grad", k));
+    ADAM_TRY(check_states(h, t, k));
+  }
+  ADAM_TRY(check_overlaps(h, 0x3du));
+
+  AdamCall c = {};
+  c.lr = call->lr;
+  c.lr_device = call->lr_device;
+  c.weight_decay = h->weight_decay;
+  c.max_norm = call->max_norm > 0.0 ? call->max_norm : INFINITY;
+  c.seed = call->seed;
+  c.check = call->max_norm > 0.0 || call->sumsq;
+  if (c.check && !call->sumsq) {
+    ADAM_TRY(enqueue_sum(h, t->grad, nullptr, c, s));
+  } else {
+    const hipError_t e = launch_adamw_decide(h->partials, 0, call->sumsq, c, h->hyper, h->rec, s);
+    if (e != hipSuccess) return afail_hip(e, "decision launch");
+  }
+  return for_tables(
+      h, adamw_chunk(h->param_bf16, h->grad_bf16, h->held),
+      [&](int k, AdamTensor* to) {
+        if (!t->grad[k]) return false;
+        to->param = t->param[k];
+        to->grad = t->grad[k];
+        fill_states(h, t, k, to);
+        return true;
+      },
+      [&](int blocks, const AdamTable& table) {
+        return launch_adamw_step(h->param_bf16, h->grad_bf16, h->held, h->stochastic, blocks, table, h->hyper, h->rec, s);
+      });
+}
+
 }  // namespace
 
 extern "C" {
@@ -343,81 +419,20 @@ edit_status_t edit_adamw_init(const edit_adamw_config_t* cfg, edit_adamw_t* out)
 }
 
 edit_status_t edit_adamw_sumsq(edit_adamw_t h, const void* const* grad, double* sumsq, void* stream) {
-  if (!h) return afail(EDIT_EINVAL, "NULL handle");
-  if (!h->numel.empty() && !grad) return afail(EDIT_EINVAL, "grad must not be NULL");
-  ADAM_TRY(check_adamw_device(h));
-  for (Kind& kind : h->kind) kind.clear();
-  ADAM_TRY(note(&h->kind[0], sumsq, 8, 8, "sumsq", 0));
-  const int64_t size = h->grad_bf16 ? 2 : 4;
-  for (size_t k = 0; k < h->numel.size(); ++k)
-    if (h->numel[k] && grad[k]) ADAM_TRY(note(&h->kind[1], grad[k], size * h->numel[k], size, "grad", static_cast<int>(k)));
-  ADAM_TRY(check_overlaps(h, 1u));
-  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  return enqueue_sum(h, grad, sumsq, AdamCall{}, s);
+  return guarded([&] { return sum_squares(h, grad, sumsq, reinterpret_cast<hipStream_t>(stream)); });
 }
 
 edit_status_t edit_adamw_step(edit_adamw_t h, const edit_adamw_tensors_t* t, const edit_adamw_call_t* call, void* stream) {
-  if (!h) return afail(EDIT_EINVAL, "NULL handle");
-  if (!t || !call) return afail(EDIT_EINVAL, "tensors and call must not be NULL");
-  if (!call->lr_device && (!(call->lr >= 0.0) || !std::isfinite(call->lr)))
-    return afail(EDIT_EINVAL, "lr must be finite and >= 0");
-  if (reinterpret_cast<uintptr_t>(call->lr_device) & 7u) return afail(EDIT_EINVAL, "lr_device must be 8-byte aligned");
-  if (reinterpret_cast<uintptr_t>(call->sumsq) & 7u) return afail(EDIT_EINVAL, "sumsq must be 8-byte aligned");
-  if (!(call->max_norm >= 0.0) || !std::isfinite(call->max_norm))
-    return afail(EDIT_EINVAL, "max_norm must be finite and > 0, or 0 for no clip");
-  ADAM_TRY(check_adamw_device(h));
-  const int tensors = static_cast<int>(h->numel.size());
-  for (Kind& kind : h->kind) kind.clear();
-  if (tensors > 0) {
-    if (!t->param || !t->grad) return afail(EDIT_EINVAL, "param and grad must not be NULL");
-    ADAM_TRY(check_state_arrays(h, t));
-  }
-  const int64_t pb = h->param_bf16 ? 2 : 4, gb = h->grad_bf16 ? 2 : 4;
-  for (int k = 0; k < tensors; ++k) {
-    const int64_t n = h->numel[k];
-    if (n == 0 || !t->grad[k]) continue;
-    ADAM_TRY(note(&h->kind[0], t->param[k], pb * n, pb, "param", k));
-    ADAM_TRY(note(&h->kind[1], t->grad[k], gb * n, gb, "grad", k));
-    ADAM_TRY(check_states(h, t, k));
-  }
-  ADAM_TRY(check_overlaps(h, 0x3du));
-
-  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  AdamCall c = {};
-  c.lr = call->lr;
-  c.lr_device = call->lr_device;
-  c.weight_decay = h->weight_decay;
-  c.max_norm = call->max_norm > 0.0 ? call->max_norm : INFINITY;
-  c.seed = call->seed;
-  c.check = call->max_norm > 0.0 || call->sumsq;
-  if (c.check && !call->sumsq) {
-    ADAM_TRY(enqueue_sum(h, t->grad, nullptr, c, s));
-  } else {
-    const hipError_t e = launch_adamw_decide(h->partials, 0, call->sumsq, c, h->hyper, h->rec, s);
-    if (e != hipSuccess) return afail_hip(e, "decision launch");
-  }
-  return for_tables(
-      h, adamw_chunk(h->param_bf16, h->grad_bf16, h->held),
-      [&](int k, AdamTensor* to) {
-        if (!t->grad[k]) return false;
-        to->param = t->param[k];
-        to->grad = t->grad[k];
-        fill_states(h, t, k, to);
-        return true;
-      },
-      [&](int blocks, const AdamTable& table) {
-        return launch_adamw_step(h->param_bf16, h->grad_bf16, h->held, h->stochastic, blocks, table, h->hyper, h->rec, s);
-      });
+  return guarded([&] { return step(h, t, call, reinterpret_cast<hipStream_t>(stream)); });
 }
-
 edit_status_t edit_adamw_pack(edit_adamw_t h, const float* const* exp_avg, const float* const* exp_avg_sq,
                               const edit_adamw_tensors_t* tensors, uint64_t seed, void* stream) {
-  return convert(h, true, tensors, exp_avg, exp_avg_sq, seed, reinterpret_cast<hipStream_t>(stream));
+  return guarded([&] { return convert(h, true, tensors, exp_avg, exp_avg_sq, seed, reinterpret_cast<hipStream_t>(stream)); });
 }
 
 edit_status_t edit_adamw_unpack(edit_adamw_t h, const edit_adamw_tensors_t* tensors, float* const* exp_avg,
                                 float* const* exp_avg_sq, void* stream) {
-  return convert(h, false, tensors, exp_avg, exp_avg_sq, 0, reinterpret_cast<hipStream_t>(stream));
+  return guarded([&] { return convert(h, false, tensors, exp_avg, exp_avg_sq, 0, reinterpret_cast<hipStream_t>(stream)); });
 }
 
 edit_status_t edit_adamw_state_get(edit_adamw_t h, edit_adamw_state_t* out) {

@@ -134,6 +134,16 @@ def test_hyper_parameters(state, over, sizes, seed):
     run.close()
 
 
+def test_elements_without_a_gradient_stay_at_any_rate():
+    """m = v = 0: a quotient of zero, however large or small the rate is."""
+    p, g = [randn(700, 1)], [torch.zeros(700, device=DEV)]
+    with AdamW(AdamWConfig([700], "f32", weight_decay=0.0, eps=1e-12), DEV) as o:
+        s, keep = o.new_state(), p[0].clone()
+        for lr in (0.0, 1e-300, 1e-3, 1e30, 1e300):
+            o.step(p, g, s, lr)
+            assert torch.equal(p[0], keep), lr
+
+
 @pytest.mark.parametrize("std", [1e-18, 1e-9, 1e3, 1e15])
 @pytest.mark.parametrize("state", ["f32", "e4m3"])
 def test_gradients_of_any_size(state, std):
