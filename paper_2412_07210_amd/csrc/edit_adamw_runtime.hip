@@ -10,6 +10,7 @@
 
 #include "edit_adamw_internal.h"
 #include "edit_group_internal.h"
+#include "written_ranges.h"
 
 using namespace edit;
 
@@ -43,22 +44,6 @@ static_assert(kMaxNumel / (kAdamThreads * 4) <= kMaxBlocks, "a tensor fits a lau
 
 int64_t chunks_of(int64_t numel, int64_t chunk) { return (numel + chunk - 1) / chunk; }
 
-struct Range {
-  uintptr_t lo, hi;
-};
-
-// Buffers of one kind, as a call lists them.
-struct Kind {
-  std::vector<Range> ranges;
-  uintptr_t lo = UINTPTR_MAX, hi = 0;  // around all of them
-  bool ascending = true;               // and disjoint
-  void clear() { ranges.clear(), lo = UINTPTR_MAX, hi = 0, ascending = true; }
-  void add(Range r) {
-    ascending = ascending && r.lo >= hi;
-    lo = std::min(lo, r.lo), hi = std::max(hi, r.hi);
-    ranges.push_back(r);
-  }
-};
 constexpr int kKinds = 6;  // parameters, gradients, m, v and their scales; of a conversion the fp32 m and v first
 
 }  // namespace
@@ -72,8 +57,7 @@ struct edit_adamw {
   int device = 0, num_cu = 0;
   AdamRecord* rec = nullptr;
   double* partials = nullptr;  // a norm launch's follow the one's before
-  Kind kind[kKinds];  // of the call being checked
-  std::vector<Range> written, read;
+  WrittenRanges<kKinds> ranges;  // of the call being checked
 };
 
 namespace {
@@ -115,54 +99,36 @@ edit_status_t check_adamw_device(const edit_adamw* h) {
 }
 
 // Notes the buffer of tensor k for the check of overlaps.
-edit_status_t note(Kind* kind, const void* p, int64_t bytes, uintptr_t align, const char* name, int k) {
+edit_status_t note(edit_adamw* h, int kind, const void* p, int64_t bytes, uintptr_t align, const char* name, int k) {
   const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
   if (!p || (lo & (align - 1))) {
     const std::string what = std::string(name) + "[" + std::to_string(k) + "]";
     if (!p) return afail(EDIT_EINVAL, what + " must not be NULL");
     return afail(EDIT_EINVAL, what + " must be " + std::to_string(align) + "-byte aligned");
   }
-  kind->add({lo, lo + static_cast<uintptr_t>(bytes)});
+  h->ranges.add(kind, lo, lo + static_cast<uintptr_t>(bytes));
   return EDIT_OK;
 }
 
-// What is written overlaps nothing; `writes`: a bit for each kind that is.
+// `writes`: a bit for each kind of buffer that the call writes.
 edit_status_t check_overlaps(edit_adamw* h, unsigned writes) {
-  // Mostly every kind lies in a stretch of its own, in order: nothing to sort.
-  bool clear = true;
-  for (int i = 0; i < kKinds; ++i) {
-    const Kind& a = h->kind[i];
-    clear = clear && (a.ascending || !(writes >> i & 1));
-    for (int j = 0; j < i; ++j)
-      if ((writes >> i | writes >> j) & 1) clear = clear && (a.hi <= h->kind[j].lo || h->kind[j].hi <= a.lo);
-  }
-  if (clear) return EDIT_OK;
-  h->written.clear();
-  h->read.clear();
-  for (int i = 0; i < kKinds; ++i) {
-    std::vector<Range>& to = writes >> i & 1 ? h->written : h->read;
-    to.insert(to.end(), h->kind[i].ranges.begin(), h->kind[i].ranges.end());
-  }
-  std::sort(h->written.begin(), h->written.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
-  for (size_t i = 1; i < h->written.size(); ++i)
-    if (h->written[i].lo < h->written[i - 1].hi)
+  switch (h->ranges.find(writes)) {
+    case kOverlapWritten:
       return afail(EDIT_EINVAL, "what is written must not overlap: parameters and states, or one of them twice");
-  // written ranges are disjoint, so ascending at both ends
-  for (const Range& r : h->read) {
-    const auto it = std::upper_bound(h->written.begin(), h->written.end(), r.lo,
-                                     [](uintptr_t lo, const Range& w) { return lo < w.hi; });
-    if (it != h->written.end() && it->lo < r.hi) return afail(EDIT_EINVAL, "what is read must not overlap what is written");
+    case kOverlapRead:
+      return afail(EDIT_EINVAL, "what is read must not overlap what is written");
+    default:
+      return EDIT_OK;
   }
-  return EDIT_OK;
 }
 
 edit_status_t check_states(edit_adamw* h, const edit_adamw_tensors_t* t, int k) {
   const int64_t n = h->numel[k], bytes = h->held ? n : 4 * n, scales = 4 * chunks_of(n, EDIT_ADAMW_BLOCK);
-  ADAM_TRY(note(&h->kind[2], t->exp_avg[k], bytes, 16, "exp_avg", k));
-  ADAM_TRY(note(&h->kind[3], t->exp_avg_sq[k], bytes, 16, "exp_avg_sq", k));
+  ADAM_TRY(note(h, 2, t->exp_avg[k], bytes, 16, "exp_avg", k));
+  ADAM_TRY(note(h, 3, t->exp_avg_sq[k], bytes, 16, "exp_avg_sq", k));
   if (h->held) {
-    ADAM_TRY(note(&h->kind[4], t->exp_avg_scale[k], scales, 4, "exp_avg_scale", k));
-    ADAM_TRY(note(&h->kind[5], t->exp_avg_sq_scale[k], scales, 4, "exp_avg_sq_scale", k));
+    ADAM_TRY(note(h, 4, t->exp_avg_scale[k], scales, 4, "exp_avg_scale", k));
+    ADAM_TRY(note(h, 5, t->exp_avg_sq_scale[k], scales, 4, "exp_avg_sq_scale", k));
   }
   return EDIT_OK;
 }
@@ -281,12 +247,12 @@ edit_status_t convert(edit_adamw* h, bool pack, const edit_adamw_tensors_t* t, c
   ADAM_TRY(check_adamw_device(h));
   if (h->numel.empty()) return EDIT_OK;
   ADAM_TRY(check_state_arrays(h, t));
-  for (Kind& kind : h->kind) kind.clear();
+  h->ranges.clear();
   for (int k = 0; k < static_cast<int>(h->numel.size()); ++k) {
     const int64_t n = h->numel[k];
     if (n == 0) continue;
-    ADAM_TRY(note(&h->kind[0], m[k], 4 * n, 16, "fp32 exp_avg", k));
-    ADAM_TRY(note(&h->kind[1], v[k], 4 * n, 16, "fp32 exp_avg_sq", k));
+    ADAM_TRY(note(h, 0, m[k], 4 * n, 16, "fp32 exp_avg", k));
+    ADAM_TRY(note(h, 1, v[k], 4 * n, 16, "fp32 exp_avg_sq", k));
     ADAM_TRY(check_states(h, t, k));
   }
   ADAM_TRY(check_overlaps(h, pack ? 0x3cu : 0x03u));
@@ -305,11 +271,11 @@ edit_status_t sum_squares(edit_adamw* h, const void* const* grad, double* sumsq,
   if (!h) return afail(EDIT_EINVAL, "NULL handle");
   if (!h->numel.empty() && !grad) return afail(EDIT_EINVAL, "grad must not be NULL");
   ADAM_TRY(check_adamw_device(h));
-  for (Kind& kind : h->kind) kind.clear();
-  ADAM_TRY(note(&h->kind[0], sumsq, 8, 8, "sumsq", 0));
+  h->ranges.clear();
+  ADAM_TRY(note(h, 0, sumsq, 8, 8, "sumsq", 0));
   const int64_t size = h->grad_bf16 ? 2 : 4;
   for (size_t k = 0; k < h->numel.size(); ++k)
-    if (h->numel[k] && grad[k]) ADAM_TRY(note(&h->kind[1], grad[k], size * h->numel[k], size, "grad", static_cast<int>(k)));
+    if (h->numel[k] && grad[k]) ADAM_TRY(note(h, 1, grad[k], size * h->numel[k], size, "grad", static_cast<int>(k)));
   ADAM_TRY(check_overlaps(h, 1u));
   return enqueue_sum(h, grad, sumsq, AdamCall{}, s);
 }
@@ -325,7 +291,7 @@ edit_status_t step(edit_adamw* h, const edit_adamw_tensors_t* t, const edit_adam
     return afail(EDIT_EINVAL, "max_norm must be finite and > 0, or 0 for no clip");
   ADAM_TRY(check_adamw_device(h));
   const int tensors = static_cast<int>(h->numel.size());
-  for (Kind& kind : h->kind) kind.clear();
+  h->ranges.clear();
   if (tensors > 0) {
     if (!t->param || !t->grad) return afail(EDIT_EINVAL, "param and grad must not be NULL");
     ADAM_TRY(check_state_arrays(h, t));
@@ -334,8 +300,8 @@ edit_status_t step(edit_adamw* h, const edit_adamw_tensors_t* t, const edit_adam
   for (int k = 0; k < tensors; ++k) {
     const int64_t n = h->numel[k];
     if (n == 0 || !t->grad[k]) continue;
-    ADAM_TRY(note(&h->kind[0], t->param[k], pb * n, pb, "param", k));
-    ADAM_TRY(note(&h->kind[1], t->grad[k], gb * n, gb, "grad", k));
+    ADAM_TRY(note(h, 0, t->param[k], pb * n, pb, "param", k));
+    ADAM_TRY(note(h, 1, t->grad[k], gb * n, gb, "grad", k));
     ADAM_TRY(check_states(h, t, k));
   }
   ADAM_TRY(check_overlaps(h, 0x3du));
@@ -392,9 +358,7 @@ edit_status_t edit_adamw_init(const edit_adamw_config_t* cfg, edit_adamw_t* out)
     h->weight_decay = cfg->weight_decay;
     h->device = dev;
     h->num_cu = num_cu;
-    for (Kind& kind : h->kind) kind.ranges.reserve(tensors + 1);
-    h->written.reserve(5 * tensors + 1);
-    h->read.reserve(4 * tensors + 1);
+    h->ranges.reserve(tensors + 1);
     // launches of the norm pass: full tables, and ones that end at their count of chunks
     int64_t chunks = 0;
     for (int64_t n : h->numel) chunks += chunks_of(n, adamw_norm_chunk(false));
