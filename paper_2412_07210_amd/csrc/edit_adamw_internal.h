@@ -59,17 +59,26 @@ constexpr int kAdamNormTensors = 192;                    // of one launch
 // 1470, 1467; its fp32 parameters, bf16 gradients, e4m3 states 795, 787, 784, 780, 783.
 constexpr int64_t kAdamNormKeep = int64_t(224) << 20;
 constexpr int adamw_norm_chunk(bool bf16, int threads = kAdamNormThreads) { return threads * kAdamNormVecs * (bf16 ? 8 : 4); }
-// Few gradients: one block takes them all, a wave a chunk, and decides: a launch
-// less.  us of a sum and of a clipped step, so and with one launch more, of 2048
-// bf16 elements in each of 8 tensors: in a graph 2.6 and 5.5, 6.0 and 8.8; 32: 4.3
-// and 5.7, 7.8 and 9.1; 64: 6.2 and 5.7, 11.5 and 10.9, but eager 7.2 and 8.5, 14.2
-// and 15.9.
+// Few gradients: one block takes them all, a wave a chunk, in one launch instead
+// of two.  us of a sum, so and otherwise, of 2048 bf16 elements in each of 8 tensors
+// in a graph 2.6 and 5.5; 32: 4.3 and 5.7; 64: 6.2 and 5.7, but eager 7.2 and 8.5.
 constexpr int kAdamSmallThreads = 1024;
 constexpr int kAdamSmallChunks = 64;
 
-// Device-resident state of a handle and what its next update pass goes by.
+// Calls of few blocks take the decision in every block of the update pass, without
+// a launch of its own.  us in a graph with a decision launch and so, without a clip
+// and with one: fp32, 256 blocks 5.1 and 3.7, 9.6 and 8.3; 2048: 6.1 and 5.0, 8.6
+// and 7.9; 4096: 7.2 and 7.6, 9.9 and 11.5; bf16 with e4m3 states, 512 blocks 6.7
+// and 5.4, 9.5 and 8.4; 2048: 9.0 and 7.7, 11.3 and 11.1; 4096: 12.2 and 11.7, 15.7
+// and 17.0.
+constexpr int kAdamFusedBlocks = 2048;
+
+// Device-resident state of a handle and what its next update pass goes by.  t, the
+// steps taken, is in an array beside it: one for every block of a call that steps
+// all tensors, which reads and writes its own (no block can tell whether another
+// one has counted on already); they are the same between calls.
 struct alignas(16) AdamRecord {
-  int64_t step;      // t: steps taken
+  int64_t step;      // t of the last call that was not left out
   int64_t skipped;   // calls left out because the gradient's norm was not finite
   double norm;       // of the last call that took one
   double lr_decay;   // lr * weight_decay of this call
@@ -100,7 +109,8 @@ struct AdamCall {
   double weight_decay;
   double max_norm;          // infinity: no clip
   uint64_t seed;
-  bool check;               // S is there
+  const double* sums;       // S: the sum of `count` parts, in their order
+  int32_t count;            // 0: there is none, and no check
 };
 
 // Block b works on the tensor whose first[] is the last one that is <= b.
@@ -110,7 +120,7 @@ struct AdamTable {
   AdamTensor tensor[kAdamTensors];
   int32_t base;  // index of tensor[0] among all
 };
-static_assert(sizeof(AdamTable) + 128 <= 4096, "kernel arguments");
+static_assert(sizeof(AdamTable) + sizeof(AdamHyper) + sizeof(AdamCall) + 64 <= 4096, "kernel arguments");
 
 struct AdamNormTable {
   int32_t first[kAdamNormTensors];
@@ -119,20 +129,28 @@ struct AdamNormTable {
   int64_t numel[kAdamNormTensors];
   const void* grad[kAdamNormTensors];
 };
-static_assert(sizeof(AdamNormTable) + sizeof(AdamCall) + 64 <= 4096, "kernel arguments");
+static_assert(sizeof(AdamNormTable) + 64 <= 4096, "kernel arguments");
+
+// The record and t of a handle.
+struct AdamState {
+  AdamRecord* rec;
+  int64_t* steps;
+  int32_t slots;  // of steps, at least 1
+};
 
 hipError_t launch_adamw_norm(bool bf16, int blocks, const AdamNormTable& table, double* partials, hipStream_t stream);
-// The same of few gradients, chunks of a wave, and what follows: *out = S, or
-// with no `out` the record.
-hipError_t launch_adamw_small(bool bf16, const AdamNormTable& table, double* out, const AdamCall& call,
-                              const AdamHyper& hyper, AdamRecord* rec, hipStream_t stream);
+// *out = S of few gradients, chunks of a wave.
+hipError_t launch_adamw_small(bool bf16, const AdamNormTable& table, double* out, hipStream_t stream);
 // out = the sum of `count` partials, in their order.
 hipError_t launch_adamw_sum(const double* partials, int count, double* out, hipStream_t stream);
-// S from `count` partials, or from *sumsq where that is given, and the record.
-hipError_t launch_adamw_decide(const double* partials, int count, const double* sumsq, const AdamCall& call,
-                               const AdamHyper& hyper, AdamRecord* rec, hipStream_t stream);
-hipError_t launch_adamw_step(bool param_bf16, bool grad_bf16, bool held, bool stochastic, int blocks, const AdamTable& table,
-                             const AdamHyper& hyper, const AdamRecord* rec, hipStream_t stream);
+// The record of a call, and t.
+hipError_t launch_adamw_decide(const AdamCall& call, const AdamHyper& hyper, const AdamState& state, hipStream_t stream);
+// `call`: takes the decision itself; `before`: blocks of the call's tables before this one.
+struct AdamKind {
+  bool param_bf16, grad_bf16, held, stochastic;
+};
+hipError_t launch_adamw_step(const AdamKind& kind, int blocks, const AdamTable& table, const AdamHyper& hyper,
+                             const AdamState& state, const AdamCall* call, int before, hipStream_t stream);
 // States in the table's m and v (fp32) from or to the codes in param (of m) and grad (of v).
 hipError_t launch_adamw_convert(bool pack, int blocks, const AdamTable& table, uint64_t key, hipStream_t stream);
 uint64_t adamw_key(uint64_t seed, uint64_t t);

@@ -3,10 +3,11 @@
 //
 //   adamw_norm     streams the gradients once: partial sums of g^2 in fp64;
 //   adamw_sum      their sum, in a fixed order;
-//   adamw_decide   the same sum, the clip, whether the call is left out, the
-//                  step count and the factors that the update goes by;
-//   adamw_small    all of these for few gradients, in one block;
+//   adamw_small    both for few gradients, in one block;
+//   adamw_decide   the sum, the clip, whether the call is left out, the step count
+//                  and the factors that the update goes by;
 //   adamw_step     streams parameters, gradients and states once;
+//   adamw_fused    decides and streams, for calls of few blocks;
 //   adamw_convert  fp32 states to 8-bit ones and back.
 //
 // All of them are bound by memory.  m and v are taken in fp64 and rounded once
@@ -356,12 +357,11 @@ __device__ __forceinline__ double power(double x, int64_t t) {
   return r;
 }
 
-// The record of a call whose S is `s`, by one thread.
-__device__ __forceinline__ void decide(double s, const AdamCall& call, const AdamHyper& hyper, AdamRecord* rec) {
-  AdamRecord r = *rec;
+// What call number t + 1 goes by, whose S is `s`; r holds the record before it.
+__device__ __forceinline__ void decide(double s, int64_t t, const AdamCall& call, const AdamHyper& hyper, AdamRecord& r) {
   float clip = 1.f;
   r.skip = 0;
-  if (call.check) {
+  if (call.count > 0) {
     r.norm = sqrt(s);
     r.skip = !(r.norm <= 1.7976931348623157e308);
     if (!r.skip) clip = static_cast<float>(fmin(call.max_norm / (r.norm + EDIT_ADAMW_CLIP_EPS), 1.0));
@@ -371,7 +371,7 @@ __device__ __forceinline__ void decide(double s, const AdamCall& call, const Ada
     r.clip = 0.f;
   } else {
     const double lr = call.lr_device ? *call.lr_device : call.lr;
-    r.step += 1;
+    r.step = t + 1;
     r.clip = clip;
     r.lr_decay = lr * call.weight_decay;
     // lr = 0 takes the largest numbers: a quotient of zero.  eps stays above what
@@ -381,23 +381,26 @@ __device__ __forceinline__ void decide(double s, const AdamCall& call, const Ada
     r.eps = static_cast<float>(fmin(fmax(over * hyper.eps, 1.2e-38), most));
     r.key = mix(mix(call.seed) + static_cast<uint64_t>(r.step));
   }
-  *rec = r;
 }
 
-__global__ __launch_bounds__(kAdamDecideThreads) void adamw_decide_kernel(const double* partials, int count,
-                                                                          const double* sumsq, const AdamCall call,
-                                                                          const AdamHyper hyper, AdamRecord* rec) {
-  double s = 0.0;
-  if (sumsq)
-    s = *sumsq;
-  else if (count > 0)
-    s = sum_partials(partials, count);
-  if (threadIdx.x == 0) decide(s, call, hyper, rec);
+__global__ __launch_bounds__(kAdamDecideThreads) void adamw_decide_kernel(const AdamCall call, const AdamHyper hyper,
+                                                                          const AdamState state) {
+  __shared__ int64_t now;
+  const double s = sum_partials(call.sums, call.count);
+  if (threadIdx.x == 0) {
+    AdamRecord r = *state.rec;
+    now = state.steps[0];
+    decide(s, now, call, hyper, r);
+    *state.rec = r;
+    if (!r.skip) now = r.step;
+  }
+  __syncthreads();
+  const int64_t t = now;
+  for (int i = threadIdx.x; i < state.slots; i += kAdamDecideThreads) state.steps[i] = t;
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kAdamSmallThreads) void adamw_small_kernel(const AdamNormTable tab, double* out, const AdamCall call,
-                                                                        const AdamHyper hyper, AdamRecord* rec) {
+__global__ __launch_bounds__(kAdamSmallThreads) void adamw_small_kernel(const AdamNormTable tab, double* out) {
   int first[kAdamNormTensors / 64];
 #pragma unroll
   for (int h = 0; h < kAdamNormTensors / 64; ++h) first[h] = tab.first[64 * h + (threadIdx.x & 63)];
@@ -405,11 +408,7 @@ __global__ __launch_bounds__(kAdamSmallThreads) void adamw_small_kernel(const Ad
   int c = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   norm_chunks<BF16, true, 64>(tab, first, kAdamSmallThreads / 64, tab.chunks, c, sum);
   const double s = block_sum<kAdamSmallThreads>(sum[0] + sum[1]);
-  if (threadIdx.x != 0) return;
-  if (out)
-    *out = s;
-  else
-    decide(s, call, hyper, rec);
+  if (threadIdx.x == 0) *out = s;
 }
 
 // Which tensor, and where in it, a block works.  Blocks are taken from the
@@ -526,23 +525,69 @@ __device__ __forceinline__ void step_block(const AdamTensor& t, float decay_fact
   }
 }
 
-// PB, GB: bf16 parameters, gradients; HELD: states in 8 bits; SR: bf16 parameters
-// rounded stochastically.
 template <bool PB, bool GB, bool HELD, bool SR, int V, int U>
-__global__ __launch_bounds__(kAdamThreads, 4) void adamw_step_kernel(const AdamTable tab, const AdamHyper hyper,
-                                                                  const AdamRecord* __restrict__ rec) {
-  constexpr int chunk = kAdamThreads * V * U;
-  const AdamRecord r = *rec;
-  const Place place = place_of(tab, chunk);
+__device__ __forceinline__ void step_tensor(const AdamTable& tab, const Place& place, const AdamHyper& hyper,
+                                            const AdamRecord& r) {
   const AdamTensor t = tab.tensor[place.k];
   const float decay = tab.decay[place.k];
-  if (place.at + chunk <= t.numel) {
+  if (place.at + kAdamThreads * V * U <= t.numel) {
     step_block<true, PB, GB, HELD, SR, V, U>(t, decay, tab.base + place.k, hyper, r, place.at);
   } else {
 #pragma unroll 1
     for (int64_t at = place.at; at < t.numel; at += kAdamThreads * V)
       step_block<false, PB, GB, HELD, SR, V, 1>(t, decay, tab.base + place.k, hyper, r, at);
   }
+}
+
+// PB, GB: bf16 parameters, gradients; HELD: states in 8 bits; SR: bf16 parameters
+// rounded stochastically.
+template <bool PB, bool GB, bool HELD, bool SR, int V, int U>
+__global__ __launch_bounds__(kAdamThreads, 4) void adamw_step_kernel(const AdamTable tab, const AdamHyper hyper,
+                                                                     const AdamRecord* __restrict__ rec) {
+  const AdamRecord r = *rec;
+  step_tensor<PB, GB, HELD, SR, V, U>(tab, place_of(tab, kAdamThreads * V * U), hyper, r);
+}
+
+__device__ __forceinline__ float same(float x) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
+__device__ __forceinline__ uint64_t same(uint64_t x) {
+  return static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x >> 32)))) << 32 |
+         static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x)));
+}
+__device__ __forceinline__ double same(double x) {
+  return __longlong_as_double(static_cast<int64_t>(same(static_cast<uint64_t>(__double_as_longlong(x)))));
+}
+
+// The same with the decision, which comes out alike in every block: S is summed in
+// the same order, and t is the block's own.
+template <bool PB, bool GB, bool HELD, bool SR, int V, int U>
+__global__ __launch_bounds__(kAdamThreads, 4) void adamw_fused_kernel(const AdamTable tab, const AdamHyper hyper,
+                                                                      const AdamCall call, const AdamState state, int before) {
+  const Place place = place_of(tab, kAdamThreads * V * U);
+  const int slot = before + gridDim.x - 1 - blockIdx.x;
+  const int64_t t = state.steps[slot];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < call.count; i += kAdamThreads) s += call.sums[i];
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
+  AdamRecord r = {};
+  decide(s, t, call, hyper, r);
+  if (threadIdx.x == 0) {
+    if (!r.skip) state.steps[slot] = r.step;
+    if (slot == 0) {  // no other block looks at the record
+      AdamRecord out = *state.rec;
+      out.skipped += r.skipped;
+      if (call.count > 0) out.norm = r.norm;
+      out.clip = r.clip;
+      if (!r.skip) out.step = r.step;
+      *state.rec = out;
+    }
+  }
+  r.skip = __builtin_amdgcn_readfirstlane(r.skip);
+  r.clip = same(r.clip), r.root = same(r.root), r.eps = same(r.eps);
+  r.lr_decay = same(r.lr_decay), r.key = same(r.key);
+  step_tensor<PB, GB, HELD, SR, V, U>(tab, place, hyper, r);
 }
 
 template <bool FULL, bool PACK, int V, int U>
@@ -626,11 +671,15 @@ hipError_t launch(void (*kernel)(A...), int blocks, int threads, int lds, hipStr
 }
 
 template <bool PB, bool GB, bool HELD, bool SR>
-hipError_t step(int blocks, const AdamTable& table, const AdamHyper& hyper, const AdamRecord* rec, hipStream_t stream) {
+hipError_t step(int blocks, const AdamTable& table, const AdamHyper& hyper, const AdamState& state, const AdamCall* call,
+                int before, hipStream_t stream) {
   constexpr int V = adamw_vec(PB, GB, HELD), U = adamw_times(HELD), resident = adamw_resident(PB, GB, HELD);
   constexpr int lds = resident == 32 ? 0 : lds_for_blocks(resident, 0, kLdsPerCu);
+  if (call)
+    return launch<AdamTable, AdamHyper, AdamCall, AdamState, int>(adamw_fused_kernel<PB, GB, HELD, SR, V, U>, blocks, kAdamThreads,
+                                                                  lds, stream, table, hyper, *call, state, before);
   return launch<AdamTable, AdamHyper, const AdamRecord*>(adamw_step_kernel<PB, GB, HELD, SR, V, U>, blocks, kAdamThreads, lds,
-                                                         stream, table, hyper, rec);
+                                                         stream, table, hyper, state.rec);
 }
 
 }  // namespace
@@ -642,40 +691,38 @@ hipError_t launch_adamw_norm(bool bf16, int blocks, const AdamNormTable& table, 
                                         kAdamNormThreads, 0, stream, table, partials);
 }
 
-hipError_t launch_adamw_small(bool bf16, const AdamNormTable& table, double* out, const AdamCall& call,
-                              const AdamHyper& hyper, AdamRecord* rec, hipStream_t stream) {
-  return launch<AdamNormTable, double*, AdamCall, AdamHyper, AdamRecord*>(
-      bf16 ? adamw_small_kernel<true> : adamw_small_kernel<false>, 1, kAdamSmallThreads, 0, stream, table, out, call, hyper, rec);
+hipError_t launch_adamw_small(bool bf16, const AdamNormTable& table, double* out, hipStream_t stream) {
+  return launch<AdamNormTable, double*>(bf16 ? adamw_small_kernel<true> : adamw_small_kernel<false>, 1, kAdamSmallThreads, 0,
+                                        stream, table, out);
 }
 
 hipError_t launch_adamw_sum(const double* partials, int count, double* out, hipStream_t stream) {
   return launch<const double*, int, double*>(adamw_sum_kernel, 1, kAdamDecideThreads, 0, stream, partials, count, out);
 }
 
-hipError_t launch_adamw_decide(const double* partials, int count, const double* sumsq, const AdamCall& call,
-                               const AdamHyper& hyper, AdamRecord* rec, hipStream_t stream) {
-  return launch<const double*, int, const double*, AdamCall, AdamHyper, AdamRecord*>(
-      adamw_decide_kernel, 1, count ? kAdamDecideThreads : 64, 0, stream, partials, count, sumsq, call, hyper, rec);
+hipError_t launch_adamw_decide(const AdamCall& call, const AdamHyper& hyper, const AdamState& state, hipStream_t stream) {
+  return launch<AdamCall, AdamHyper, AdamState>(adamw_decide_kernel, 1, kAdamDecideThreads, 0, stream, call, hyper, state);
 }
 
-hipError_t launch_adamw_step(bool param_bf16, bool grad_bf16, bool held, bool stochastic, int blocks, const AdamTable& table,
-                             const AdamHyper& hyper, const AdamRecord* rec, hipStream_t stream) {
-  if (param_bf16) {
-    if (stochastic) {
-      if (grad_bf16) return held ? step<true, true, true, true>(blocks, table, hyper, rec, stream)
-                                 : step<true, true, false, true>(blocks, table, hyper, rec, stream);
-      return held ? step<true, false, true, true>(blocks, table, hyper, rec, stream)
-                  : step<true, false, false, true>(blocks, table, hyper, rec, stream);
-    }
-    if (grad_bf16) return held ? step<true, true, true, false>(blocks, table, hyper, rec, stream)
-                               : step<true, true, false, false>(blocks, table, hyper, rec, stream);
-    return held ? step<true, false, true, false>(blocks, table, hyper, rec, stream)
-                : step<true, false, false, false>(blocks, table, hyper, rec, stream);
-  }
-  if (grad_bf16) return held ? step<false, true, true, false>(blocks, table, hyper, rec, stream)
-                             : step<false, true, false, false>(blocks, table, hyper, rec, stream);
-  return held ? step<false, false, true, false>(blocks, table, hyper, rec, stream)
-              : step<false, false, false, false>(blocks, table, hyper, rec, stream);
+hipError_t launch_adamw_step(const AdamKind& kind, int blocks, const AdamTable& table, const AdamHyper& hyper,
+                             const AdamState& state, const AdamCall* call, int before, hipStream_t stream) {
+#define EDIT_ADAMW_KIND(PB, GB, HELD, SR)                                                                        \
+  if (kind.param_bf16 == PB && kind.grad_bf16 == GB && kind.held == HELD && kind.stochastic == SR)               \
+    return step<PB, GB, HELD, SR>(blocks, table, hyper, state, call, before, stream);
+  EDIT_ADAMW_KIND(true, true, true, true)
+  EDIT_ADAMW_KIND(true, true, false, true)
+  EDIT_ADAMW_KIND(true, false, true, true)
+  EDIT_ADAMW_KIND(true, false, false, true)
+  EDIT_ADAMW_KIND(true, true, true, false)
+  EDIT_ADAMW_KIND(true, true, false, false)
+  EDIT_ADAMW_KIND(true, false, true, false)
+  EDIT_ADAMW_KIND(true, false, false, false)
+  EDIT_ADAMW_KIND(false, true, true, false)
+  EDIT_ADAMW_KIND(false, true, false, false)
+  EDIT_ADAMW_KIND(false, false, true, false)
+  EDIT_ADAMW_KIND(false, false, false, false)
+#undef EDIT_ADAMW_KIND
+  return hipErrorInvalidValue;
 }
 
 hipError_t launch_adamw_convert(bool pack, int blocks, const AdamTable& table, uint64_t key, hipStream_t stream) {

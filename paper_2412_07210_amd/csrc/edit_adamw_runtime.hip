@@ -51,11 +51,13 @@ constexpr int kKinds = 6;  // parameters, gradients, m, v and their scales; of a
 struct edit_adamw {
   std::vector<int64_t> numel;
   std::vector<float> decay;
-  bool param_bf16 = false, grad_bf16 = false, held = false, stochastic = false;
+  AdamKind kind{};
   AdamHyper hyper{};
   double weight_decay = 0.0;
   int device = 0, num_cu = 0;
-  AdamRecord* rec = nullptr;
+  int64_t blocks = 0;  // of the update pass over all tensors
+  char* arena = nullptr;
+  AdamState state{};
   double* partials = nullptr;  // a norm launch's follow the one's before
   WrittenRanges<kKinds> ranges;  // of the call being checked
 };
@@ -123,10 +125,10 @@ edit_status_t check_overlaps(edit_adamw* h, unsigned writes) {
 }
 
 edit_status_t check_states(edit_adamw* h, const edit_adamw_tensors_t* t, int k) {
-  const int64_t n = h->numel[k], bytes = h->held ? n : 4 * n, scales = 4 * chunks_of(n, EDIT_ADAMW_BLOCK);
+  const int64_t n = h->numel[k], bytes = h->kind.held ? n : 4 * n, scales = 4 * chunks_of(n, EDIT_ADAMW_BLOCK);
   ADAM_TRY(note(h, 2, t->exp_avg[k], bytes, 16, "exp_avg", k));
   ADAM_TRY(note(h, 3, t->exp_avg_sq[k], bytes, 16, "exp_avg_sq", k));
-  if (h->held) {
+  if (h->kind.held) {
     ADAM_TRY(note(h, 4, t->exp_avg_scale[k], scales, 4, "exp_avg_scale", k));
     ADAM_TRY(note(h, 5, t->exp_avg_sq_scale[k], scales, 4, "exp_avg_sq_scale", k));
   }
@@ -135,7 +137,7 @@ edit_status_t check_states(edit_adamw* h, const edit_adamw_tensors_t* t, int k) 
 
 edit_status_t check_state_arrays(const edit_adamw* h, const edit_adamw_tensors_t* t) {
   if (!t->exp_avg || !t->exp_avg_sq) return afail(EDIT_EINVAL, "exp_avg and exp_avg_sq must not be NULL");
-  if (h->held && (!t->exp_avg_scale || !t->exp_avg_sq_scale))
+  if (h->kind.held && (!t->exp_avg_scale || !t->exp_avg_sq_scale))
     return afail(EDIT_EINVAL, "exp_avg_scale and exp_avg_sq_scale must not be NULL");
   return EDIT_OK;
 }
@@ -158,49 +160,51 @@ void fill_norm_table(const edit_adamw* h, const void* const* grad, int chunk, in
   t->keep = t->chunks;
 }
 
-// S of the gradients, to *out, or with no `out` into the record that the update
-// pass goes by.
-edit_status_t enqueue_sum(edit_adamw* h, const void* const* grad, double* out, const AdamCall& call, hipStream_t s) {
-  const int tensors = static_cast<int>(h->numel.size()), chunk = adamw_norm_chunk(h->grad_bf16);
+// S of the gradients: to *out, or with no `out` as parts in the workspace, named in *call.
+edit_status_t enqueue_sum(edit_adamw* h, const void* const* grad, double* out, AdamCall* call, hipStream_t s) {
+  const int tensors = static_cast<int>(h->numel.size()), chunk = adamw_norm_chunk(h->kind.grad_bf16);
   int64_t left = 0, waves = 0;  // chunks of this launch and those behind it; ones of a wave
   int present = 0;
   for (int k = 0; k < tensors; ++k)
     if (grad[k] && h->numel[k]) {
       left += chunks_of(h->numel[k], chunk);
-      waves += chunks_of(h->numel[k], adamw_norm_chunk(h->grad_bf16, 64));
+      waves += chunks_of(h->numel[k], adamw_norm_chunk(h->kind.grad_bf16, 64));
       ++present;
     }
   hipError_t e = hipSuccess;
-  int k = 0;
+  int k = 0, count = 0;
   if (present <= kAdamNormTensors && waves <= kAdamSmallChunks) {
     AdamNormTable t;
-    fill_norm_table(h, grad, adamw_norm_chunk(h->grad_bf16, 64), &k, &t);
-    e = launch_adamw_small(h->grad_bf16, t, out, call, h->hyper, h->rec, s);
-    return e == hipSuccess ? EDIT_OK : afail_hip(e, "norm pass launch");
+    fill_norm_table(h, grad, adamw_norm_chunk(h->kind.grad_bf16, 64), &k, &t);
+    e = launch_adamw_small(h->kind.grad_bf16, t, out ? out : h->partials, s);
+    count = 1;
+  } else {
+    // the update pass reads the gradients next, the last ones first
+    const int64_t keep = out ? 0 : kAdamNormKeep / (chunk * (h->kind.grad_bf16 ? 2 : 4));
+    while (e == hipSuccess && k < tensors) {
+      AdamNormTable t;
+      fill_norm_table(h, grad, chunk, &k, &t);
+      if (t.chunks == 0) continue;
+      t.keep = static_cast<int32_t>(std::min<int64_t>(std::max<int64_t>(left - keep, 0), t.chunks));
+      left -= t.chunks;
+      const int blocks = std::min(t.chunks, kAdamNormBlocksPerCu * h->num_cu);
+      e = launch_adamw_norm(h->kind.grad_bf16, blocks, t, h->partials + count, s);
+      count += blocks;
+    }
+    if (e == hipSuccess && out) e = launch_adamw_sum(h->partials, count, out, s);
   }
-  // the update pass reads the gradients next, the last ones first
-  const int64_t keep = out ? 0 : kAdamNormKeep / (chunk * (h->grad_bf16 ? 2 : 4));
-  int count = 0;
-  while (k < tensors) {
-    AdamNormTable t;
-    fill_norm_table(h, grad, chunk, &k, &t);
-    if (t.chunks == 0) continue;
-    t.keep = static_cast<int32_t>(std::min<int64_t>(std::max<int64_t>(left - keep, 0), t.chunks));
-    left -= t.chunks;
-    const int blocks = std::min(t.chunks, kAdamNormBlocksPerCu * h->num_cu);
-    if ((e = launch_adamw_norm(h->grad_bf16, blocks, t, h->partials + count, s)) != hipSuccess)
-      return afail_hip(e, "norm pass launch");
-    count += blocks;
-  }
-  e = out ? launch_adamw_sum(h->partials, count, out, s)
-          : launch_adamw_decide(h->partials, count, nullptr, call, h->hyper, h->rec, s);
-  return e == hipSuccess ? EDIT_OK : afail_hip(e, "decision launch");
+  if (e != hipSuccess) return afail_hip(e, "norm pass launch");
+  if (call) call->sums = h->partials, call->count = count;
+  return EDIT_OK;
 }
 
-// Calls launch(blocks, table) for every table of tensors, the last ones first;
-// fill(k, &tensor): whether tensor k takes part; chunk: elements of a block.
+// Calls launch(blocks, table, before) for every table of tensors, the last ones
+// first; fill(k, &tensor): whether tensor k takes part; chunk: elements of a block;
+// before: blocks of the tensors before the table's, were all to take part.
 template <typename Fill, typename Launch>
 edit_status_t for_tables(const edit_adamw* h, int chunk, const Fill& fill, const Launch& launch) {
+  int64_t before = 0;
+  for (int64_t n : h->numel) before += chunks_of(n, chunk);
   for (int end = static_cast<int>(h->numel.size()), begin = end; end > 0; end = begin) {
     int64_t blocks = 0;
     for (; begin > 0 && end - begin < kAdamTensors; --begin) {
@@ -208,6 +212,7 @@ edit_status_t for_tables(const edit_adamw* h, int chunk, const Fill& fill, const
       if (blocks + more > kMaxBlocks) break;
       blocks += more;
     }
+    before -= blocks;
     AdamTable t;
     t.base = begin;
     blocks = 0;
@@ -224,7 +229,7 @@ edit_status_t for_tables(const edit_adamw* h, int chunk, const Fill& fill, const
     }
     if (blocks == 0) continue;
     std::fill(t.first + (end - begin), t.first + 64, INT32_MAX);
-    const hipError_t e = launch(static_cast<int>(blocks), t);
+    const hipError_t e = launch(static_cast<int>(blocks), t, before);
     if (e != hipSuccess) return afail_hip(e, "update pass launch");
   }
   return EDIT_OK;
@@ -233,7 +238,7 @@ edit_status_t for_tables(const edit_adamw* h, int chunk, const Fill& fill, const
 void fill_states(const edit_adamw* h, const edit_adamw_tensors_t* t, int k, AdamTensor* to) {
   to->m = t->exp_avg[k];
   to->v = t->exp_avg_sq[k];
-  if (h->held) {
+  if (h->kind.held) {
     to->m_scale = t->exp_avg_scale[k];
     to->v_scale = t->exp_avg_sq_scale[k];
   }
@@ -242,7 +247,7 @@ void fill_states(const edit_adamw* h, const edit_adamw_tensors_t* t, int k, Adam
 edit_status_t convert(edit_adamw* h, bool pack, const edit_adamw_tensors_t* t, const float* const* m, const float* const* v,
                       uint64_t seed, hipStream_t s) {
   if (!h) return afail(EDIT_EINVAL, "NULL handle");
-  if (!h->held) return afail(EDIT_EINVAL, "the handle holds its states in fp32");
+  if (!h->kind.held) return afail(EDIT_EINVAL, "the handle holds its states in fp32");
   if (!t || (!h->numel.empty() && (!m || !v))) return afail(EDIT_EINVAL, "tensors, exp_avg and exp_avg_sq must not be NULL");
   ADAM_TRY(check_adamw_device(h));
   if (h->numel.empty()) return EDIT_OK;
@@ -264,7 +269,7 @@ edit_status_t convert(edit_adamw* h, bool pack, const edit_adamw_tensors_t* t, c
         to->grad = v[k];
         return true;
       },
-      [&](int blocks, const AdamTable& table) { return launch_adamw_convert(pack, blocks, table, adamw_key(seed, 0), s); });
+      [&](int blocks, const AdamTable& table, int64_t) { return launch_adamw_convert(pack, blocks, table, adamw_key(seed, 0), s); });
 }
 
 edit_status_t sum_squares(edit_adamw* h, const void* const* grad, double* sumsq, hipStream_t s) {
@@ -273,11 +278,11 @@ edit_status_t sum_squares(edit_adamw* h, const void* const* grad, double* sumsq,
   ADAM_TRY(check_adamw_device(h));
   h->ranges.clear();
   ADAM_TRY(note(h, 0, sumsq, 8, 8, "sumsq", 0));
-  const int64_t size = h->grad_bf16 ? 2 : 4;
+  const int64_t size = h->kind.grad_bf16 ? 2 : 4;
   for (size_t k = 0; k < h->numel.size(); ++k)
     if (h->numel[k] && grad[k]) ADAM_TRY(note(h, 1, grad[k], size * h->numel[k], size, "grad", static_cast<int>(k)));
   ADAM_TRY(check_overlaps(h, 1u));
-  return enqueue_sum(h, grad, sumsq, AdamCall{}, s);
+  return enqueue_sum(h, grad, sumsq, nullptr, s);
 }
 
 edit_status_t step(edit_adamw* h, const edit_adamw_tensors_t* t, const edit_adamw_call_t* call, hipStream_t s) {
@@ -296,9 +301,11 @@ edit_status_t step(edit_adamw* h, const edit_adamw_tensors_t* t, const edit_adam
     if (!t->param || !t->grad) return afail(EDIT_EINVAL, "param and grad must not be NULL");
     ADAM_TRY(check_state_arrays(h, t));
   }
-  const int64_t pb = h->param_bf16 ? 2 : 4, gb = h->grad_bf16 ? 2 : 4;
+  const int64_t pb = h->kind.param_bf16 ? 2 : 4, gb = h->kind.grad_bf16 ? 2 : 4;
+  bool all = true;  // tensors take part
   for (int k = 0; k < tensors; ++k) {
     const int64_t n = h->numel[k];
+    all = all && (n == 0 || t->grad[k]);
     if (n == 0 || !t->grad[k]) continue;
     ADAM_TRY(note(h, 0, t->param[k], pb * n, pb, "param", k));
     ADAM_TRY(note(h, 1, t->grad[k], gb * n, gb, "grad", k));
@@ -312,15 +319,18 @@ edit_status_t step(edit_adamw* h, const edit_adamw_tensors_t* t, const edit_adam
   c.weight_decay = h->weight_decay;
   c.max_norm = call->max_norm > 0.0 ? call->max_norm : INFINITY;
   c.seed = call->seed;
-  c.check = call->max_norm > 0.0 || call->sumsq;
-  if (c.check && !call->sumsq) {
-    ADAM_TRY(enqueue_sum(h, t->grad, nullptr, c, s));
-  } else {
-    const hipError_t e = launch_adamw_decide(h->partials, 0, call->sumsq, c, h->hyper, h->rec, s);
+  if (call->sumsq)
+    c.sums = call->sumsq, c.count = 1;
+  else if (call->max_norm > 0.0)
+    ADAM_TRY(enqueue_sum(h, t->grad, nullptr, &c, s));
+  // where every block has a t of its own, and every one counts it on
+  const bool fused = all && h->blocks > 0 && h->blocks == h->state.slots;
+  if (!fused) {
+    const hipError_t e = launch_adamw_decide(c, h->hyper, h->state, s);
     if (e != hipSuccess) return afail_hip(e, "decision launch");
   }
   return for_tables(
-      h, adamw_chunk(h->param_bf16, h->grad_bf16, h->held),
+      h, adamw_chunk(h->kind.param_bf16, h->kind.grad_bf16, h->kind.held),
       [&](int k, AdamTensor* to) {
         if (!t->grad[k]) return false;
         to->param = t->param[k];
@@ -328,8 +338,8 @@ edit_status_t step(edit_adamw* h, const edit_adamw_tensors_t* t, const edit_adam
         fill_states(h, t, k, to);
         return true;
       },
-      [&](int blocks, const AdamTable& table) {
-        return launch_adamw_step(h->param_bf16, h->grad_bf16, h->held, h->stochastic, blocks, table, h->hyper, h->rec, s);
+      [&](int blocks, const AdamTable& table, int64_t before) {
+        return launch_adamw_step(h->kind, blocks, table, h->hyper, h->state, fused ? &c : nullptr, static_cast<int>(before), s);
       });
 }
 
@@ -350,10 +360,10 @@ edit_status_t edit_adamw_init(const edit_adamw_config_t* cfg, edit_adamw_t* out)
     h->numel.assign(cfg->numel, cfg->numel + tensors);
     h->decay.assign(tensors, 1.f);
     for (size_t k = 0; cfg->decay && k < tensors; ++k) h->decay[k] = static_cast<float>(cfg->decay[k]);
-    h->param_bf16 = cfg->dtype == EDIT_BF16;
-    h->grad_bf16 = cfg->grad_dtype == EDIT_BF16;
-    h->held = cfg->held == EDIT_ADAMW_E4M3;
-    h->stochastic = cfg->flags & EDIT_ADAMW_STOCHASTIC;
+    h->kind.param_bf16 = cfg->dtype == EDIT_BF16;
+    h->kind.grad_bf16 = cfg->grad_dtype == EDIT_BF16;
+    h->kind.held = cfg->held == EDIT_ADAMW_E4M3;
+    h->kind.stochastic = cfg->flags & EDIT_ADAMW_STOCHASTIC;
     h->hyper = {cfg->beta1, cfg->beta2, cfg->eps};
     h->weight_decay = cfg->weight_decay;
     h->device = dev;
@@ -364,17 +374,21 @@ edit_status_t edit_adamw_init(const edit_adamw_config_t* cfg, edit_adamw_t* out)
     for (int64_t n : h->numel) chunks += chunks_of(n, adamw_norm_chunk(false));
     const size_t launches = tensors / kAdamNormTensors + 2 + static_cast<size_t>(2 * (chunks / (INT32_MAX / 2)));
     const size_t partials = launches * kAdamNormBlocksPerCu * num_cu * sizeof(double);
-    char* arena = nullptr;
-    hipError_t e = hipMalloc(reinterpret_cast<void**>(&arena), 256 + partials);
+    const int chunk = adamw_chunk(h->kind.param_bf16, h->kind.grad_bf16, h->kind.held);
+    for (int64_t n : h->numel) h->blocks += chunks_of(n, chunk);
+    h->state.slots = h->blocks > 0 && h->blocks <= kAdamFusedBlocks ? static_cast<int32_t>(h->blocks) : 1;
+    const size_t kept = 256 + (h->state.slots * sizeof(int64_t) + 255) / 256 * 256;  // the record and t, zero at first
+    hipError_t e = hipMalloc(reinterpret_cast<void**>(&h->arena), kept + partials);
     if (e != hipSuccess) return afail(EDIT_ENOMEM, std::string("hipMalloc of the workspace: ") + hipGetErrorString(e));
-    e = hipMemset(arena, 0, 256);
+    e = hipMemset(h->arena, 0, kept);
     if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e != hipSuccess) {
-      (void)hipFree(arena);
+      (void)hipFree(h->arena);
       return afail_hip(e, "edit_adamw_init");
     }
-    h->rec = reinterpret_cast<AdamRecord*>(arena);
-    h->partials = reinterpret_cast<double*>(arena + 256);
+    h->state.rec = reinterpret_cast<AdamRecord*>(h->arena);
+    h->state.steps = reinterpret_cast<int64_t*>(h->arena + 256);
+    h->partials = reinterpret_cast<double*>(h->arena + kept);
     *out = h.release();
     return EDIT_OK;
   } catch (const std::exception&) {  // the lists' host memory
@@ -404,9 +418,11 @@ edit_status_t edit_adamw_state_get(edit_adamw_t h, edit_adamw_state_t* out) {
   ADAM_TRY(check_adamw_device(h));
   hipError_t e = hipDeviceSynchronize();
   AdamRecord r;
-  if (e == hipSuccess) e = hipMemcpy(&r, h->rec, sizeof r, hipMemcpyDeviceToHost);
+  int64_t step = 0;
+  if (e == hipSuccess) e = hipMemcpy(&r, h->state.rec, sizeof r, hipMemcpyDeviceToHost);
+  if (e == hipSuccess) e = hipMemcpy(&step, h->state.steps, sizeof step, hipMemcpyDeviceToHost);
   if (e != hipSuccess) return afail_hip(e, "edit_adamw_state_get");
-  *out = {r.step, r.skipped, r.norm, r.clip};
+  *out = {step, r.skipped, r.norm, r.clip};
   return EDIT_OK;
 }
 
@@ -414,19 +430,22 @@ edit_status_t edit_adamw_state_set(edit_adamw_t h, int64_t step) {
   if (!h) return afail(EDIT_EINVAL, "NULL handle");
   if (step < 0) return afail(EDIT_EINVAL, "step must be >= 0");
   ADAM_TRY(check_adamw_device(h));
-  hipError_t e = hipDeviceSynchronize();
-  if (e == hipSuccess) e = hipMemcpy(&h->rec->step, &step, sizeof step, hipMemcpyHostToDevice);
-  if (e == hipSuccess) e = hipDeviceSynchronize();
-  return e == hipSuccess ? EDIT_OK : afail_hip(e, "edit_adamw_state_set");
+  return guarded([&] {
+    const std::vector<int64_t> steps(h->state.slots, step);
+    hipError_t e = hipDeviceSynchronize();
+    if (e == hipSuccess) e = hipMemcpy(h->state.steps, steps.data(), steps.size() * sizeof step, hipMemcpyHostToDevice);
+    if (e == hipSuccess) e = hipDeviceSynchronize();
+    return e == hipSuccess ? EDIT_OK : afail_hip(e, "edit_adamw_state_set");
+  });
 }
 
 void edit_adamw_destroy(edit_adamw_t h) {
   if (!h) return;
   int prev = -1;
   if (hipGetDevice(&prev) == hipSuccess && prev != h->device) (void)hipSetDevice(h->device);
-  if (h->rec) {
+  if (h->arena) {
     (void)hipDeviceSynchronize();
-    (void)hipFree(h->rec);
+    (void)hipFree(h->arena);
   }
   if (prev >= 0 && prev != h->device) (void)hipSetDevice(prev);
   delete h;

@@ -190,6 +190,32 @@ def test_tables_without_a_gradient():
     run.close()
 
 
+@pytest.mark.parametrize("large", [0, 3_000_000])
+@pytest.mark.parametrize("dtype,state", [("bf16", "e4m3"), ("f32", "f32")])
+def test_calls_with_and_without_every_gradient(dtype, state, large):
+    """Few blocks decide in the update pass where every tensor has a gradient, and in a
+    launch before it otherwise (as many blocks do): t counts on from one to the other,
+    clipped or not, left out or not, set anew or not."""
+    sizes = [700, 0, 5000, 60, 300 + large]
+    run = Run(sizes, dtype, None, state, seed=17, stochastic=dtype == "bf16")
+    full = list(run.grads)
+    for t, missing in enumerate([[], [2], [], [], [0, 3], [4], [], [2]]):
+        run.draw(t)
+        run.no_grad = set(missing)
+        run.grads = [None if k in missing else g for k, g in enumerate(full)]
+        run.step(max_norm=0.2 if t % 3 == 1 else None, seed=t)
+        if t in (3, 4):  # left out in between
+            keep = run.snapshot()
+            full[2 if t == 3 else 4][7] = float("inf")
+            run.opt.step(run.params, run.grads, run.state, 1e-2, max_norm=1.0)
+            assert run.opt.state_get().step == t + 1 and run.opt.state_get().skipped == t - 2
+            assert all(torch.equal(x, y) for x, y in zip(run.snapshot(), keep))
+        if t == 5:
+            run.opt.state_set(6)
+    assert run.opt.state_get().step == 8
+    run.close()
+
+
 def test_no_tensors():
     for sizes in ([], [0], [0, 0]):
         run = Run(sizes, seed=1)
