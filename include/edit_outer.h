@@ -547,7 +547,7 @@ typedef struct {
   const void *const *grad;       /* [numel] of grad_dtype; NULL: tensor k stays as it */
                                  /* is in this call, states included                  */
   void *const *exp_avg;          /* m: [numel] fp32, or e4m3 codes                    */
-  void *const *exp_avg_sq;       /* v                                                 */
+  void *const *exp_avg_sq;       /* v, >= 0                                           */
   float *const *exp_avg_scale;   /* [ceil(numel / EDIT_ADAMW_BLOCK)], E4M3 only       */
   float *const *exp_avg_sq_scale;
 } edit_adamw_tensors_t;
@@ -581,7 +581,8 @@ edit_status_t edit_adamw_sumsq(edit_adamw_t h, const void *const *grad, double *
 /* One step of all tensors, enqueued on `stream`, in place on parameters and
  * states.  If S is there (max_norm > 0 or sumsq) and not finite, the call
  * changes nothing but `skipped`: t, parameters and states stay.  What is written
- * must overlap nothing else; gradients may share memory with each other.
+ * must overlap nothing else, lr_device and sumsq included; gradients may share
+ * memory with each other.
  * EDIT_EINVAL otherwise, before anything is enqueued. */
 edit_status_t edit_adamw_step(edit_adamw_t h, const edit_adamw_tensors_t *tensors, const edit_adamw_call_t *call,
                               void *stream);
@@ -594,8 +595,8 @@ edit_status_t edit_adamw_pack(edit_adamw_t h, const float *const *exp_avg, const
 edit_status_t edit_adamw_unpack(edit_adamw_t h, const edit_adamw_tensors_t *tensors, float *const *exp_avg,
                                 float *const *exp_avg_sq, void *stream);
 
-/* The record of the last call, after waiting for the handle's device; t (0 or
- * more) for a run that is resumed, likewise. */
+/* The record of the last call, after waiting for the handle's device; t (0 to
+ * 2^62) for a run that is resumed, likewise. */
 edit_status_t edit_adamw_state_get(edit_adamw_t h, edit_adamw_state_t *out);
 edit_status_t edit_adamw_state_set(edit_adamw_t h, int64_t step);
 

@@ -25,7 +25,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// The first 64 bits behind the point of sqrt(2) and of sqrt(3).
+// The first 64 bits behind the point of sqrt(2), the last one set, and of sqrt(3).
 constexpr uint64_t kMixA = 0x6A09E667F3BCC909ull, kMixB = 0xBB67AE8584CAA73Bull;
 
 __host__ __device__ __forceinline__ uint64_t mix(uint64_t z) {

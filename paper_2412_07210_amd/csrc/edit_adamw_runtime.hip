@@ -39,6 +39,7 @@ edit_status_t guarded(const F& f) {
 }
 
 constexpr int64_t kMaxNumel = int64_t(1) << 33;
+constexpr int64_t kMaxStep = int64_t(1) << 62;
 constexpr int64_t kMaxBlocks = (int64_t(1) << 32) / kAdamThreads - 1;  // of a launch: fewer than 2^32 threads
 static_assert(kMaxNumel / (kAdamThreads * 4) <= kMaxBlocks, "a tensor fits a launch");
 
@@ -311,7 +312,13 @@ edit_status_t step(edit_adamw* h, const edit_adamw_tensors_t* t, const edit_adam
     ADAM_TRY(note(h, 1, t->grad[k], gb * n, gb, "grad", k));
     ADAM_TRY(check_states(h, t, k));
   }
-  ADAM_TRY(check_overlaps(h, 0x3du));
+  constexpr unsigned writes = 0x3du;
+  ADAM_TRY(check_overlaps(h, writes));
+  for (const double* p : {call->lr_device, call->sumsq}) {
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+    if (p && h->ranges.written_at(writes, lo, lo + sizeof *p))
+      return afail(EDIT_EINVAL, "lr_device and sumsq must not overlap what is written");
+  }
 
   AdamCall c = {};
   c.lr = call->lr;
@@ -428,7 +435,7 @@ edit_status_t edit_adamw_state_get(edit_adamw_t h, edit_adamw_state_t* out) {
 
 edit_status_t edit_adamw_state_set(edit_adamw_t h, int64_t step) {
   if (!h) return afail(EDIT_EINVAL, "NULL handle");
-  if (step < 0) return afail(EDIT_EINVAL, "step must be >= 0");
+  if (step < 0 || step > kMaxStep) return afail(EDIT_EINVAL, "step must be in [0, 2^62]");
   ADAM_TRY(check_adamw_device(h));
   return guarded([&] {
     const std::vector<int64_t> steps(h->state.slots, step);

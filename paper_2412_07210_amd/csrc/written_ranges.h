@@ -60,6 +60,17 @@ class WrittenRanges {
     }
     return kOverlapNone;
   }
+  // Whether [lo, hi) meets a written buffer.  For the few buffers that lie anywhere,
+  // a number of the call, say: added above, they would have all of it sorted.
+  bool written_at(unsigned writes, uintptr_t lo, uintptr_t hi) const {
+    for (int i = 0; i < N; ++i) {
+      const Kind& a = kind_[i];
+      if (!(writes >> i & 1) || a.hi <= lo || hi <= a.lo) continue;
+      for (const Range& r : a.ranges)
+        if (r.lo < hi && lo < r.hi) return true;
+    }
+    return false;
+  }
 
  private:
   struct Range {

@@ -493,6 +493,8 @@ def test_refusals_change_nothing():
             run.opt.step(p, g, s, lr)
     with pytest.raises(EditOuterError, match="step must be"):
         run.opt.state_set(-1)
+    with pytest.raises(EditOuterError, match="step must be"):
+        run.opt.state_set(2 ** 62 + 1)
     with pytest.raises(ValueError, match=r"params\[0\]"):
         run.opt.step([p[0].cpu(), p[1]], g, s, 1e-3)
     assert run.opt.state_get().step == 0
@@ -508,6 +510,26 @@ def test_refusals_change_nothing():
     plain.close()
     with pytest.raises(EditOuterError, match="NULL handle"):
         plain.step([torch.zeros(600, device=DEV)], [torch.zeros(600, device=DEV)], plain.new_state(), 1e-3)
+
+
+@pytest.mark.parametrize("over", ["param", "exp_avg", "exp_avg_sq"])
+def test_numbers_read_on_the_device_are_not_written(over):
+    run = Run([600, 700], "f32", None, "f32", seed=16)
+    keep = run.snapshot()
+    buffer = {"param": run.flat_p[int(run.at[0]):], "exp_avg": run.state.exp_avg[1], "exp_avg_sq": run.state.exp_avg_sq[0]}[over]
+    skip = buffer.data_ptr() % 8 // 4
+    number = buffer[skip + 200:skip + 202].view(torch.float64)
+    for lr, sumsq in ((number, None), (1e-3, number)):
+        with pytest.raises(EditOuterError, match="lr_device and sumsq must not overlap") as e:
+            run.opt.step(run.params, run.grads, run.state, lr, sumsq=sumsq)
+        assert e.value.status == EDIT_EINVAL
+    assert run.opt.state_get().step == 0
+    assert all(torch.equal(x, y) for x, y in zip(run.snapshot(), keep))
+    # between the buffers, as an allocator may place it, is another matter
+    apart = torch.tensor([1e-3], dtype=torch.float64, device=DEV)
+    run.opt.step(run.params, run.grads, run.state, apart)
+    assert run.opt.state_get().step == 1
+    run.close()
 
 
 @pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two devices")

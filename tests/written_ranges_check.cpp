@@ -1,6 +1,7 @@
 // Drives WrittenRanges beside a comparison of every pair, over lists in order
 // and out of it, of kinds apart and mixed.  Prints how often it found none, a
-// written buffer met by a written one, and by a read one.
+// written buffer met by a written one, and by a read one; how often a stretch
+// met no written buffer, and one.
 #include <cstdio>
 #include <random>
 #include <vector>
@@ -15,7 +16,7 @@ struct One {
 int main() {
   constexpr int N = 6;
   std::mt19937 gen(7);
-  long found[3] = {0, 0, 0};
+  long found[3] = {0, 0, 0}, hit[2] = {0, 0};
   edit::WrittenRanges<N> set;
   set.reserve(64);
   for (int round = 0; round < 300000; ++round) {
@@ -51,7 +52,15 @@ int main() {
       return 1;
     }
     ++found[want];
+    const uintptr_t lo = gen() % (apart ? 4000 * N : span), hi = lo + 1 + gen() % 10;
+    bool met = false;
+    for (const One& a : list) met = met || ((writes >> a.kind & 1) && a.lo < hi && lo < a.hi);
+    if (set.written_at(writes, lo, hi) != met) {
+      std::printf("round %d: [%lu, %lu) %d\n", round, static_cast<unsigned long>(lo), static_cast<unsigned long>(hi), met);
+      return 1;
+    }
+    ++hit[met];
   }
-  std::printf("%ld %ld %ld\n", found[0], found[1], found[2]);
+  std::printf("%ld %ld %ld %ld %ld\n", found[0], found[1], found[2], hit[0], hit[1]);
   return 0;
 }
