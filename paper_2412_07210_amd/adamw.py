@@ -235,9 +235,10 @@ class AdamW:
                exp_avg_sq: Optional[Sequence[torch.Tensor]] = None, stream: Optional[torch.cuda.Stream] = None) -> tuple:
         """Enqueue the values of 8-bit states in fp32 (edit_adamw_unpack) and return (exp_avg, exp_avg_sq)."""
         tensors = _AdamWTensors(None, None, *self._state_pointers(state))
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
-            exp_avg = self._flat_views(torch.float32) if exp_avg is None else exp_avg
-            exp_avg_sq = self._flat_views(torch.float32) if exp_avg_sq is None else exp_avg_sq
+        if exp_avg is None or exp_avg_sq is None:
+            with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(self.device)):
+                exp_avg = self._flat_views(torch.float32) if exp_avg is None else exp_avg
+                exp_avg_sq = self._flat_views(torch.float32) if exp_avg_sq is None else exp_avg_sq
         self._call(self._lib.edit_adamw_unpack, "edit_adamw_unpack", ctypes.byref(tensors),
                    self._pointers(exp_avg, torch.float32, "exp_avg"),
                    self._pointers(exp_avg_sq, torch.float32, "exp_avg_sq"), _stream_handle(stream, self.device))
