@@ -486,6 +486,10 @@ void edit_ortho_destroy(edit_ortho_t h);
  * begin at any element (views into a flat unit) and are contiguous; states are
  * 16-byte aligned, scales 4-byte aligned.
  *
+ * A call is left out, and changes nothing but its count `skipped`, if its S is not
+ * finite (a call without max_norm and sumsq has none), or its lr is read on the
+ * device and is negative or not finite.  -0 is 0.
+ *
  * Precision.  S is summed in fp64, g' is rounded to fp32, m and v are taken in
  * fp64 and rounded once to fp32, and the step of p is taken in fp32 with one
  * rounding of p behind it: an fp32 p is off by half a place and 1e-6 of its
@@ -555,7 +559,9 @@ typedef struct {
 typedef struct {
   double lr;               /* finite and >= 0                                   */
   const double *lr_device; /* device: lr is read there when the call runs (a    */
-                           /* schedule under a captured graph); NULL: lr        */
+                           /* schedule under a captured graph), and one that is */
+                           /* negative or not finite leaves the call out; NULL: */
+                           /* lr                                                */
   double max_norm;         /* clips; finite, > 0; 0: no clip                    */
   const double *sumsq;     /* device: S, e.g. added up over a module's shards;  */
                            /* NULL: taken from grad where max_norm > 0          */
@@ -565,7 +571,7 @@ typedef struct {
 /* Of the last call that ran (host memory). */
 typedef struct {
   int64_t step;     /* t                                                      */
-  int64_t skipped;  /* calls left out: their S was not finite                 */
+  int64_t skipped;  /* calls left out: for their S, or lr on the device       */
   double norm;      /* sqrt(S) of the last call that had one                  */
   double clip_coef; /* c of the last call; 0 if it was left out               */
 } edit_adamw_state_t;
@@ -579,8 +585,7 @@ edit_status_t edit_adamw_init(const edit_adamw_config_t *cfg, edit_adamw_t *out)
 edit_status_t edit_adamw_sumsq(edit_adamw_t h, const void *const *grad, double *sumsq, void *stream);
 
 /* One step of all tensors, enqueued on `stream`, in place on parameters and
- * states.  If S is there (max_norm > 0 or sumsq) and not finite, the call
- * changes nothing but `skipped`: t, parameters and states stay.  What is written
+ * states, or left out (above): t, parameters and states stay.  What is written
  * must overlap nothing else, lr_device and sumsq included; gradients may share
  * memory with each other.
  * EDIT_EINVAL otherwise, before anything is enqueued. */

@@ -48,7 +48,7 @@ class AdamWState:
 @dataclass
 class AdamWRecord:
     step: int         # t
-    skipped: int      # calls left out: their gradients were not finite
+    skipped: int      # calls left out: their gradients were not finite, or their rate no rate
     norm: float       # of the last call that took one
     clip_coef: float  # c of the last call; 0 if it was left out
 
@@ -299,10 +299,10 @@ class AdamWPlan(GradPlan):
     def run(self, lr: Union[float, torch.Tensor], max_norm: Optional[float] = None, sumsq: Optional[torch.Tensor] = None,
             seed: int = 0, stream: Optional[torch.cuda.Stream] = None) -> None:
         """Enqueue one step (edit_adamw_step).  `lr`: a number, or one fp64
-        element on the device, read when the step runs.  `max_norm` clips the
-        gradients' norm; `sumsq` is its square where it covers more than these
-        gradients.  With either, gradients that are not finite leave the whole
-        call out.  `seed`: of the random numbers, which differ from step to step."""
+        element on the device, read when the step runs; one that is negative or not
+        finite leaves the whole call out.  `max_norm` clips the gradients' norm;
+        `sumsq` is its square where it covers more than these gradients.  With
+        either, gradients that are not finite leave the call out too.  `seed`: of the random numbers, which differ from step to step."""
         h = self._handle
         if max_norm is not None and not (max_norm > 0.0 and math.isfinite(max_norm)):
             raise ValueError("max_norm must be finite and > 0, or None")

@@ -79,7 +79,7 @@ constexpr int kAdamFusedBlocks = 2048;
 // one has counted on already); they are the same between calls.
 struct alignas(16) AdamRecord {
   int64_t step;      // t of the last call that was not left out
-  int64_t skipped;   // calls left out because the gradient's norm was not finite
+  int64_t skipped;   // calls left out because of the gradient's norm or the rate
   double norm;       // of the last call that took one
   double lr_decay;   // lr * weight_decay of this call
   uint64_t key;      // of this call's random numbers

@@ -359,24 +359,25 @@ __device__ __forceinline__ double power(double x, int64_t t) {
 
 // What call number t + 1 goes by, whose S is `s`; r holds the record before it.
 __device__ __forceinline__ void decide(double s, int64_t t, const AdamCall& call, const AdamHyper& hyper, AdamRecord& r) {
+  constexpr double largest = 1.7976931348623157e308;
+  const double lr = call.lr_device ? *call.lr_device : call.lr;
   float clip = 1.f;
-  r.skip = 0;
+  r.skip = !(lr >= 0.0 && lr <= largest);  // one on the device; the host refuses such a number
   if (call.count > 0) {
     r.norm = sqrt(s);
-    r.skip = !(r.norm <= 1.7976931348623157e308);
+    r.skip |= !(r.norm <= largest);
     if (!r.skip) clip = static_cast<float>(fmin(call.max_norm / (r.norm + EDIT_ADAMW_CLIP_EPS), 1.0));
   }
   if (r.skip) {
     r.skipped += 1;
     r.clip = 0.f;
   } else {
-    const double lr = call.lr_device ? *call.lr_device : call.lr;
     r.step = t + 1;
     r.clip = clip;
     r.lr_decay = lr * call.weight_decay;
-    // lr = 0 takes the largest numbers: a quotient of zero.  eps stays above what
-    // the reciprocal takes as zero, however large lr is.
-    const double most = 3.4028234663852886e38, over = fmax((1.0 - power(hyper.beta1, r.step)) / lr, 0.0);
+    // lr = 0 of either sign takes the largest numbers: a quotient of zero.  eps stays
+    // above what the reciprocal takes as zero, however large lr is.
+    const double most = 3.4028234663852886e38, over = lr > 0.0 ? (1.0 - power(hyper.beta1, r.step)) / lr : largest;
     r.root = static_cast<float>(fmin(over / sqrt(1.0 - power(hyper.beta2, r.step)), most));
     r.eps = static_cast<float>(fmin(fmax(over * hyper.eps, 1.2e-38), most));
     r.key = mix(mix(call.seed) + static_cast<uint64_t>(r.step));
