@@ -592,8 +592,8 @@ edit_status_t edit_adamw_sumsq(edit_adamw_t h, const void *const *grad, double *
 edit_status_t edit_adamw_step(edit_adamw_t h, const edit_adamw_tensors_t *tensors, const edit_adamw_call_t *call,
                               void *stream);
 
-/* fp32 states (16-byte aligned) to E4M3 ones as a step holds them, with t = 0 in
- * the random numbers, and back (exactly).  Handles of EDIT_ADAMW_E4M3; param and
+/* fp32 states (16-byte aligned) to E4M3 ones as a step holds them, v by its size
+ * (-0 is held as 0 is) and with t = 0 in the random numbers, and back (exactly).  Handles of EDIT_ADAMW_E4M3; param and
  * grad of `tensors` are not looked at.  Overlaps as in edit_adamw_step. */
 edit_status_t edit_adamw_pack(edit_adamw_t h, const float *const *exp_avg, const float *const *exp_avg_sq,
                               const edit_adamw_tensors_t *tensors, uint64_t seed, void *stream);

@@ -627,11 +627,11 @@ __device__ __forceinline__ void convert_block(const AdamTensor& t, int tensor, u
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         m[e] = element<false, V>(m_raw[u], e);
-        v[e] = element<false, V>(v_raw[u], e);
+        // -0 and a negative v, which no step makes, are taken by their size
+        v[e] = fabsf(element<false, V>(v_raw[u], e));
         word[e] = random_word(base ^ e, key.k1);
       }
-      // a negative v, which no step makes, is taken by its size
-      const uint32_t em = block_exponent<true>(m), ev = block_exponent<true>(v);
+      const uint32_t em = block_exponent<true>(m), ev = block_exponent<false>(v);
       store_codes<FULL, V>(vp, at[u], left, encode<true>(v, ev, word));
       store_codes<FULL, V>(mp, at[u], left, encode<false>(m, em, word));
       if (at[u] % EDIT_ADAMW_BLOCK == 0 && (FULL || at[u] < left)) {
