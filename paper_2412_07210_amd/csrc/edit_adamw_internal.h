@@ -116,7 +116,7 @@ struct AdamCall {
 // Block b works on the tensor whose first[] is the last one that is <= b.
 struct AdamTable {
   int32_t first[64];  // beyond the tensors: more than any block
-  float decay[kAdamTensors];
+  double decay[kAdamTensors];  // in 64 bits: with lambda it may be a number of fp32 where it alone is none
   AdamTensor tensor[kAdamTensors];
   int32_t base;  // index of tensor[0] among all
 };

@@ -441,7 +441,7 @@ __device__ __forceinline__ Key key_of(uint64_t key, int tensor, int64_t at) {
 // 792 (6.26), bf16 rounded stochastically in 514 (6.03), where the vector units
 // are busy for 85% of the time too (42 instructions an element; 44 took 2% more).
 template <bool FULL, bool PB, bool GB, bool HELD, bool SR, int V, int U>
-__device__ __forceinline__ void step_block(const AdamTensor& t, float decay_factor, int tensor, const AdamHyper& hyper,
+__device__ __forceinline__ void step_block(const AdamTensor& t, double decay_factor, int tensor, const AdamHyper& hyper,
                                            const AdamRecord& rec, int64_t begin) {
   if (rec.skip) return;  // here, so that the record is loaded beside the tensor's entry
   void* const pp = element_at<PB>(t.param, begin);
@@ -530,7 +530,7 @@ template <bool PB, bool GB, bool HELD, bool SR, int V, int U>
 __device__ __forceinline__ void step_tensor(const AdamTable& tab, const Place& place, const AdamHyper& hyper,
                                             const AdamRecord& r) {
   const AdamTensor t = tab.tensor[place.k];
-  const float decay = tab.decay[place.k];
+  const double decay = tab.decay[place.k];
   if (place.at + kAdamThreads * V * U <= t.numel) {
     step_block<true, PB, GB, HELD, SR, V, U>(t, decay, tab.base + place.k, hyper, r, place.at);
   } else {

@@ -51,7 +51,7 @@ constexpr int kKinds = 6;  // parameters, gradients, m, v and their scales; of a
 
 struct edit_adamw {
   std::vector<int64_t> numel;
-  std::vector<float> decay;
+  std::vector<double> decay;
   AdamKind kind{};
   AdamHyper hyper{};
   double weight_decay = 0.0;
@@ -365,8 +365,8 @@ edit_status_t edit_adamw_init(const edit_adamw_config_t* cfg, edit_adamw_t* out)
     auto h = std::make_unique<edit_adamw>();
     const size_t tensors = static_cast<size_t>(cfg->num_tensors);
     h->numel.assign(cfg->numel, cfg->numel + tensors);
-    h->decay.assign(tensors, 1.f);
-    for (size_t k = 0; cfg->decay && k < tensors; ++k) h->decay[k] = static_cast<float>(cfg->decay[k]);
+    h->decay.assign(tensors, 1.0);
+    if (cfg->decay) h->decay.assign(cfg->decay, cfg->decay + tensors);
     h->kind.param_bf16 = cfg->dtype == EDIT_BF16;
     h->kind.grad_bf16 = cfg->grad_dtype == EDIT_BF16;
     h->kind.held = cfg->held == EDIT_ADAMW_E4M3;

@@ -5,7 +5,7 @@ import torch
 
 import adamw_reference as ref
 from paper_2412_07210_amd import AdamW, AdamWConfig
-from test_gpu_adamw import DEV, randn
+from test_gpu_adamw import DEV, Run, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,17 @@ def test_pack_takes_v_by_its_size(n):
     opt.step(p, [torch.zeros(n, device=DEV)], state, 1e-3)
     assert torch.isfinite(p[0].cpu()[torch.from_numpy(fine)]).all()
     opt.close()
+
+
+@pytest.mark.parametrize("missing", [(), (1,)], ids=["fused", "apart"])
+@pytest.mark.parametrize("state", ["f32", "e4m3"])
+@pytest.mark.parametrize("factor,decay", [(1e39, 0.0), (1e300, 0.0), (1e40, 1e-41), (1e-46, 1e45), (2.5, 0.1)])
+def test_decay_factors_of_any_size(state, factor, decay, missing):
+    """lambda d_k is taken in 64 bits: factors beyond fp32's range are factors."""
+    run = Run([700, 300, 5000], "f32", None, state, seed=33, no_grad=missing, weight_decay=decay, decay=[factor] * 3)
+    old, g = run.params[0].double().cpu().numpy(), run.grads[0].cpu().numpy()
+    run.opt.step(run.params, run.grads, run.state, 1e-2)
+    p, _, _, step, _ = ref.step64(old, g, np.zeros(700), np.zeros(700), 1, 1e-2, (0.9, 0.95), 1e-8, decay * factor, 1.0)
+    assert np.isfinite(p).all()
+    ref.assert_params(run.params[0], p, step, f"{factor} {decay}")
+    run.close()
