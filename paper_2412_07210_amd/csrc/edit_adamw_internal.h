@@ -86,6 +86,7 @@ struct alignas(16) AdamRecord {
   float clip;        // c
   float root, eps;   // 1 / sqrt(1 - beta2^t) and eps, over lr / (1 - beta1^t)
   int32_t skip;      // this call changes nothing
+  int32_t tiny;      // roots of v below 2^-126 show beside eps
 };
 
 struct AdamTensor {

@@ -378,8 +378,12 @@ __device__ __forceinline__ void decide(double s, int64_t t, const AdamCall& call
     // lr = 0 of either sign takes the largest numbers: a quotient of zero.  eps stays
     // above what the reciprocal takes as zero, however large lr is.
     const double most = 3.4028234663852886e38, over = lr > 0.0 ? (1.0 - power(hyper.beta1, r.step)) / lr : largest;
-    r.root = static_cast<float>(fmin(over / sqrt(1.0 - power(hyper.beta2, r.step)), most));
+    const double scale = 1.0 / sqrt(1.0 - power(hyper.beta2, r.step));
+    r.root = static_cast<float>(fmin(over * scale, most));
     r.eps = static_cast<float>(fmin(fmax(over * hyper.eps, 1.2e-38), most));
+    // 2^-63 / sqrt(1 - beta2^t), the largest of them, is 2^-24 of eps at least: with
+    // an eps of 1e-8 only for beta2 next to 1
+    r.tiny = scale > hyper.eps * 0x1p39;
     r.key = mix(mix(call.seed) + static_cast<uint64_t>(r.step));
   }
 }
@@ -496,11 +500,22 @@ __device__ __forceinline__ void step_block(const AdamTensor& t, double decay_fac
       const double g = clip * element<GB, V>(g_raw[u], e);
       m[e] = static_cast<float>(__builtin_fma(keep1, static_cast<double>(m[e]), a1 * g));
       v[e] = static_cast<float>(__builtin_fma(keep2, static_cast<double>(v[e]), a2 * g * g));
-      // The hardware's square root is off by one place and takes values below
-      // 2^-126 as zero; beside an eps of 1e-12 at least neither is seen in p.
-      const float d = __builtin_fmaf(__builtin_amdgcn_sqrtf(v[e]), root, eps);
-      p[e] -= __builtin_fmaf(decay, p[e], m[e] * __builtin_amdgcn_rcpf(d));
     }
+    // The hardware's square root is off by one place and takes values below 2^-126
+    // as zero.
+    auto update = [&](auto tiny) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const bool up = tiny && v[e] < 0x1p-126f;
+        const float s = __builtin_amdgcn_sqrtf(up ? v[e] * 0x1p64f : v[e]);
+        const float d = __builtin_fmaf(up ? s * 0x1p-32f : s, root, eps);
+        p[e] -= __builtin_fmaf(decay, p[e], m[e] * __builtin_amdgcn_rcpf(d));
+      }
+    };
+    if (__builtin_expect(rec.tiny, 0))  // all lanes alike
+      update(std::true_type{});
+    else
+      update(std::false_type{});
     uint32_t word[V], second[V];
     if constexpr (HELD || SR) {
       const uint32_t base = (static_cast<uint32_t>(begin) + at[u]) ^ key.k0;  // both are multiples of V: + e is ^ e
@@ -586,6 +601,7 @@ __global__ __launch_bounds__(kAdamThreads, 4) void adamw_fused_kernel(const Adam
     }
   }
   r.skip = __builtin_amdgcn_readfirstlane(r.skip);
+  r.tiny = __builtin_amdgcn_readfirstlane(r.tiny);
   r.clip = same(r.clip), r.root = same(r.root), r.eps = same(r.eps);
   r.lr_decay = same(r.lr_decay), r.key = same(r.key);
   step_tensor<PB, GB, HELD, SR, V, U>(tab, place, hyper, r);

@@ -51,3 +51,17 @@ def test_decay_factors_of_any_size(state, factor, decay, missing):
     assert np.isfinite(p).all()
     ref.assert_params(run.params[0], p, step, f"{factor} {decay}")
     run.close()
+
+
+@pytest.mark.parametrize("std", [1e-21, 1e-19, 1e-18, 1e-17])
+@pytest.mark.parametrize("beta2", [0.95, 0.999, 0.9999, 0.999999])
+@pytest.mark.parametrize("state", ["f32", "e4m3"])
+def test_steps_where_the_roots_argument_is_subnormal(state, beta2, std):
+    """With the smallest eps and few steps taken, sqrt(v / (1 - beta2^t)) of a v below
+    2^-126 shows beside eps.  Parameters of zero: the step is all that is compared."""
+    run = Run([3000, 257], "f32", None, state, seed=34, std=std, eps=1e-12, betas=(0.9, beta2))
+    for t in range(3):
+        run.draw(t)
+        run.flat_p.zero_()
+        run.step(lr=1e4)
+    run.close()
