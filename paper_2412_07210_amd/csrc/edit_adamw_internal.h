@@ -19,25 +19,25 @@ constexpr int kAdamDecideThreads = 512;
 // times, the next V beside its neighbour's: a block V * U * 64.  Eight bf16 and
 // eight codes are 16 and 8 bytes; with fp32 buffers four, as 16-byte accesses
 // 32 bytes apart run at half the rate.  Twice for 8-bit states, whose loads are
-// short, once for fp32 ones.  us for 308M elements at the best cap below: e4m3
-// states with bf16 parameters and gradients, V U = 8 1 and 8 2, 520 and 514 (4 2
-// 10% more); fp32 and bf16, 8 1, 4 1 and 4 2, 770, 686 and 690; fp32 states, 4 1
-// and 4 2: bf16 1028 and 1053, fp32 1294 and 1374.  Blocks of 256 threads take 0
-// to 2% more.
+// short, once for fp32 ones.  us for 308M elements at the cap below: e4m3 states with
+// bf16 parameters and gradients, V U = 8 1, 8 2 and 4 2, 517, 502 and 556; fp32 and
+// bf16, 4 1 and 4 2, 715 and 699 (8 1 10% more); fp32 states, 4 1 and 4 2: bf16 1045 and
+// 1098, fp32 1311 and 1415.  Blocks of 256 threads take 0 to 2% more.
 constexpr int adamw_vec(bool param_bf16, bool grad_bf16, bool held) { return param_bf16 && grad_bf16 && held ? 8 : 4; }
 constexpr int adamw_times(bool held) { return held ? 2 : 1; }
 constexpr int adamw_chunk(bool param_bf16, bool grad_bf16, bool held) {
   return kAdamThreads * adamw_vec(param_bf16, grad_bf16, held) * adamw_times(held);
 }
-// Blocks of it that run on a CU, of the 32 that fit: the mix of reads and writes
-// runs faster with fewer of its loads in flight.  us uncapped, capped and (two
-// blocks a CU more and fewer): e4m3 states: bf16 521, 514 (520, 516); bf16 and
-// fp32 gradients 599, none (616 at 22); fp32 and bf16 709, 690 (691, 696); fp32
-// 813, 792 (793, 798).  fp32 states: bf16 1105, 1028 (1040, 1028); bf16 and fp32
-// 1199, 1129 (1143, 1152); fp32 and bf16 1309, 1221 (1231, 1224); fp32 1404, 1294
-// (1305, 1307).
+// Blocks of it that run on a CU: the mix of reads and writes runs faster with fewer
+// of its loads in flight.  Registers leave room for 32, with bf16 and e4m3 states for
+// 24 (20 rounded to nearest); LDS, handed out in whole pieces, for 25, 21, 18, 16, 14,
+// 12 or 11.  32: no cap.  us for 308M elements uncapped, capped and (at the nearest
+// numbers above and below): e4m3 states: bf16 506, none (505 at 25, 511 at 21); bf16
+// and fp32 gradients 602, none (610 at 25); fp32 and bf16 724, 699 (704, 701); fp32
+// 821, 787 (791, 792).  fp32 states: bf16 1089, 1040 (1047, 1047); bf16 and fp32 1187,
+// 1124 (1133, 1142); fp32 and bf16 1286, 1219 (1224, 1226); fp32 1408, 1309 (1322, 1316).
 constexpr int adamw_resident(bool param_bf16, bool grad_bf16, bool held) {
-  if (held) return param_bf16 ? (grad_bf16 ? 22 : 32) : grad_bf16 ? 20 : 18;
+  if (held) return param_bf16 ? 32 : grad_bf16 ? 21 : 18;
   return param_bf16 && grad_bf16 ? 16 : param_bf16 || grad_bf16 ? 14 : 12;
 }
 // Conversions: a lane takes four elements once to pack (308M elements in 458 us,

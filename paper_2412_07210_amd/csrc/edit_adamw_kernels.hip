@@ -692,6 +692,7 @@ hipError_t step(int blocks, const AdamTable& table, const AdamHyper& hyper, cons
                 int before, hipStream_t stream) {
   constexpr int V = adamw_vec(PB, GB, HELD), U = adamw_times(HELD), resident = adamw_resident(PB, GB, HELD);
   constexpr int lds = resident == 32 ? 0 : lds_for_blocks(resident, 0, kLdsPerCu);
+  static_assert(resident == 32 || lds_blocks(lds, kLdsPerCu) == resident, "a number that LDS can leave room for");
   if (call)
     return launch<AdamTable, AdamHyper, AdamCall, AdamState, int>(adamw_fused_kernel<PB, GB, HELD, SR, V, U>, blocks, kAdamThreads,
                                                                   lds, stream, table, hyper, *call, state, before);
@@ -743,10 +744,11 @@ hipError_t launch_adamw_step(const AdamKind& kind, int blocks, const AdamTable& 
 }
 
 hipError_t launch_adamw_convert(bool pack, int blocks, const AdamTable& table, uint64_t key, hipStream_t stream) {
+  constexpr int lds = lds_for_blocks(kAdamUnpackResident, 0, kLdsPerCu);
+  static_assert(lds_blocks(lds, kLdsPerCu) == kAdamUnpackResident, "a number that LDS can leave room for");
   return launch<AdamTable, uint64_t>(pack ? adamw_convert_kernel<true, 4, adamw_convert_times(true)>
                                           : adamw_convert_kernel<false, 4, adamw_convert_times(false)>,
-                                     blocks, kAdamThreads, pack ? 0 : lds_for_blocks(kAdamUnpackResident, 0, kLdsPerCu), stream,
-                                     table, key);
+                                     blocks, kAdamThreads, pack ? 0 : lds, stream, table, key);
 }
 
 }  // namespace edit
