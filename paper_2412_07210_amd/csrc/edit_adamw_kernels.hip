@@ -440,10 +440,11 @@ __device__ __forceinline__ Key key_of(uint64_t key, int tensor, int64_t at) {
 
 // The work of one block: U times V elements a lane of every buffer, each time
 // next to its neighbour's; FULL: all of them are there.  Bound by memory, which
-// moves what the formulas need and 1 to 3% more: 308M elements in fp32 in 1294 us
-// (6.67 TB/s), in bf16 with fp32 states in 1028 (6.60); with e4m3 states fp32 in
-// 792 (6.26), bf16 rounded stochastically in 514 (6.03), where the vector units
-// are busy for 85% of the time too (42 instructions an element; 44 took 2% more).
+// moves what the formulas need and up to 4% more (whole lines for a block's few
+// scales): 308M elements in fp32 in 1309 us (6.59 TB/s), in bf16 with fp32 states in
+// 1040 (6.52); with e4m3 states fp32 in 787 (6.29), bf16 rounded stochastically in 502
+// (6.18), where the vector units are busy for 85% of the time too (43 instructions an
+// element; two more took 2% more).
 template <bool FULL, bool PB, bool GB, bool HELD, bool SR, int V, int U>
 __device__ __forceinline__ void step_block(const AdamTensor& t, double decay_factor, int tensor, const AdamHyper& hyper,
                                            const AdamRecord& rec, int64_t begin) {
