@@ -488,7 +488,7 @@ void edit_ortho_destroy(edit_ortho_t h);
  *
  * A call is left out, and changes nothing but its count `skipped`, if its S is not
  * finite (a call without max_norm and sumsq has none), or its lr is read on the
- * device and is negative or not finite.  -0 is 0.
+ * device and is negative or not finite.  A rate of -0 is one of 0.
  *
  * Precision.  S is summed in fp64, g' is rounded to fp32, m and v are taken in
  * fp64 and rounded once to fp32, and the step of p is taken in fp32 with one
@@ -587,14 +587,14 @@ edit_status_t edit_adamw_sumsq(edit_adamw_t h, const void *const *grad, double *
 /* One step of all tensors, enqueued on `stream`, in place on parameters and
  * states, or left out (above): t, parameters and states stay.  What is written
  * must overlap nothing else, lr_device and sumsq included; gradients may share
- * memory with each other.
- * EDIT_EINVAL otherwise, before anything is enqueued. */
+ * memory with each other.  EDIT_EINVAL otherwise, before anything is enqueued. */
 edit_status_t edit_adamw_step(edit_adamw_t h, const edit_adamw_tensors_t *tensors, const edit_adamw_call_t *call,
                               void *stream);
 
 /* fp32 states (16-byte aligned) to E4M3 ones as a step holds them, v by its size
- * (-0 is held as 0 is) and with t = 0 in the random numbers, and back (exactly).  Handles of EDIT_ADAMW_E4M3; param and
- * grad of `tensors` are not looked at.  Overlaps as in edit_adamw_step. */
+ * (-0 is held as 0 is) and with t = 0 in the random numbers, and back (exactly).
+ * Handles of EDIT_ADAMW_E4M3; param and grad of `tensors` are not looked at.
+ * Overlaps as in edit_adamw_step. */
 edit_status_t edit_adamw_pack(edit_adamw_t h, const float *const *exp_avg, const float *const *exp_avg_sq,
                               const edit_adamw_tensors_t *tensors, uint64_t seed, void *stream);
 edit_status_t edit_adamw_unpack(edit_adamw_t h, const edit_adamw_tensors_t *tensors, float *const *exp_avg,

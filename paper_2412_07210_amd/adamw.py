@@ -302,7 +302,8 @@ class AdamWPlan(GradPlan):
         element on the device, read when the step runs; one that is negative or not
         finite leaves the whole call out.  `max_norm` clips the gradients' norm;
         `sumsq` is its square where it covers more than these gradients.  With
-        either, gradients that are not finite leave the call out too.  `seed`: of the random numbers, which differ from step to step."""
+        either, gradients that are not finite leave the call out too.  `seed`: of
+        the random numbers, which differ from step to step."""
         h = self._handle
         if max_norm is not None and not (max_norm > 0.0 and math.isfinite(max_norm)):
             raise ValueError("max_norm must be finite and > 0, or None")

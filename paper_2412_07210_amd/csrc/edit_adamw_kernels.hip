@@ -381,8 +381,8 @@ __device__ __forceinline__ void decide(double s, int64_t t, const AdamCall& call
     const double scale = 1.0 / sqrt(1.0 - power(hyper.beta2, r.step));
     r.root = static_cast<float>(fmin(over * scale, most));
     r.eps = static_cast<float>(fmin(fmax(over * hyper.eps, 1.2e-38), most));
-    // 2^-63 / sqrt(1 - beta2^t), the largest of them, is 2^-24 of eps at least: with
-    // an eps of 1e-8 only for beta2 next to 1
+    // Such a root is below 2^-63: whether, over sqrt(1 - beta2^t), that is above 2^-24
+    // of eps.  With an eps of 1e-8 only for beta2 next to 1.
     r.tiny = scale > hyper.eps * 0x1p39;
     r.key = mix(mix(call.seed) + static_cast<uint64_t>(r.step));
   }
